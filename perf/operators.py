@@ -231,8 +231,7 @@ def prepare(case, seed):
         state["entropy"] = torch.empty(M, device="cuda")
         state["top_ids"] = torch.empty((M, case["k"]), dtype=torch.int32, device="cuda")
         state["top_logprobs"] = torch.empty((M, case["k"]), device="cuda")
-    if kind != "quantize":
-        state["workspace"] = torch.empty(1 << 25, dtype=torch.uint8, device="cuda")
+        state["workspace"] = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
     return state
 
 
@@ -310,12 +309,12 @@ def run(st):
         return dict(values=st["codes"][:, :cols] * st["steps"][:, None], steps=st["steps"])
     if kind == "product":
         B.ocs_qgemm_rows(st["xq"], st["pitch"], st["wq"], st["pitch"], M, st["N"], st["Ke"], 8, st["bits_w"], st["xstep"],
-                         st["wstep"], st.get("bias"), st["y"], st["N"], st["workspace"])
+                         st["wstep"], st.get("bias"), st["y"], st["N"])
         return st["y"]
     if kind in ("forward", "score"):
         B.ocs_forward_rows(st["x"], M, st["C"], 1, st["x"].stride(0), st["src"], st["Ke"] - st["C"], 8, 1.0, st["codes"],
                            st["pitch"], st["steps"], st["wq"], st["pitch"], st["N"], st["bits_w"], st["wstep"],
-                           st.get("bias"), st["y"], st["N"], st["workspace"])
+                           st.get("bias"), st["y"], st["N"])
         if kind == "forward":
             return st["y"]
     x = st["y"] if kind == "score" else st["x"]
