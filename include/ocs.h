@@ -68,9 +68,17 @@ extern "C" {
 #define OCS_E_HIP (-8)       /* a HIP call failed; ocs_last_hip_error() has the text         */
 #define OCS_E_MODE (-9)      /* unknown mode                                                 */
 #define OCS_E_CLIP (-10)     /* clip_ratio is not a positive finite number                   */
+#define OCS_E_TYPE (-11)     /* unknown element type                                         */
+#define OCS_E_TOP (-12)      /* top_k negative, above OCS_MAX_TOP or above the row's length   */
 
 #define OCS_MODE_HALVE 0 /* choose channels on this tensor and halve both copies (Eq. 3)     */
 #define OCS_MODE_DUP 1   /* channel choice given; copy channels un-halved (Eq. 4, weights)   */
+
+#define OCS_F32 0  /* element types of the calls with a grid per row and of token scoring      */
+#define OCS_BF16 1
+#define OCS_F16 2
+
+#define OCS_MAX_TOP 32 /* most alternatives per row of ocs_token_logprobs                       */
 
 #define OCS_MAX_EXPANDED_CHANNELS 8000  /* C + num_splits may not exceed this                */
 
@@ -486,6 +494,60 @@ int ocs_duplicate_weight_codes(int8_t *Wq, int64_t ldq, int64_t N, int C, int g,
 int ocs_fold_weights(const int8_t *Wq, int64_t ldq, int64_t N, int C, int g, int num_splits,
                      const int32_t *chan_src, int8_t *Wf, int64_t ldf, int32_t *max_abs_out,
                      void *stream);
+
+/*
+ * Layers with a grid per row: every row of X (a token) and every row of W (an output channel) has a
+ * threshold and a step of its own, where the calls above share one over the tensor.  One outlier token
+ * then costs only itself precision.  M = 0 (no tokens) is OCS_OK and launches nothing.
+ *
+ * ocs_split_quantize_rows: X [M, C*g] of element type `type` (OCS_F32, OCS_BF16, OCS_F16), any ldx >= C*g,
+ *   base aligned to its element -> codes of the expanded rows.  For expanded column j*g + t of row m
+ *        x' = X[m, chan_src[j]*g + t] * 2^-chan_depth[j]           (fp32; chan_depth NULL: no factor)
+ *        T_m = clip_ratio * max |x'| over the row,  step_out[m] = T_m / qmax,  qmax = 2^(bits-1) - 1
+ *        Xq[m, .] = Eq. 1's code of x' on the grid of T_m, pad columns zero
+ *   with the arithmetic of ocs_quantize on that row alone (a row of zeros: step 0, codes 0).
+ *   chan_src [C + num_splits] as the selection writes it: its first C entries are 0 .. C-1 (NULL with
+ *   num_splits = 0).  Activations of Eq. 3 take chan_depth = NULL; weights [N, C*g] take the selection's
+ *   chan_src and chan_depth and give codes with a step per output channel.
+ *   A row with NaN or an infinity: its step is not finite and its codes are unspecified, other rows are as without.
+ *   Xq: ldq >= (C + num_splits)*g, a multiple of OCS_CALIGN, 16-byte aligned base.  step_out: M floats.
+ *
+ * ocs_qgemm_rows: Y[m, n] = acc * (step_x[m] * step_w[n]) + bias[n] with acc as ocs_qgemm's, exact in 32 bits, the rest in fp32
+ *   (the factor first, then the product, then the sum), rounded once to out_type; bias [N] fp32 or NULL.
+ *   Codes: pitches as for ocs_qgemm.  Y: any ldy >= N, base aligned to its element.
+ *
+ * ocs_forward_rows: the two as one call (weight OCS, Eq. 3: activations' copies un-scaled), Xq and step_x_out left
+ *   as ocs_split_quantize_rows leaves them, Y as ocs_qgemm_rows does, bit for bit; `type` is X's and Y's is `out_type`.
+ */
+int ocs_split_quantize_rows(const void *X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t *chan_src,
+                            const int32_t *chan_depth, int num_splits, int bits, float clip_ratio, int8_t *Xq,
+                            int64_t ldq, float *step_out, void *stream);
+int ocs_qgemm_rows(const int8_t *Xq, int64_t ldx, const int8_t *Wq, int64_t ldw, int64_t M, int64_t N, int64_t Kexp,
+                   int bits_x, int bits_w, const float *step_x, const float *step_w, const float *bias, void *Y,
+                   int out_type, int64_t ldy, void *stream);
+int ocs_forward_rows(const void *X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t *chan_src, int num_splits,
+                     int bits_x, float clip_ratio, int8_t *Xq, int64_t ldq, float *step_x_out, const int8_t *Wq,
+                     int64_t ldw, int64_t N, int bits_w, const float *step_w, const float *bias, void *Y, int out_type,
+                     int64_t ldy, void *stream);
+
+/*
+ * Scoring of tokens: what a language model is judged by (perplexity is exp of the mean of -logprob).
+ *   logits [M, V] of element type `type`, any ld >= V, base aligned to its element; p = softmax of a row in fp32.
+ *   tokens [M] int32 (may be NULL): logprob[m] = log p[tokens[m]]; a token outside 0 .. V-1 marks a position
+ *        without one (padding) and gets logprob 0.
+ *   entropy [M] (may be NULL): -sum p log p in nats.
+ *   top_ids, top_logprobs [M, top_k] (dense; NULL with top_k = 0): the top_k most likely tokens by logit,
+ *        descending, the lowest index first among equals (-0 and +0 are equal).  0 <= top_k <= min(V, OCS_MAX_TOP).
+ *   A logit of -inf is a token ruled out: log p = -inf, no part of the sums.  A row with nothing left: every
+ *   log p = -inf, entropy 0, alternatives 0, 1, 2, ...  A row with NaN or +inf: every value NaN (but for a position without a
+ *   token, whose logprob stays 0), ids by logit with NaN ahead of everything.
+ *   workspace: at least ocs_token_logprobs_workspace_bytes(M, V, top_k) bytes, 256-byte aligned; it may be NULL where that is 0.
+ *        Needs no initialisation.  M = 0 is OCS_OK and launches nothing.
+ */
+size_t ocs_token_logprobs_workspace_bytes(int64_t M, int64_t V, int top_k);
+int ocs_token_logprobs(const void *logits, int type, int64_t M, int64_t V, int64_t ld, const int32_t *tokens, int top_k,
+                       float *logprob, float *entropy, int32_t *top_ids, float *top_logprobs, void *workspace,
+                       size_t ws_bytes, void *stream);
 
 /*
  * Measurement helper (no passage of the paper).  Arms a pair of caller-created hipEvent_t

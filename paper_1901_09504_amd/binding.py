@@ -16,6 +16,8 @@ KALIGN = 64
 MODE_HALVE = 0
 MODE_DUP = 1
 MAX_EXPANDED_CHANNELS = 8000
+MAX_TOP = 32
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # OCS_F32, OCS_BF16, OCS_F16
 
 
 class OcsError(RuntimeError):
@@ -119,6 +121,17 @@ def lib():
     L.ocs_split_act_qgemm.restype = _i32
     L.ocs_split_act_qgemm.argtypes = [_vp, _i64, _i32, _i32, _i64, _vp, _i32, _i32, _vp, _vp, _i64, _i64, _i32, _vp,
                                       _vp, _vp, _i64, _vp, _i64, _vp]
+    L.ocs_split_quantize_rows.restype = _i32
+    L.ocs_split_quantize_rows.argtypes = [_vp, _i32, _i64, _i32, _i32, _i64, _vp, _vp, _i32, _i32, _f32, _vp, _i64, _vp, _vp]
+    L.ocs_qgemm_rows.restype = _i32
+    L.ocs_qgemm_rows.argtypes = [_vp, _i64, _vp, _i64, _i64, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _i64, _vp]
+    L.ocs_forward_rows.restype = _i32
+    L.ocs_forward_rows.argtypes = [_vp, _i32, _i64, _i32, _i32, _i64, _vp, _i32, _i32, _f32, _vp, _i64, _vp, _vp, _i64, _i64,
+                                   _i32, _vp, _vp, _vp, _i32, _i64, _vp]
+    L.ocs_token_logprobs_workspace_bytes.restype = _sz
+    L.ocs_token_logprobs_workspace_bytes.argtypes = [_i64, _i64, _i32]
+    L.ocs_token_logprobs.restype = _i32
+    L.ocs_token_logprobs.argtypes = [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
     L.ocs_time_next.restype = _i32
     L.ocs_time_next.argtypes = [_i32, _vp, _vp]
     L.ocs_calib_copy.restype = _i32
@@ -413,3 +426,41 @@ def ocs_qgemm_split_k(Xq, ldx, Wq, ldw, M, N, Kexp, bits_x, bits_w, scale_x, sca
     _check(lib().ocs_qgemm_split_k(_ptr(Xq), ldx, _ptr(Wq), ldw, M, N, Kexp, bits_x, bits_w, _ptr(scale_x),
                                    _ptr(scale_w), _ptr(acc_out), ldacc, _ptr(Y), ldy, int(parts), w, wb,
                                    _stream(stream)), "ocs_qgemm_split_k")
+
+
+# ---- a grid per row, and the scoring of tokens (element types are the tensors' own) ------------
+
+def _type(t):
+    return -1 if t is None else TYPES.get(t.dtype, -1)
+
+
+def _bias(t):
+    """bias: fp32 [N], or None or False for a layer without."""
+    return None if t is None or t is False else t.data_ptr()
+
+
+def ocs_split_quantize_rows(X, M, Cn, g, ldx, chan_src, chan_depth, num_splits, bits, clip_ratio, Xq, ldq, step_out, stream=None):
+    _check(lib().ocs_split_quantize_rows(_ptr(X), _type(X), M, Cn, g, ldx, _ptr(chan_src), _ptr(chan_depth), num_splits, bits,
+                                         clip_ratio, _ptr(Xq), ldq, _ptr(step_out), _stream(stream)), "ocs_split_quantize_rows")
+
+
+def ocs_qgemm_rows(Xq, ldx, Wq, ldw, M, N, Kexp, bits_x, bits_w, step_x, step_w, bias, Y, ldy, stream=None):
+    _check(lib().ocs_qgemm_rows(_ptr(Xq), ldx, _ptr(Wq), ldw, M, N, Kexp, bits_x, bits_w, _ptr(step_x), _ptr(step_w), _bias(bias),
+                                _ptr(Y), _type(Y), ldy, _stream(stream)), "ocs_qgemm_rows")
+
+
+def ocs_forward_rows(X, M, Cn, g, ldx, chan_src, num_splits, bits_x, clip_ratio, Xq, ldq, step_x_out, Wq, ldw, N, bits_w, step_w,
+                     bias, Y, ldy, stream=None):
+    _check(lib().ocs_forward_rows(_ptr(X), _type(X), M, Cn, g, ldx, _ptr(chan_src), num_splits, bits_x, clip_ratio, _ptr(Xq), ldq,
+                                  _ptr(step_x_out), _ptr(Wq), ldw, N, bits_w, _ptr(step_w), _bias(bias), _ptr(Y), _type(Y), ldy,
+                                  _stream(stream)), "ocs_forward_rows")
+
+
+def ocs_token_logprobs_workspace_bytes(M, V, top_k):
+    return int(lib().ocs_token_logprobs_workspace_bytes(int(M), int(V), int(top_k)))
+
+
+def ocs_token_logprobs(logits, M, V, ld, tokens, top_k, logprob, entropy, top_ids, top_logprobs, workspace=None, stream=None):
+    w, wb = _ws(workspace)
+    _check(lib().ocs_token_logprobs(_ptr(logits), _type(logits), M, V, ld, _ptr(tokens), top_k, _ptr(logprob), _ptr(entropy),
+                                    _ptr(top_ids), _ptr(top_logprobs), w, wb, _stream(stream)), "ocs_token_logprobs")

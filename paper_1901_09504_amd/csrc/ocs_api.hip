@@ -116,6 +116,8 @@ const char* ocs_strerror(int code) {
         case OCS_E_HIP: return "a HIP call failed (see ocs_last_hip_error)";
         case OCS_E_MODE: return "unknown mode or key";
         case OCS_E_CLIP: return "clip_ratio is not a positive finite number";
+        case OCS_E_TYPE: return "unknown element type";
+        case OCS_E_TOP: return "top_k negative, above OCS_MAX_TOP or above the row's length";
         default: return "unknown error code";
     }
 }
@@ -939,6 +941,120 @@ int ocs_fold_weights(const int8_t* Wq, int64_t ldq, int64_t N, int C, int g, int
                                        static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e);
     return OCS_OK;
+}
+
+// ---- a grid per row --------------------------------------------------------------------------
+
+static bool type_ok(int type) { return type == OCS_F32 || type == OCS_BF16 || type == OCS_F16; }
+static size_t type_bytes(int type) { return type == OCS_F32 ? 4 : 2; }
+
+// M = 0: what holds a row each may be NULL, everything else is checked as for one row.
+static int check_row_grids(const void* X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t* chan_src, int num_splits,
+                           int bits, float clip_ratio, const int8_t* Xq, int64_t ldq, const float* step) {
+    if ((M != 0 && (!X || !Xq || !step)) || (num_splits > 0 && !chan_src)) return OCS_E_NULL;
+    if (!type_ok(type)) return OCS_E_TYPE;
+    int rc = check_layer(M == 0 ? 1 : M, C, g, ldx, num_splits);
+    if (rc) return rc;
+    const int64_t Ke = (int64_t)(C + num_splits) * g;
+    if (Ke > (int64_t)1 << 30) return OCS_E_SHAPE;
+    rc = check_codes(Xq, ldq, Ke);
+    if (rc) return rc;
+    if (!aligned(X, type_bytes(type)) || !aligned(step, 4)) return OCS_E_ALIGN;
+    if (!bits_ok(bits)) return OCS_E_BITS;
+    if (!clip_ok(clip_ratio)) return OCS_E_CLIP;
+    return OCS_OK;
+}
+
+int ocs_split_quantize_rows(const void* X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t* chan_src,
+                            const int32_t* chan_depth, int num_splits, int bits, float clip_ratio, int8_t* Xq,
+                            int64_t ldq, float* step_out, void* stream) {
+    int rc = check_row_grids(X, type, M, C, g, ldx, chan_src, num_splits, bits, clip_ratio, Xq, ldq, step_out);
+    if (rc) return rc;
+    if (M == 0) return OCS_OK;
+    hipError_t e = launch_row_grids(X, type, ldx, M, C, g, num_splits, chan_src, chan_depth, clip_ratio, qmax_of(bits), Xq, ldq,
+                                    step_out, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+static int check_rows_output(const void* Y, int out_type, int64_t M, int64_t N, int64_t ldy, const float* step_w, const float* bias) {
+    if ((M != 0 && !Y) || !step_w) return OCS_E_NULL;
+    if (!type_ok(out_type)) return OCS_E_TYPE;
+    if (ldy < N) return OCS_E_SHAPE;
+    if (!aligned(Y, type_bytes(out_type)) || !aligned(step_w, 4) || !aligned(bias, 4)) return OCS_E_ALIGN;
+    return OCS_OK;
+}
+
+int ocs_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, int64_t ldw, int64_t M, int64_t N, int64_t Kexp,
+                   int bits_x, int bits_w, const float* step_x, const float* step_w, const float* bias, void* Y,
+                   int out_type, int64_t ldy, void* stream) {
+    if (!Wq || (M != 0 && (!Xq || !step_x))) return OCS_E_NULL;
+    int rc = check_rows_output(Y, out_type, M, N, ldy, step_w, bias);
+    if (rc) return rc;
+    rc = check_gemm_operands(Xq, ldx, Wq, ldw, M == 0 ? 1 : M, N, Kexp, bits_x, bits_w, nullptr, 0);
+    if (rc) return rc;
+    if (!aligned(step_x, 4)) return OCS_E_ALIGN;
+    if (M == 0) return OCS_OK;
+    hipError_t e = launch_qgemm_rows(Xq, ldx, Wq, ldw, M, N, Kexp, step_x, step_w, bias, Y, out_type, ldy,
+                                     static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+int ocs_forward_rows(const void* X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t* chan_src, int num_splits,
+                     int bits_x, float clip_ratio, int8_t* Xq, int64_t ldq, float* step_x_out, const int8_t* Wq,
+                     int64_t ldw, int64_t N, int bits_w, const float* step_w, const float* bias, void* Y, int out_type,
+                     int64_t ldy, void* stream) {
+    if (!Wq) return OCS_E_NULL;
+    int rc = check_row_grids(X, type, M, C, g, ldx, chan_src, num_splits, bits_x, clip_ratio, Xq, ldq, step_x_out);
+    if (rc) return rc;
+    rc = check_rows_output(Y, out_type, M, N, ldy, step_w, bias);
+    if (rc) return rc;
+    const int64_t Kexp = (int64_t)(C + num_splits) * g;
+    rc = check_gemm_operands(Xq, ldq, Wq, ldw, M == 0 ? 1 : M, N, Kexp, bits_x, bits_w, nullptr, 0);
+    if (rc) return rc;
+    if (M == 0) return OCS_OK;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipError_t e = launch_row_grids(X, type, ldx, M, C, g, num_splits, chan_src, nullptr, clip_ratio, qmax_of(bits_x), Xq, ldq,
+                                    step_x_out, st);
+    if (e == hipSuccess)
+        e = launch_qgemm_rows(Xq, ldq, Wq, ldw, M, N, Kexp, step_x_out, step_w, bias, Y, out_type, ldy, st);
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+// ---- scoring of tokens -----------------------------------------------------------------------
+
+static int check_token_rows(int64_t M, int64_t V, int top_k) {
+    if (M < 0 || M > (int64_t)1 << 30 || V <= 0 || V > (int64_t)1 << 30) return OCS_E_SHAPE;
+    if (top_k < 0 || top_k > OCS_MAX_TOP || top_k > V) return OCS_E_TOP;
+    return OCS_OK;
+}
+
+size_t ocs_token_logprobs_workspace_bytes(int64_t M, int64_t V, int top_k) {
+    if (M == 0 || check_token_rows(M, V, top_k)) return 0;
+    return token_logprobs_workspace_bytes(M, V, top_k);
+}
+
+int ocs_token_logprobs(const void* logits, int type, int64_t M, int64_t V, int64_t ld, const int32_t* tokens, int top_k,
+                       float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,
+                       size_t ws_bytes, void* stream) {
+    if (M != 0) {
+        if (!logits || (tokens == nullptr) != (logprob == nullptr)) return OCS_E_NULL;
+        if (top_k > 0 && (!top_ids || !top_logprobs)) return OCS_E_NULL;
+        if (!logprob && !entropy && top_k == 0) return OCS_E_NULL;
+    }
+    if (!type_ok(type)) return OCS_E_TYPE;
+    int rc = check_token_rows(M, V, top_k);
+    if (rc) return rc;
+    if (ld < V) return OCS_E_SHAPE;
+    if (!aligned(logits, type_bytes(type)) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
+        !aligned(top_ids, 4) || !aligned(top_logprobs, 4))
+        return OCS_E_ALIGN;
+    if (M == 0) return OCS_OK;
+    const size_t need = token_logprobs_workspace_bytes(M, V, top_k);
+    if (need > 0 && (workspace == nullptr || ws_bytes < need)) return OCS_E_WORKSPACE;
+    if (need > 0 && !aligned(workspace, 256)) return OCS_E_ALIGN;
+    hipError_t e = launch_token_logprobs(logits, type, M, V, ld, tokens, top_k, logprob, entropy, top_ids, top_logprobs, workspace,
+                                         static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
 }
 
 int ocs_time_next(int family, void* start_event, void* stop_event) {

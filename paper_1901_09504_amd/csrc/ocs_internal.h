@@ -225,6 +225,19 @@ hipError_t launch_qconv(const int8_t* Aq, int64_t ldc, int B, int H, int W, int 
 hipError_t launch_tap_major(const int8_t* Wq, int64_t ldq, int64_t N, int E, int g, int64_t ldc,
                             int8_t* Wt, hipStream_t stream);
 
+// A grid per row (csrc/row_grids.hip), the product with a scale per row of either operand (csrc/qgemm_rows.hip) and the scoring
+// of tokens (csrc/token_logprobs.hip).  type / out_type: OCS_F32, OCS_BF16 or OCS_F16.
+hipError_t launch_row_grids(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src,
+                            const int32_t* chan_depth, float clip, float qmax, int8_t* Xq, int64_t ldq, float* step,
+                            hipStream_t stream);
+hipError_t launch_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, int64_t ldw, int64_t M, int64_t N, int64_t Kexp,
+                             const float* step_x, const float* step_w, const float* bias, void* Y, int out_type, int64_t ldy,
+                             hipStream_t stream);
+size_t token_logprobs_workspace_bytes(int64_t M, int64_t V, int k);
+hipError_t launch_token_logprobs(const void* logits, int type, int64_t M, int64_t V, int64_t ld, const int32_t* tokens, int k,
+                                 float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,
+                                 hipStream_t stream);
+
 // 16-byte copy of `bytes` (multiple of 16) device bytes: counter calibration only.
 hipError_t launch_calib_copy(const void* src, void* dst, size_t bytes, int workgroups, hipStream_t stream);
 hipError_t launch_calib_pack(const void* src, void* dst, size_t bytes, int workgroups, hipStream_t stream);

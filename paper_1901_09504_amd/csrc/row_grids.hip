@@ -1,0 +1,265 @@
+// Splitting and quantization with a grid per row: Eq. 1 with T taken over one row (a token of X, an output channel of W)
+// of the expanded tensor.
+//
+// A row is read once: its values wait in registers for the row's maximum, then become codes.  A wave takes a short row, a
+// workgroup a longer one; a row beyond what a workgroup's registers hold is read twice.  Bound by HBM for many rows (a row's
+// elements in, a byte per expanded column out) and by latency for few.
+#include "row_types.h"
+
+namespace ocs {
+
+struct RowGrids {
+    const void* X;
+    int64_t ldx, M;
+    int C, g, s;
+    const int32_t* chan_src;
+    const int32_t* chan_depth;
+    float clip, qmax;
+    int8_t* Xq;
+    int64_t ldq;
+    float* step;
+};
+
+// the column that expanded column k copies, and its channel
+__device__ __forceinline__ int source_column(const RowGrids& p, int k, int* channel) {
+    const int j = p.g == 1 ? k : k / p.g;
+    int src = p.chan_src[j];
+    src = src < 0 ? 0 : (src >= p.C ? p.C - 1 : src);
+    *channel = j;
+    return p.g == 1 ? src : src * p.g + (k - j * p.g);
+}
+
+__device__ __forceinline__ float depth_factor(const RowGrids& p, int channel) {
+    int d = p.chan_depth[channel];
+    d = d < 0 ? 0 : (d > 255 ? 255 : d);
+    return ldexpf(1.0f, -d);
+}
+
+// magnitudes as whole numbers: they order like them, and NaN comes above infinity
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// The largest word over the NT lanes of a row (64: the wave, 256: the workgroup).
+template <int NT>
+__device__ __forceinline__ unsigned row_max(unsigned v, unsigned* red) {
+    v = wave_umax32(v);
+    if constexpr (NT == 64) return v;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    unsigned m = red[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) m = red[w] > m ? red[w] : m;
+    return m;
+}
+
+template <int NT>
+__device__ __forceinline__ void row_barrier() {
+    if constexpr (NT == 64) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        __syncthreads();
+    }
+}
+
+// Bytes of LDS for a row's codes: whole pieces.
+static int64_t image_bytes(int64_t K) { return round_up(K, 16); }
+
+// NT lanes per row, U 16-byte pieces per lane: rows of up to NT * U pieces.  SCALED: 2^-chan_depth applies.
+// Codes of whole pieces go straight to memory and into the row's image in LDS; what lies behind them (a last partial
+// piece, the copies, the padding) is put together from the image, or with SCALED from the row again.
+template <Elem T, int NT, int U, bool SCALED>
+__global__ __launch_bounds__(256) void row_grid_kernel(RowGrids p) {
+    constexpr int VEC = kVec<T>;
+    __shared__ unsigned red[4];
+    extern __shared__ __align__(16) int8_t images[];
+    const int K = p.C * p.g, Ke = (p.C + p.s) * p.g;
+    const int t = (int)threadIdx.x % NT;
+    const int64_t row = (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT;
+    if (row >= p.M) return;                               // NT == 64: whole waves; NT == 256: never
+    int8_t* image = images + (threadIdx.x / NT) * ((K + 15) & ~15);
+    const elem_t<T>* x = static_cast<const elem_t<T>*>(p.X) + row * p.ldx;
+    int8_t* q = p.Xq + row * p.ldq;
+    const int pieces = K / VEC, rest = K % VEC;
+
+    u32x4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = u * NT + t;
+        raw[u] = u32x4{0u, 0u, 0u, 0u};
+        if (i < pieces) raw[u] = load_piece<T>(x + i * VEC);
+        else if (i == pieces && rest) raw[u] = load_partial<T>(x + i * VEC, rest);
+    }
+    auto value = [&](int u, int e) {
+        float v = piece_elem<T>(raw[u], e);
+        if constexpr (SCALED) {
+            const int k = (u * NT + t) * VEC + e;
+            if (k < K) v *= depth_factor(p, p.g == 1 ? k : k / p.g);
+        }
+        return v;
+    };
+    unsigned big = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const unsigned m = magnitude(value(u, e));
+            big = m > big ? m : big;
+        }
+    if constexpr (SCALED) {                               // a copy may carry fewer halvings than its source
+        for (int k = K + t; k < Ke; k += NT) {
+            int j;
+            const int src = source_column(p, k, &j);
+            const unsigned m = magnitude(elem_to_float<T>(x[src]) * depth_factor(p, j));
+            big = m > big ? m : big;
+        }
+    }
+    const float thr = p.clip * __uint_as_float(row_max<NT>(big, red));
+    const float inv = inv_step_of(thr, p.qmax);
+    if (t == 0) p.step[row] = __fdiv_rn(thr, p.qmax);
+
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = u * NT + t;
+        unsigned code[VEC / 4];
+#pragma unroll
+        for (int d = 0; d < VEC / 4; ++d)
+            code[d] = pack4(code_bits(value(u, 4 * d), inv, p.qmax), code_bits(value(u, 4 * d + 1), inv, p.qmax),
+                            code_bits(value(u, 4 * d + 2), inv, p.qmax), code_bits(value(u, 4 * d + 3), inv, p.qmax));
+        if (i < pieces + (rest ? 1 : 0)) {
+            unsigned* at = reinterpret_cast<unsigned*>(image + i * VEC);
+            unsigned* to = reinterpret_cast<unsigned*>(q + i * VEC);
+#pragma unroll
+            for (int d = 0; d < VEC / 4; ++d) {
+                at[d] = code[d];
+                if (i < pieces) to[d] = code[d];
+            }
+        }
+    }
+    row_barrier<NT>();
+    const int tail0 = pieces * VEC;
+    for (int k0 = tail0 + 4 * t; k0 < (int)p.ldq; k0 += 4 * NT) {
+        unsigned word = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int k = k0 + b;
+            unsigned byte = 0;
+            if (k < K) {
+                byte = (unsigned char)image[k];
+            } else if (k < Ke) {
+                int j;
+                const int src = source_column(p, k, &j);
+                if constexpr (SCALED)
+                    byte = code_bits(elem_to_float<T>(x[src]) * depth_factor(p, j), inv, p.qmax) & 0xFFu;
+                else
+                    byte = (unsigned char)image[src];
+            }
+            word |= byte << (8 * b);
+        }
+        *reinterpret_cast<unsigned*>(q + k0) = word;
+    }
+}
+
+// Rows beyond the registers of a workgroup: the maximum first, then the row again (from the caches as far as they hold it).
+template <Elem T, bool SCALED>
+__global__ __launch_bounds__(256) void row_grid_long_kernel(RowGrids p) {
+    constexpr int VEC = kVec<T>;
+    __shared__ unsigned red[4];
+    const int64_t K = (int64_t)p.C * p.g, Ke = (int64_t)(p.C + p.s) * p.g;
+    const int t = (int)threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const elem_t<T>* x = static_cast<const elem_t<T>*>(p.X) + row * p.ldx;
+    int8_t* q = p.Xq + row * p.ldq;
+    const int64_t pieces = K / VEC;
+    auto at = [&](int64_t k) {                            // expanded column k
+        float v;
+        if (k < K) {
+            v = elem_to_float<T>(x[k]);
+            if constexpr (SCALED) v *= depth_factor(p, (int)(k / p.g));
+        } else {
+            int j;
+            v = elem_to_float<T>(x[source_column(p, (int)k, &j)]);
+            if constexpr (SCALED) v *= depth_factor(p, j);
+        }
+        return v;
+    };
+    unsigned big = 0;
+    for (int64_t i = t; i < pieces; i += 256) {
+        const u32x4 raw = load_piece<T>(x + i * VEC);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            float v = piece_elem<T>(raw, e);
+            if constexpr (SCALED) v *= depth_factor(p, (int)((i * VEC + e) / p.g));
+            const unsigned m = magnitude(v);
+            big = m > big ? m : big;
+        }
+    }
+    for (int64_t k = pieces * VEC + t; k < (SCALED ? Ke : K); k += 256) {
+        const unsigned m = magnitude(at(k));
+        big = m > big ? m : big;
+    }
+    const float thr = p.clip * __uint_as_float(row_max<256>(big, red));
+    const float inv = inv_step_of(thr, p.qmax);
+    if (t == 0) p.step[row] = __fdiv_rn(thr, p.qmax);
+    for (int64_t i = t; i < pieces; i += 256) {
+        const u32x4 raw = load_piece<T>(x + i * VEC);
+        unsigned* to = reinterpret_cast<unsigned*>(q + i * VEC);
+#pragma unroll
+        for (int d = 0; d < VEC / 4; ++d) {
+            unsigned c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = piece_elem<T>(raw, 4 * d + e);
+                if constexpr (SCALED) v *= depth_factor(p, (int)((i * VEC + 4 * d + e) / p.g));
+                c[e] = code_bits(v, inv, p.qmax);
+            }
+            to[d] = pack4(c[0], c[1], c[2], c[3]);
+        }
+    }
+    for (int64_t k0 = pieces * VEC + 4 * t; k0 < p.ldq; k0 += 4 * 256) {
+        unsigned word = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            if (k0 + b < Ke) word |= (code_bits(at(k0 + b), inv, p.qmax) & 0xFFu) << (8 * b);
+        *reinterpret_cast<unsigned*>(q + k0) = word;
+    }
+}
+
+template <Elem T, int NT, int U>
+static hipError_t run_row_grids(const RowGrids& p, hipStream_t stream) {
+    const int64_t groups = ceil_div(p.M, 256 / NT);
+    if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
+    const unsigned lds = (unsigned)(image_bytes((int64_t)p.C * p.g) * (256 / NT));
+    return launch_kernel(kTimeSplitQuantize, p.chan_depth ? row_grid_kernel<T, NT, U, true> : row_grid_kernel<T, NT, U, false>,
+                         dim3((unsigned)groups), dim3(256), lds, stream, p);
+}
+
+template <Elem T>
+static hipError_t run_row_grids_of(const RowGrids& p, hipStream_t stream) {
+    const int64_t K = (int64_t)p.C * p.g, pieces = ceil_div(K, kVec<T>);
+    if (p.ldq <= 0x7FFFFFFF) {
+        // a wave per row while two pieces a lane hold it, then a workgroup
+        if (pieces <= 64) return run_row_grids<T, 64, 1>(p, stream);
+        if (pieces <= 128) return run_row_grids<T, 64, 2>(p, stream);
+        if (pieces <= 256) return run_row_grids<T, 256, 1>(p, stream);
+        if (pieces <= 512) return run_row_grids<T, 256, 2>(p, stream);
+        if (pieces <= 1024) return run_row_grids<T, 256, 4>(p, stream);
+        if (pieces <= 2048) return run_row_grids<T, 256, 8>(p, stream);
+    }
+    if (p.M > 0x7FFFFFFF) return hipErrorInvalidValue;
+    return launch_kernel(kTimeSplitQuantize, p.chan_depth ? row_grid_long_kernel<T, true> : row_grid_long_kernel<T, false>,
+                         dim3((unsigned)p.M), dim3(256), 0, stream, p);
+}
+
+hipError_t launch_row_grids(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src,
+                            const int32_t* chan_depth, float clip, float qmax, int8_t* Xq, int64_t ldq, float* step,
+                            hipStream_t stream) {
+    const RowGrids p{X, ldx, M, C, g, s, chan_src, chan_depth, clip, qmax, Xq, ldq, step};
+    switch (static_cast<Elem>(type)) {
+        case Elem::f32: return run_row_grids_of<Elem::f32>(p, stream);
+        case Elem::bf16: return run_row_grids_of<Elem::bf16>(p, stream);
+        case Elem::f16: return run_row_grids_of<Elem::f16>(p, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace ocs
