@@ -10,6 +10,7 @@
 namespace ocs {
 
 constexpr int kThreads = 256;      // every kernel here runs 256-thread workgroups (4 wave64)
+constexpr int kMaxDevices = 64;     // GPUs whose once-per-device settings are kept
 constexpr int kMaxExpanded = 8000;  // C + s limit of the single-workgroup greedy selector
 constexpr int kFlatMaxGrid = 4096;  // most workgroups (= partial maxima) of the flat max|x| pass
 

@@ -1433,7 +1433,6 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void qconv_patch_kernel(
 }
 
 constexpr int64_t kWholeKMaxLds = 160 * 1024;  // LDS of one CU
-constexpr int kMaxDevices = 64;
 
 int compute_units() {
     static std::atomic<int> cached[kMaxDevices];

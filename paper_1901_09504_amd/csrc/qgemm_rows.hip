@@ -5,6 +5,9 @@
 // holds four consecutive outputs of one token and stores them as they are, without a detour through LDS.
 // Codes go from memory straight into LDS, 128 bytes (one line) of 8 rows per request, 16-byte chunks XOR-ed with the row so that
 // the matrix cores' reads of consecutive rows fall into different banks.
+#include <atomic>
+#include <type_traits>
+
 #include "row_types.h"
 
 namespace ocs {
@@ -38,6 +41,18 @@ __device__ __forceinline__ void request_1k(const int8_t* from, unsigned lds_addr
 #endif
 }
 
+// The same from a wave-uniform base and each lane's offset (no vector arithmetic from step to step).
+__device__ __forceinline__ void request_1k(const int8_t* base, unsigned offset, unsigned lds_addr) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const unsigned m0 = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(m0) : "memory");
+#else
+    (void)base;
+    (void)offset;
+    (void)lds_addr;
+#endif
+}
+
 // until at most N of this wave's requests are under way
 template <int N>
 __device__ __forceinline__ void wait_requests() {
@@ -56,22 +71,37 @@ __device__ __forceinline__ unsigned lds_address(const int8_t* p) {
 #endif
 }
 
-// Four outputs of one token, from column n on.
+// fp32: outputs of a token lie 4 to a lane.  Two-byte outputs: the rows of two neighbouring weight tiles are dealt so that a lane
+// has 8 in a row, 16 bytes either way.  Row R of the tiles' image holds output column_of(R).
 template <Elem OUT>
-__device__ __forceinline__ void store4(const RowsGemm& p, int m, int n, i32x4 acc, float sx) {
-    if (m >= p.M) return;
-    elem_t<OUT>* y = static_cast<elem_t<OUT>*>(p.Y) + (int64_t)m * p.ldy + n;
-    elem_t<OUT> v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int c = n + e < p.N ? n + e : p.N - 1;
-        float o = (float)acc[e] * (sx * p.step_w[c]);
-        if (p.bias) o += p.bias[c];
-        v[e] = float_to_elem<OUT>(o);
-    }
+__device__ __forceinline__ int column_of(int R) {
+    if constexpr (OUT == Elem::f32) return R;
+    else return (R & ~31) + ((R & 15) >> 2) * 8 + ((R >> 4) & 1) * 4 + (R & 3);
+}
+
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// p[at .. at + 3] of an array of n floats (what lies past it is never used)
+__device__ __forceinline__ f32x4 four_of(const float* p, int at, int n) {
+    if (at + 4 <= n) return *reinterpret_cast<const f32x4_a4*>(p + at);
+    f32x4 r = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (n + e < p.N) y[e] = v[e];
+        if (at + e < n) r[e] = p[at + e];
+    return r;
+}
+
+// Workgroup ids are dealt to the 8 XCDs in turn, each with an L2 of its own.  An XCD gets a run of tiles, and the run goes down
+// kTileRows rows of tiles before it goes to the next column: what runs at one time on an XCD is a block of tiles, whose panels of X and
+// W the L2 holds for all of them.
+constexpr int kTileRows = 8;
+__device__ __forceinline__ void tile_of(unsigned w, int tiles_m, int tiles_n, int* bm, int* bn) {
+    const unsigned total = (unsigned)tiles_m * (unsigned)tiles_n, each = total / 8, more = total % 8, xcd = w % 8;
+    const unsigned id = xcd * each + (xcd < more ? xcd : more) + w / 8;
+    const unsigned band = (unsigned)kTileRows * (unsigned)tiles_n, b = id / band, in = id - b * band;
+    const unsigned first = b * kTileRows, rows = (unsigned)tiles_m - first < kTileRows ? (unsigned)tiles_m - first : kTileRows;
+    *bm = (int)(first + in % rows);
+    *bn = (int)(in / rows);
 }
 
 // A BM x BN tile (tokens x outputs) per workgroup, a ring of NBUF steps in LDS.
@@ -82,38 +112,45 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsG
     constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;
     constexpr int STEP = (BM + BN) * 128;
     static_assert(XL >= 1 && WL >= 1 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole requests per wave");
-    static_assert((NBUF - 1) * LPS < 64 && NBUF >= 2, "requests under way");
+    static_assert(NBUF * LPS < 64 && NBUF >= 2, "requests under way");
     __shared__ __align__(1024) int8_t lds[NBUF * STEP];
     const int tid = (int)threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WAVES_N, wn = wave % WAVES_N;
-    const int bm = (int)(blockIdx.x / (unsigned)p.tiles_n), bn = (int)(blockIdx.x % (unsigned)p.tiles_n);
+    int bm, bn;
+    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, &bm, &bn);
     const int row0 = bm * BM, col0 = bn * BN;
 
-    // request u of a step: rows 8 (u NW + wave) + lane / 8, chunk slot lane % 8 of the step's image
+    // request u of a step: rows 8 (u NW + wave) + lane / 8 of the step's image, chunk slot lane % 8; first the rows of X, then those of W
     const int piece = (lane & 7) ^ (lane >> 3);
-    const int8_t* xsrc[XL];
-    const int8_t* wsrc[WL];
+    const int8_t* xbase = p.Xq + (int64_t)row0 * p.ldx;
+    const int8_t* wbase = p.Wq + (int64_t)col0 * p.ldw;
+    unsigned from[LPS];
 #pragma unroll
     for (int u = 0; u < XL; ++u) {
-        const int r = row0 + (u * NW + wave) * 8 + (lane >> 3);
-        xsrc[u] = p.Xq + (int64_t)(r < p.M ? r : p.M - 1) * p.ldx + piece * 16;
+        int r = (u * NW + wave) * 8 + (lane >> 3);
+        r = row0 + r < p.M ? r : p.M - 1 - row0;
+        from[u] = (unsigned)(r * p.ldx + piece * 16);
     }
 #pragma unroll
     for (int u = 0; u < WL; ++u) {
-        const int r = col0 + (u * NW + wave) * 8 + (lane >> 3);
-        wsrc[u] = p.Wq + (int64_t)(r < p.N ? r : p.N - 1) * p.ldw + piece * 16;
+        int r = column_of<OUT>((u * NW + wave) * 8 + (lane >> 3));
+        r = col0 + r < p.N ? r : p.N - 1 - col0;
+        from[XL + u] = (unsigned)(r * p.ldw + piece * 16);
     }
     const unsigned lds0 = lds_address(lds) + (unsigned)wave * 1024;
+    const bool cut = p.ldx < (int64_t)p.ksteps * 128 || p.ldw < (int64_t)p.ksteps * 128;   // a pitch that ends inside the last step
+    auto request = [&](int u, int kt, int buf) {
+        const unsigned to = lds0 + (unsigned)(buf * STEP + u * NW * 1024);
+        const int8_t* base = (u < XL ? xbase : wbase) + (int64_t)kt * 128;
+        if (cut && kt == p.ksteps - 1)
+            request_1k((int64_t)kt * 128 + piece * 16 < (u < XL ? p.ldx : p.ldw) ? base + from[u] : rows_zero_chunk, to);
+        else
+            request_1k(base, from[u], to);
+    };
     auto fetch = [&](int kt, int buf) {
-        const int64_t k = (int64_t)kt * 128;
-        const bool xin = k + piece * 16 < p.ldx, win = k + piece * 16 < p.ldw;
 #pragma unroll
-        for (int u = 0; u < XL; ++u)
-            request_1k(xin ? xsrc[u] + k : rows_zero_chunk, lds0 + (unsigned)(buf * STEP + u * NW * 1024));
-#pragma unroll
-        for (int u = 0; u < WL; ++u)
-            request_1k(win ? wsrc[u] + k : rows_zero_chunk, lds0 + (unsigned)(buf * STEP + BM * 128 + u * NW * 1024));
+        for (int u = 0; u < LPS; ++u) request(u, kt, buf);
     };
 
     i32x4 acc[TN][TM];
@@ -123,45 +160,62 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsG
         for (int j = 0; j < TM; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
     const int fr = lane & 15, fq = lane >> 4;
     i32x4 xf[2][TM], wf[2][TN];
-    auto read = [&](int buf, int ks, i32x4 (&x)[TM], i32x4 (&w)[TN]) {
+    // fragment f of a half step: the token tiles first, then the weight tiles
+    auto read = [&](int f, int buf, int ks) {
         const int slot = ((ks * 4 + fq) ^ (fr & 7)) * 16;
-        const int8_t* xa = lds + buf * STEP + (wm * (BM / WAVES_M) + fr) * 128 + slot;
-        const int8_t* wa = lds + buf * STEP + BM * 128 + (wn * (BN / WAVES_N) + fr) * 128 + slot;
-#pragma unroll
-        for (int j = 0; j < TM; ++j) x[j] = *reinterpret_cast<const i32x4*>(xa + j * 2048);
-#pragma unroll
-        for (int i = 0; i < TN; ++i) w[i] = *reinterpret_cast<const i32x4*>(wa + i * 2048);
+        if (f < TM)
+            xf[ks][f] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + (wm * (BM / WAVES_M) + fr) * 128 + slot + f * 2048);
+        else
+            wf[ks][f - TM] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + BM * 128 + (wn * (BN / WAVES_N) + fr) * 128 + slot +
+                                                             (f - TM) * 2048);
     };
-    auto multiply = [&](i32x4 (&x)[TM], i32x4 (&w)[TN]) {
+    auto multiply = [&](int i, int ks) {
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int j = 0; j < TM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < TM; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[ks][i], xf[ks][j], acc[i][j], 0, 0, 0);
     };
 
+    // Step kt: its first half is in registers when it begins; the second is read while the first is multiplied.  Then comes the
+    // one barrier of a step: every wave's part of step kt + 1 has landed and every wave has read all of step kt, so that the requests of
+    // step kt + NBUF go into its buffer, NBUF - 1 whole steps ahead of their use.  Reads and requests are dealt over the rows of
+    // products: the matrix cores run on while they are issued.
+    constexpr int FR = TM + TN, FPR = (FR + TN - 1) / TN, RPR = (LPS + TN - 1) / TN;
     const int steps = p.ksteps;
 #pragma unroll
-    for (int u = 0; u < NBUF - 1; ++u)
+    for (int u = 0; u < NBUF; ++u)
         if (u < steps) fetch(u, u);
-    if (steps >= NBUF - 1) wait_requests<(NBUF - 2) * LPS>();
+    if (steps >= NBUF) wait_requests<(NBUF - 1) * LPS>();
     else wait_requests<0>();
     __syncthreads();
-    read(0, 0, xf[0], wf[0]);
+#pragma unroll
+    for (int f = 0; f < FR; ++f) read(f, 0, 0);
     auto step = [&](int buf, int kt) {
-        const bool more = kt + NBUF - 1 < steps;
-        if (more) fetch(kt + NBUF - 1, (buf + NBUF - 1) % NBUF);
-        read(buf, 1, xf[1], wf[1]);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(xf[0], wf[0]);
-        __builtin_amdgcn_sched_barrier(0);
-        // step kt + 1 has landed for every wave, and every wave has read step kt: its buffer is free
-        if (more) wait_requests<(NBUF - 2) * LPS>();
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+#pragma unroll
+            for (int f = i * FPR; f < (i + 1) * FPR && f < FR; ++f) read(f, buf, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(i, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (kt + NBUF <= steps) wait_requests<(NBUF - 2) * LPS>();
         else wait_requests<0>();
         __syncthreads();
-        if (kt + 1 < steps) read((buf + 1) % NBUF, 0, xf[0], wf[0]);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(xf[1], wf[1]);
-        __builtin_amdgcn_sched_barrier(0);
+        const bool more = kt + NBUF < steps, next = kt + 1 < steps;
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            if (next) {
+#pragma unroll
+                for (int f = i * FPR; f < (i + 1) * FPR && f < FR; ++f) read(f, (buf + 1) % NBUF, 0);
+            }
+            if (more) {
+#pragma unroll
+                for (int u = i * RPR; u < (i + 1) * RPR && u < LPS; ++u) request(u, kt + NBUF, buf);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(i, 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     for (int kt = 0; kt < steps; kt += NBUF) {
 #pragma unroll
@@ -169,16 +223,50 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsG
             if (kt + u < steps) step(u, kt + u);
     }
 
+    // NV accumulator tiles make 16 bytes of a token's outputs
+    constexpr int NV = OUT == Elem::f32 ? 1 : 2;
+    const int n0 = col0 + wn * (BN / WAVES_N) + fq * 4 * NV, m0 = row0 + wm * (BM / WAVES_M) + fr;
+    const bool whole = row0 + BM <= p.M && col0 + BN <= p.N;
+    f32x4 sw[TN], bias[TN];
+    float sx[TM];
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-        const int m = row0 + wm * (BM / WAVES_M) + j * 16 + fr;
-        const float sx = p.step_x[m < p.M ? m : p.M - 1];
-#pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            const int n = col0 + wn * (BN / WAVES_N) + i * 16 + fq * 4;
-            if (n < p.N) store4<OUT>(p, m, n, acc[i][j], sx);
-        }
+    for (int i = 0; i < TN; ++i) {
+        const int n = n0 + (i / NV) * 16 * NV + (i % NV) * 4;
+        sw[i] = four_of(p.step_w, n, p.N);
+        bias[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (p.bias) bias[i] = four_of(p.bias, n, p.N);
     }
+#pragma unroll
+    for (int j = 0; j < TM; ++j) sx[j] = p.step_x[m0 + j * 16 < p.M ? m0 + j * 16 : p.M - 1];
+    auto emit = [&](auto inside, auto with_bias) {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+            const int m = m0 + j * 16;
+            elem_t<OUT>* y = static_cast<elem_t<OUT>*>(p.Y) + (int64_t)m * p.ldy + n0;
+#pragma unroll
+            for (int i = 0; i < TN; i += NV) {
+                elem_t<OUT> v[4 * NV];
+#pragma unroll
+                for (int q = 0; q < NV; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float o = (float)acc[i + q][j][e] * (sx[j] * sw[i + q][e]);
+                        if constexpr (with_bias.value) o += bias[i + q][e];
+                        v[4 * q + e] = float_to_elem<OUT>(o);
+                    }
+                if (inside.value || (m < p.M && n0 + i * 16 + 4 * NV <= p.N)) {
+                    store_piece<OUT>(y + i * 16, v);
+                } else if (m < p.M) {
+#pragma unroll
+                    for (int e = 0; e < 4 * NV; ++e)
+                        if (n0 + i * 16 + e < p.N) y[i * 16 + e] = v[e];
+                }
+            }
+        }
+    };
+    if (whole && p.bias == nullptr) emit(std::true_type{}, std::false_type{});
+    else if (whole) emit(std::true_type{}, std::true_type{});
+    else emit(std::false_type{}, std::true_type{});
 }
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT>
@@ -191,9 +279,189 @@ static hipError_t run_rows_tile(RowsGemm p, hipStream_t stream) {
                          dim3(WAVES_M * WAVES_N * 64), 0, stream, p);
 }
 
+// Few tiles: 8 XB tokens and 8 WB outputs per workgroup, the steps of K dealt over its NW waves, each with a ring of its own and no
+// barrier until the waves' sums meet in LDS.  XB and WB count requests of 8 rows: a matrix tile whose last 8 rows are not there reads
+// its first 8 twice.
+template <int XB, int WB, int NW, int NBUF, Elem OUT>
+__global__ __launch_bounds__(NW * 64) void rows_few_kernel(RowsGemm p) {
+    constexpr int XT = (XB + 1) / 2, WT = (WB + 1) / 2, LPS = XB + WB;
+    constexpr int STEP = LPS * 1024, RING = NBUF * STEP;
+    constexpr int BN = WB * 8, PITCH = BN + 4;              // of the sums: [token][output], 16-byte quads
+    static_assert(XB * 8 * PITCH * 4 <= RING, "a wave's sums take its ring's place");
+    static_assert(NBUF * LPS < 64, "requests under way");
+    extern __shared__ __align__(1024) int8_t rings[];
+    const int tid = (int)threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col0 = (int)(blockIdx.x % (unsigned)p.tiles_n) * BN, row0 = (int)(blockIdx.x / (unsigned)p.tiles_n) * (XB * 8);
+    const int rows = p.M - row0 < XB * 8 ? p.M - row0 : XB * 8;
+
+    const int piece = (lane & 7) ^ (lane >> 3);
+    const int8_t* xbase = p.Xq + (int64_t)row0 * p.ldx;
+    const int8_t* wbase = p.Wq + (int64_t)col0 * p.ldw;
+    unsigned from[LPS];
+#pragma unroll
+    for (int u = 0; u < XB; ++u) {
+        const int r = u * 8 + (lane >> 3);
+        from[u] = (unsigned)((r < rows ? r : rows - 1) * p.ldx + piece * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < WB; ++u) {
+        int r = u * 8 + (lane >> 3);
+        r = col0 + r < p.N ? r : p.N - 1 - col0;
+        from[XB + u] = (unsigned)(r * p.ldw + piece * 16);
+    }
+    int8_t* ring = rings + wave * RING;
+    const unsigned lds0 = lds_address(ring);
+    const bool cut = p.ldx < (int64_t)p.ksteps * 128 || p.ldw < (int64_t)p.ksteps * 128;
+    const int trips = (p.ksteps - wave + NW - 1) / NW;
+    auto fetch = [&](int it, int buf) {
+        const int kt = it * NW + wave;
+        const int64_t k = (int64_t)kt * 128;
+#pragma unroll
+        for (int u = 0; u < LPS; ++u) {
+            const int8_t* base = (u < XB ? xbase : wbase) + k;
+            const unsigned to = lds0 + (unsigned)(buf * STEP + u * 1024);
+            if (cut && kt == p.ksteps - 1)
+                request_1k(k + piece * 16 < (u < XB ? p.ldx : p.ldw) ? base + from[u] : rows_zero_chunk, to);
+            else
+                request_1k(base, from[u], to);
+        }
+    };
+
+    i32x4 acc[WT][XT];
+#pragma unroll
+    for (int i = 0; i < WT; ++i)
+#pragma unroll
+        for (int j = 0; j < XT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    const int fr = lane & 15, fq = lane >> 4;
+#pragma unroll
+    for (int u = 0; u < NBUF; ++u)
+        if (u < trips) fetch(u, u);
+    for (int it0 = 0; it0 < trips; it0 += NBUF) {
+#pragma unroll
+        for (int u = 0; u < NBUF; ++u) {
+            const int it = it0 + u, left = trips - 1 - it;      // this wave's steps after this one
+            if (left < 0) break;
+            if (left >= NBUF - 1) wait_requests<(NBUF - 1) * LPS>();
+            else if (NBUF > 3 && left == 2) wait_requests<(NBUF > 3 ? 2 : 0) * LPS>();
+            else if (NBUF > 2 && left == 1) wait_requests<(NBUF > 2 ? 1 : 0) * LPS>();
+            else wait_requests<0>();
+            const int8_t* at = ring + u * STEP;
+            i32x4 x[2][XT], w[2][WT];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const int slot = ((ks * 4 + fq) ^ (fr & 7)) * 16;
+#pragma unroll
+                for (int j = 0; j < XT; ++j)
+                    x[ks][j] = *reinterpret_cast<const i32x4*>(at + (j * 16 + (2 * j + 1 < XB ? fr : fr & 7)) * 128 + slot);
+#pragma unroll
+                for (int i = 0; i < WT; ++i)
+                    w[ks][i] = *reinterpret_cast<const i32x4*>(at + XB * 1024 + (i * 16 + (2 * i + 1 < WB ? fr : fr & 7)) * 128 + slot);
+            }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int i = 0; i < WT; ++i)
+#pragma unroll
+                    for (int j = 0; j < XT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[ks][i], x[ks][j], acc[i][j], 0, 0, 0);
+            if (left >= NBUF) {
+                __builtin_amdgcn_sched_barrier(0);              // the reads of this buffer have returned: the products took them
+                __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+                fetch(it + NBUF, u);
+            }
+        }
+    }
+    // every request has landed and every read has returned: the sums take the ring's place
+    int32_t* mine = reinterpret_cast<int32_t*>(ring);
+#pragma unroll
+    for (int i = 0; i < WT; ++i)
+#pragma unroll
+        for (int j = 0; j < XT; ++j) {
+            const int t = j * 16 + fr, n = i * 16 + fq * 4;
+            if (t < XB * 8 && n < BN) *reinterpret_cast<i32x4*>(mine + t * PITCH + n) = acc[i][j];
+        }
+    __syncthreads();
+    const int32_t* sums = reinterpret_cast<const int32_t*>(rings);
+    for (int o = tid; o < rows * BN; o += NW * 64) {
+        const int t = o / BN, c = o - t * BN, m = row0 + t, n = col0 + c;
+        if (n >= p.N) continue;
+        int a = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) a += sums[w * (RING / 4) + t * PITCH + c];
+        float v = (float)a * (p.step_x[m] * p.step_w[n]);
+        if (p.bias) v += p.bias[n];
+        static_cast<elem_t<OUT>*>(p.Y)[(int64_t)m * p.ldy + n] = float_to_elem<OUT>(v);
+    }
+}
+
+template <int XB, int WB, int NW, int NBUF, Elem OUT>
+static hipError_t run_rows_few(RowsGemm p, hipStream_t stream) {
+    constexpr int LDS = NW * NBUF * (XB + WB) * 1024;
+    static_assert(LDS <= 160 * 1024, "a compute unit's LDS");
+    p.tiles_m = (int)ceil_div(p.M, XB * 8);
+    p.tiles_n = (int)ceil_div(p.N, WB * 8);
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
+    if (total > 0x7FFFFFFF || p.ksteps < 1) return hipErrorInvalidValue;
+    if constexpr (LDS > 65536) {                            // once per device
+        static std::atomic<bool> allowed[kMaxDevices];
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
+        if (!allowed[dev].load(std::memory_order_acquire)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&rows_few_kernel<XB, WB, NW, NBUF, OUT>),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+            if (e != hipSuccess) return e;
+            allowed[dev].store(true, std::memory_order_release);
+        }
+    }
+    return launch_kernel(kTimeGemm, rows_few_kernel<XB, WB, NW, NBUF, OUT>, dim3((unsigned)total), dim3(NW * 64),
+                         (unsigned)LDS, stream, p);
+}
+
+// The kernel by shape.
+//
+// Up to 32 tokens: the weights' bytes are what is to be had, and every workgroup takes all tokens and a share of the outputs; the
+// share grows with the outputs per compute unit, as far as two workgroups' rings fit one (us, one launch after the other: 1 x 6000 x
+// 3150 8 / 16 / 24 outputs a workgroup 5.8 / 5.1 / 4.9, 1 x 33001 x 1575 16.3 / 10.8 / 10.9; 20 x 6000 x 3150 8.4 / 7.1 / 5.4, 48 outputs
+// of 4 waves 6.5; 20 x 33001 x 1575 33 / 20 / 17, 48 outputs 12.5).
+// Beyond, while 64 x 16 (64 x 32) tiles are no more than the compute units, K is dealt over a workgroup's waves all the same (100 x 500 x
+// 3150 5.0 against 11.1 in 64 x 64 tiles, 1000 x 256 x 2000 5.6 / 7.9, 300 x 500 x 5000 7.9 / 15.7; 64 x 6000 x 3150 8.6 / 11.0).
+// Then tiles: rounds of the chip times what a tile takes, a constant and a cost per step in 10 ns, fitted to tiles of every size alone
+// and under load.  It finds the fastest of the five on all 19 shapes that were measured (us): 333 x 2049 x 1052 64 x 64 6.7 (128 x
+// 128 10.7), 400 x 8000 x 3150 128 x 128 17.2 (64 x 64 24, 256 x 128 25.5), 700 x 6000 x 3150 192 x 128 23 (256 x 128 28, 128 x 128 33),
+// 8192 x 4096 x 4178 256 x 256 132 (256 x 128 153, 128 x 128 177), 700 x 33001 x 1575 256 x 256 65 (192 x 128 75).
 template <Elem OUT>
 static hipError_t run_rows_gemm(const RowsGemm& p, hipStream_t stream) {
-    return run_rows_tile<128, 128, 2, 2, 3, OUT>(p, stream);
+    const int64_t cus = compute_units(), per_cu = ceil_div(ceil_div(p.N, 8), cus);   // requests of 8 outputs a compute unit
+#define OCS_ROWS_FEW(XB)                                                        \
+    (per_cu <= 2   ? run_rows_few<XB, 2, 8, 2, OUT>(p, stream)                  \
+     : per_cu <= 3 ? run_rows_few<XB, 3, 8, 2, OUT>(p, stream)                  \
+                   : run_rows_few<XB, XB == 1 ? 4 : 6, XB == 1 ? 8 : 4, 2, OUT>(p, stream))
+    if (p.M <= 8) return OCS_ROWS_FEW(1);
+    if (p.M <= 16) return OCS_ROWS_FEW(2);
+    if (p.M <= 24) return OCS_ROWS_FEW(3);
+    if (p.M <= 32) return OCS_ROWS_FEW(4);
+#undef OCS_ROWS_FEW
+    const int64_t m64 = ceil_div(p.M, 64);
+    if (m64 * ceil_div(p.N, 16) <= cus) return run_rows_few<8, 2, 8, 2, OUT>(p, stream);
+    if (m64 * ceil_div(p.N, 32) <= cus) return run_rows_few<8, 4, 4, 2, OUT>(p, stream);
+    const auto cost = [&](int64_t bm, int64_t bn, int64_t fixed, int64_t step) {
+        return ceil_div(ceil_div(p.M, bm) * ceil_div(p.N, bn), cus) * (fixed + step * p.ksteps);
+    };
+    const int64_t by_tile[5] = {cost(64, 64, 50, 26), cost(128, 128, 150, 58), cost(192, 128, 250, 72), cost(256, 128, 350, 92),
+                                cost(256, 256, 600, 150)};
+    int best = 0;
+    for (int i = 1; i < 5; ++i)
+        if (by_tile[i] < by_tile[best]) best = i;
+    switch (best) {
+        case 0: return run_rows_tile<64, 64, 2, 2, 4, OUT>(p, stream);
+        case 1: return run_rows_tile<128, 128, 2, 4, 3, OUT>(p, stream);
+        case 2: return run_rows_tile<192, 128, 2, 4, 3, OUT>(p, stream);
+        case 3: return run_rows_tile<256, 128, 4, 2, 3, OUT>(p, stream);
+        default: return run_rows_tile<256, 256, 2, 4, 2, OUT>(p, stream);
+    }
 }
 
 hipError_t launch_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, int64_t ldw, int64_t M, int64_t N, int64_t Kexp,

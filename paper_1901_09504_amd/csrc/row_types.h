@@ -77,4 +77,19 @@ __device__ __forceinline__ elem_t<T> float_to_elem(float v) {
     else return (elem_t<T>)v;
 }
 
+// kVec elements to any address of the element's alignment
+template <Elem T>
+__device__ __forceinline__ void store_piece(elem_t<T>* p, const elem_t<T> (&v)[kVec<T>]) {
+    u32x4 r;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        if constexpr (T == Elem::f32)
+            r[d] = __float_as_uint(v[d]);
+        else
+            r[d] = (unsigned)__builtin_bit_cast(unsigned short, v[2 * d]) | (unsigned)__builtin_bit_cast(unsigned short, v[2 * d + 1]) << 16;
+    }
+    if constexpr (T == Elem::f32) *reinterpret_cast<u32x4_a4*>(p) = r;
+    else *reinterpret_cast<u32x4_a2*>(p) = r;
+}
+
 }  // namespace ocs
