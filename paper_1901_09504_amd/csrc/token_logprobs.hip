@@ -47,6 +47,19 @@ __device__ __forceinline__ int index_of(unsigned long long key) { return (int)(0
 
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
+// The sum over the 64 lanes of a wave, the same in all of them (rows of 16 lanes by DPP, then the four rows).
+__device__ __forceinline__ float wave_sum(float v) {
+    v += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0xB1, 0xF, 0xF, false));    // quad_perm [1,0,3,2]
+    v += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x4E, 0xF, 0xF, false));    // quad_perm [2,3,0,1]
+    v += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x141, 0xF, 0xF, false));   // row_half_mirror
+    v += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x140, 0xF, 0xF, false));   // row_mirror
+    const float a = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), 0));
+    const float b = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), 16));
+    const float c = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), 32));
+    const float d = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), 48));
+    return (a + b) + (c + d);
+}
+
 struct Running {
     float m = kLowest, s = 0.0f, w = 0.0f;
 };
@@ -58,6 +71,12 @@ __device__ __forceinline__ void raise(Running& r, float top) {
     r.w = f * __builtin_fmaf(r.s, d, r.w);
     r.s *= f;
     r.m = top;
+}
+
+__device__ __forceinline__ void join_wave(Running& r) {
+    raise(r, value_of(wave_umax32(order_of(r.m))));
+    r.s = wave_sum(r.s);
+    r.w = wave_sum(r.w);
 }
 
 template <int N>
@@ -75,64 +94,79 @@ __device__ __forceinline__ void add_logits(Running& r, const float (&v)[N]) {
     }
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
+template <Elem T>
+__device__ __forceinline__ void add_piece(Running& r, u32x4 raw) {
+    float v[kVec<T>];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    for (int e = 0; e < kVec<T>; ++e) v[e] = piece_elem<T>(raw, e);
+    add_logits(r, v);
+}
+
+// What a row comes to.
+struct RowResult {
+    float m, log_s;
+    bool bad;                                       // NaN or +inf in the row
+};
+__device__ __forceinline__ RowResult result_of(const Running& r) {
+    const bool none = r.m == kLowest && r.s == 0.0f;               // every token ruled out
+    return {r.m, none ? 0.0f : logf(r.s), !(r.s < 3.402823466e+38f)};
+}
+__device__ __forceinline__ void write_row(const TokenRows& p, int64_t row, const Running& r, const RowResult& q, float given,
+                                          bool has_token) {
+    const float nan = __uint_as_float(0x7FC00000u);
+    if (p.logprob) p.logprob[row] = !has_token ? 0.0f : q.bad ? nan : (given - q.m) - q.log_s;
+    if (p.entropy) p.entropy[row] = q.bad ? nan : r.s == 0.0f ? 0.0f : q.log_s - r.w / r.s;
+}
+__device__ __forceinline__ void write_top(const TokenRows& p, int64_t row, const RowResult& q, int i, unsigned long long key) {
+    p.top_ids[row * p.k + i] = index_of(key);
+    p.top_logprobs[row * p.k + i] = q.bad ? __uint_as_float(0x7FC00000u) : (value_of((unsigned)(key >> 32)) - q.m) - q.log_s;
+}
+
+constexpr unsigned kFirstFinite = 0x00800000u;      // order_of(kLowest): what is below is -inf or nothing
+
+// The largest number of which at least k of the wave's 256 keys (4 a lane) are no smaller, to its upper 16 bits.
+__device__ __forceinline__ unsigned bound_of(u32x4 keys, int k) {
+    unsigned bound = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const unsigned next = bound | (1u << bit);
+        int reach = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) reach += (int)__popcll(__ballot(keys[e] >= next));
+        bound = reach >= k ? next : bound;
+    }
+    return bound;
 }
 
 template <int NT>
 struct TopShared {
-    float wave_m[NT / 64], wave_s[NT / 64], wave_w[NT / 64];
     alignas(16) unsigned group[kTopGroups];
-    int reach[kTopGroups];
-    unsigned long long list[kTopList];
+    float wave_m[NT / 64], wave_s[NT / 64], wave_w[NT / 64];
+    unsigned long long list[kTopList + 8];
     unsigned long long top[32];
     unsigned long long wave_key[NT / 64];
-    unsigned bound;
-    int reach_n, list_n;
+    int list_n;
 };
 
-// What a row (or a part of one) comes to.
-__device__ __forceinline__ void write_row(const TokenRows& p, int64_t row, const Running& r, float given, bool has_token, int lane) {
-    const bool none = r.m == kLowest && r.s == 0.0f;               // every token ruled out
-    const bool bad = !(r.s < 3.402823466e+38f);                    // NaN or +inf in the row
-    const float nan = __uint_as_float(0x7FC00000u);
-    const float log_s = none ? 0.0f : logf(r.s);
-    if (lane == 0) {
-        if (p.logprob) p.logprob[row] = !has_token ? 0.0f : bad ? nan : (given - r.m) - log_s;
-        if (p.entropy) p.entropy[row] = bad ? nan : none ? 0.0f : log_s - r.w / r.s;
-    }
-}
-__device__ __forceinline__ void write_top(const TokenRows& p, int64_t row, const Running& r, int i, unsigned long long key) {
-    const bool none = r.m == kLowest && r.s == 0.0f;
-    const bool bad = !(r.s < 3.402823466e+38f);
-    const float log_s = none ? 0.0f : logf(r.s);
-    p.top_ids[row * p.k + i] = index_of(key);
-    p.top_logprobs[row * p.k + i] = bad ? __uint_as_float(0x7FC00000u) : (value_of((unsigned)(key >> 32)) - r.m) - log_s;
-}
+template <Elem T>
+constexpr unsigned kNoLogits = T == Elem::f32 ? 0xFF800000u : T == Elem::bf16 ? 0xFF80FF80u : 0xFC00FC00u;   // -inf
 
-// NT lanes per row (or part of a row), U 16-byte pieces a lane requested at once.
-template <Elem T, int NT, int U>
+// NT lanes per row (or part of a row).  HELD: the row's pieces stay in registers, U a lane; otherwise they pass through, U requested
+// ahead of the U that are added up.
+template <Elem T, int NT, int U, bool HELD>
 __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
     constexpr int VEC = kVec<T>;
     constexpr int GW = NT / kTopGroups;                            // lanes of a group
+    static_assert(GW == 1 || GW == 4, "a lane or a quad");
     __shared__ TopShared<NT> sh;
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = (int)threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = p.parts == 1 ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)p.parts);
     const int part = p.parts == 1 ? 0 : (int)(blockIdx.x % (unsigned)p.parts);
     const elem_t<T>* whole = static_cast<const elem_t<T>*>(p.logits) + row * p.ld;
     const int first = part * p.part_len;
     const int n = p.V - first < p.part_len ? p.V - first : p.part_len;
     const elem_t<T>* x = whole + first;
-
-    int token = -1;
-    float given = 0.0f;
-    if (p.parts == 1 && p.tokens != nullptr) {
-        token = p.tokens[row];
-        if (token < 0 || token >= p.V) token = -1;
-        if (token >= 0) given = elem_to_float<T>(whole[token]);
-    }
 
     // pieces at 16-byte addresses; what lies before and behind them, at most VEC - 1 logits each, one lane each
     int head = (int)((16u - ((unsigned)(uintptr_t)x & 15u)) & 15u) / (int)sizeof(elem_t<T>);
@@ -142,108 +176,140 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
     int edge = -1;                                                 // this lane's single logit
     if (tid < head) edge = tid;
     else if (tid >= VEC && tid - VEC < rest) edge = head + body * VEC + tid - VEC;
-    Running r;
-    float edge_v = 0.0f;
-    if (edge >= 0) edge_v = elem_to_float<T>(x[edge]);
 
-    int i0 = 0;
-    for (; i0 + NT * U <= body; i0 += NT * U) {
-        u32x4 raw[U];
+    u32x4 raw[U];
+    if constexpr (HELD) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = load_piece<T>(xb + (int64_t)(i0 + u * NT + tid) * VEC);
-        float v[U * VEC];
+        for (int u = 0; u < U; ++u) {
+            raw[u] = u32x4{kNoLogits<T>, kNoLogits<T>, kNoLogits<T>, kNoLogits<T>};
+            if (u * NT + tid < body) raw[u] = load_piece<T>(xb + (u * NT + tid) * VEC);
+        }
+    }
+    float edge_v = -__builtin_inff();
+    if (edge >= 0) edge_v = elem_to_float<T>(x[edge]);
+    int token = -1;
+    float given = 0.0f;
+    if (p.parts == 1 && p.tokens != nullptr) {
+        token = p.tokens[row];
+        if (token < 0 || token >= p.V) token = -1;
+        if (token >= 0) given = elem_to_float<T>(whole[token]);
+    }
+    if (tid == 0) sh.list_n = 0;
+
+    Running r;
+    if constexpr (HELD) {
+        float top = fmaxf(kLowest, edge_v);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[u * VEC + e] = piece_elem<T>(raw[u], e);
-        add_logits(r, v);
-    }
-    for (; i0 + tid < body; i0 += NT) {
-        const u32x4 raw = load_piece<T>(xb + (int64_t)(i0 + tid) * VEC);
-        float v[VEC];
+            for (int e = 0; e < VEC; ++e) top = fmaxf(top, piece_elem<T>(raw[u], e));
+        r.m = top;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = piece_elem<T>(raw, e);
-        add_logits(r, v);
+        for (int u = 0; u < U; ++u) add_piece<T>(r, raw[u]);
+    } else {
+        int i0 = 0;
+        if (NT * U <= body) {
+            u32x4 next[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u] = load_piece<T>(xb + (int64_t)(u * NT + tid) * VEC);
+            for (; i0 + NT * U <= body; i0 += NT * U) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u] = next[u];
+                if (i0 + 2 * NT * U <= body) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) next[u] = load_piece<T>(xb + (int64_t)(i0 + (U + u) * NT + tid) * VEC);
+                }
+                float v[U * VEC];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[u * VEC + e] = piece_elem<T>(raw[u], e);
+                add_logits(r, v);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * NT + tid < body) raw[u] = load_piece<T>(xb + (int64_t)(i0 + u * NT + tid) * VEC);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * NT + tid < body) add_piece<T>(r, raw[u]);
     }
     if (edge >= 0) {
         const float v[1] = {edge_v};
         add_logits(r, v);
     }
 
-    // the row's maximum and sums
-    const float mine = r.m;
+    // each wave's maximum and sums, and the lanes' maxima (0: nothing but -inf)
+    const unsigned mine = r.s == 0.0f ? 0u : order_of(r.m);
     {
-        const unsigned wm = wave_umax32(order_of(r.m));
-        if (lane == 0) sh.wave_m[wave] = value_of(wm);
-        if (tid == 0) sh.reach_n = sh.list_n = 0;
-        if constexpr (GW == 1) {
-            sh.group[tid] = order_of(mine);
-        } else {
-            float g = mine;
-#pragma unroll
-            for (int o = 1; o < GW; o <<= 1) g = fmaxf(g, __shfl_xor(g, o));
-            if (tid % GW == 0) sh.group[tid / GW] = order_of(g);
+        unsigned g = mine;
+        if constexpr (GW == 4) {
+            unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0xB1, 0xF, 0xF, false);   // quad_perm [1,0,3,2]
+            g = other > g ? other : g;
+            other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0x4E, 0xF, 0xF, false);            // quad_perm [2,3,0,1]
+            g = other > g ? other : g;
+        }
+        if (tid % GW == 0) sh.group[tid / GW] = g;
+        join_wave(r);
+        if (lane == 0) {
+            sh.wave_m[wave] = r.m;
+            sh.wave_s[wave] = r.s;
+            sh.wave_w[wave] = r.w;
         }
     }
     __syncthreads();
-    float top = sh.wave_m[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) top = fmaxf(top, sh.wave_m[w]);
-    raise(r, top);
-    r.s = wave_sum(r.s);
-    r.w = wave_sum(r.w);
-    if (lane == 0) {
-        sh.wave_s[wave] = r.s;
-        sh.wave_w[wave] = r.w;
+    r = Running{};
+    if (lane < NT / 64) {
+        r.m = sh.wave_m[lane];
+        r.s = sh.wave_s[lane];
+        r.w = sh.wave_w[lane];
     }
-    if (p.k > 0 && tid < kTopGroups) {
-        const unsigned me = sh.group[tid];
-        int ahead = 0;
-        for (int j = 0; j < kTopGroups; j += 4) {
-            const u32x4 o = *reinterpret_cast<const u32x4*>(&sh.group[j]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) ahead += o[e] > me || (o[e] == me && j + e < tid) ? 1 : 0;
-        }
-        if (ahead == p.k - 1) sh.bound = me;
-    }
-    __syncthreads();
-    r.s = sh.wave_s[0];
-    r.w = sh.wave_w[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) {
-        r.s += sh.wave_s[w];
-        r.w += sh.wave_w[w];
-    }
-    if (p.parts == 1) {
-        write_row(p, row, r, given, token >= 0, tid);
-    } else if (tid == 0) {
+    join_wave(r);                                                  // the row's, in every wave
+    if (tid == 0 && p.parts > 1) {
         float* to = p.sums + ((int64_t)row * p.parts + part) * 4;
         to[0] = r.m;
         to[1] = r.s;
         to[2] = r.w;
     }
-    if (p.k == 0) return;
+    if (p.k == 0) {
+        if (tid == 0 && p.parts == 1) write_row(p, row, r, result_of(r), given, token >= 0);
+        return;
+    }
 
-    const unsigned bound = sh.bound;
     const bool odd = !(r.s < 3.402823466e+38f);                    // NaN or +inf: the maxima do not show them all
     const int want = p.k < n ? p.k : n;
-    if (tid < kTopGroups && sh.group[tid] >= bound) sh.reach[atomicAdd(&sh.reach_n, 1)] = tid;
-    __syncthreads();
-    auto offer = [&](float v, int index) {
-        if (order_of(v) >= bound) {
-            const int at = atomicAdd(&sh.list_n, 1);
-            if (at < kTopList) sh.list[at] = key_of(v, first + index);
-        }
-    };
     if (!odd) {
+        const u32x4 groups = *reinterpret_cast<const u32x4*>(&sh.group[4 * lane]);
+        const unsigned reached = bound_of(groups, p.k), bound = reached > kFirstFinite ? reached : kFirstFinite;
+        auto offer = [&](float v, int index) {
+            if (order_of(v) >= bound) {
+                const int at = atomicAdd(&sh.list_n, 1);
+                if (at < kTopList) sh.list[at] = key_of(v, first + index);
+            }
+        };
         if (edge >= 0) offer(edge_v, edge);
-        const int reach_n = sh.reach_n;
-        for (int a = wave; a < reach_n; a += NT / 64) {
-            const int t0 = sh.reach[a] * GW + lane % GW;
-            for (int i = t0 + (lane / GW) * NT; i < body; i += (64 / GW) * NT) {
-                const u32x4 raw = load_piece<T>(xb + (int64_t)i * VEC);
+        if constexpr (HELD) {
+            if (mine >= bound) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) offer(piece_elem<T>(raw, e), head + i * VEC + e);
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) offer(piece_elem<T>(raw[u], e), head + (u * NT + tid) * VEC + e);
+            }
+        } else {
+            // the groups that reach the bound, dealt over the waves: group 4 l + e is lane l's key e
+            int turn = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                unsigned long long in = __ballot(groups[e] >= bound);
+                for (; in != 0; in &= in - 1) {
+                    if (turn++ % (NT / 64) != wave) continue;
+                    const int t0 = (4 * ((int)__ffsll(in) - 1) + e) * GW + lane % GW;
+                    for (int i = t0 + (lane / GW) * NT; i < body; i += (64 / GW) * NT) {
+                        const u32x4 again = load_piece<T>(xb + (int64_t)i * VEC);
+#pragma unroll
+                        for (int q = 0; q < VEC; ++q) offer(piece_elem<T>(again, q), head + i * VEC + q);
+                    }
+                }
             }
         }
     }
@@ -272,36 +338,59 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
             last = best;
             __syncthreads();
         }
+        if (wave != 0) return;
     } else {
-        for (int i = tid; i < got; i += NT) {
-            const unsigned long long key = sh.list[i];
+        // a list of a wave's size or less, most of the time: the first wave has the rest
+        if (got > 64) {
+            for (int i = tid; i < got; i += NT) {
+                const unsigned long long key = sh.list[i];
+                int ahead = 0;
+                for (int j = 0; j < got; ++j) ahead += sh.list[j] > key ? 1 : 0;
+                if (ahead < want) sh.top[ahead] = key;
+            }
+            __syncthreads();
+            if (wave != 0) return;
+        } else {
+            if (wave != 0) return;
+            const unsigned long long key = lane < got ? sh.list[lane] : 0ull;
             int ahead = 0;
-            for (int j = 0; j < got; ++j) ahead += sh.list[j] > key ? 1 : 0;
-            if (ahead < want) sh.top[ahead] = key;
+            for (int j = 0; j < got; j += 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ahead += j + e < got && sh.list[j + e] > key ? 1 : 0;
+            }
+            if (lane < got && ahead < want) sh.top[ahead] = key;
         }
         // fewer finite logits than alternatives: then all others are -inf, and the first of them follow
-        for (int j0 = 0; got < want && j0 < n; j0 += 64) {         // (every wave the same; wave 0 writes)
+        for (int j0 = 0; got < want && j0 < n; j0 += 64) {
             const float v = j0 + lane < n ? elem_to_float<T>(x[j0 + lane]) : 0.0f;
             const bool out = j0 + lane < n && v == -__builtin_inff();
             const unsigned long long mask = __ballot(out);
             const int at = got + (int)__popcll(mask & ((1ull << lane) - 1ull));
-            if (wave == 0 && out && at < want) sh.top[at] = key_of(v, first + j0 + lane);
+            if (out && at < want) sh.top[at] = key_of(v, first + j0 + lane);
             got += (int)__popcll(mask);
         }
-        __syncthreads();
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
-    if (tid < p.k) {
-        const unsigned long long key = tid < want ? sh.top[tid] : 0ull;   // (a part shorter than k)
-        if (p.parts == 1) write_top(p, row, r, tid, key);
-        else p.keys[((int64_t)row * p.parts + part) * p.k + tid] = key;
+    if (p.parts == 1) {
+        const RowResult q = result_of(r);
+        if (tid == 0) write_row(p, row, r, q, given, token >= 0);
+        if (tid < p.k) write_top(p, row, q, tid, sh.top[tid]);
+    } else if (tid < p.k) {
+        p.keys[((int64_t)row * p.parts + part) * p.k + tid] = tid < want ? sh.top[tid] : 0ull;   // (a part shorter than k)
     }
 }
 
 // The parts of a row joined by one wave, a lane per part: sums at the row's maximum, and the lists, each in order, merged.
+constexpr int kMostParts = 64;
 template <Elem T>
 __global__ __launch_bounds__(64) void token_join_kernel(TokenRows p) {
+    __shared__ unsigned long long keys[kMostParts * 33];           // a list's end: 0
     const int lane = (int)threadIdx.x;
     const int64_t row = blockIdx.x;
+    const unsigned long long* from = p.keys + (int64_t)row * p.parts * p.k;
+    for (int i = lane; i < p.parts * p.k; i += 64) keys[(i / p.k) * 33 + i % p.k] = from[i];
+    for (int i = lane; i < p.parts; i += 64) keys[i * 33 + p.k] = 0ull;
     int token = -1;
     float given = 0.0f;
     if (p.tokens != nullptr) {
@@ -310,51 +399,44 @@ __global__ __launch_bounds__(64) void token_join_kernel(TokenRows p) {
         if (token >= 0) given = elem_to_float<T>((static_cast<const elem_t<T>*>(p.logits) + row * p.ld)[token]);
     }
     Running r;
-    const unsigned long long* keys = p.keys + ((int64_t)row * p.parts + lane) * p.k;
-    unsigned long long next = 0;
-    int used = 0;
     if (lane < p.parts) {
-        const float* from = p.sums + ((int64_t)row * p.parts + lane) * 4;
-        r.m = from[0];
-        r.s = from[1];
-        r.w = from[2];
-        if (p.k > 0) next = keys[0];
+        const float* sums = p.sums + ((int64_t)row * p.parts + lane) * 4;
+        r.m = sums[0];
+        r.s = sums[1];
+        r.w = sums[2];
     }
-    raise(r, value_of(wave_umax32(order_of(r.m))));
-    r.s = wave_sum(r.s);
-    r.w = wave_sum(r.w);
-    write_row(p, row, r, given, token >= 0, lane);
+    join_wave(r);
+    const RowResult q = result_of(r);
+    if (lane == 0) write_row(p, row, r, q, given, token >= 0);
+    __syncthreads();
+    const unsigned long long* mine = keys + lane * 33;
+    unsigned long long next = lane < p.parts ? mine[0] : 0ull;
+    unsigned long long best_of_i = 0ull;                           // lane i keeps the i-th
     for (int i = 0; i < p.k; ++i) {
         const unsigned hi = wave_umax32((unsigned)(next >> 32));
         const unsigned lo = wave_umax32((unsigned)(next >> 32) == hi ? (unsigned)next : 0u);
         const unsigned long long best = ((unsigned long long)hi << 32) | lo;
-        if (next == best) {
-            write_top(p, row, r, i, best);
-            ++used;
-            next = used < p.k ? keys[used] : 0ull;
-        }
+        if (lane == i) best_of_i = best;
+        if (next == best && best != 0ull) next = *++mine;          // (keys differ: one lane)
     }
+    if (lane < p.k) write_top(p, row, q, lane, best_of_i);
 }
+
+// Logits that 1024 lanes hold, whatever their type: 16 pieces a lane of fp32, 8 of the others.
+constexpr int kHeldLogits = 65536;
 
 struct TokenPlan {
     int parts, part_len;
     size_t keys_off, total;
 };
+// Rows that fill the chip have a workgroup each.  Fewer ones, longer than a workgroup holds, are cut into parts that it does.
 static TokenPlan plan_token_rows(int64_t M, int64_t V, int k) {
     TokenPlan t{1, (int)V, 0, 0};
-    int64_t parts = 1;
-    if (M < compute_units()) {
-        parts = compute_units() / (M > 0 ? M : 1);
-        const int64_t most = V / 16384;
-        parts = parts < most ? parts : most;
-        parts = parts < 64 ? parts : 64;
-        if (parts < 1) parts = 1;
-    }
-    if (parts > 1) {
+    if (M <= compute_units() && V > kHeldLogits) {
+        int64_t parts = ceil_div(V, kHeldLogits);
+        parts = parts < kMostParts ? parts : kMostParts;
         t.part_len = (int)round_up(ceil_div(V, parts), 64);
         t.parts = (int)ceil_div(V, t.part_len);
-    }
-    if (t.parts > 1) {
         t.keys_off = (size_t)round_up(M * t.parts * 16, 256);
         t.total = t.keys_off + (size_t)M * t.parts * k * 8;
     }
@@ -362,13 +444,22 @@ static TokenPlan plan_token_rows(int64_t M, int64_t V, int k) {
 }
 size_t token_logprobs_workspace_bytes(int64_t M, int64_t V, int k) { return plan_token_rows(M, V, k).total; }
 
+template <Elem T, int NT, int U, bool HELD>
+static hipError_t run_token_kernel(const TokenRows& p, int64_t groups, hipStream_t stream) {
+    return launch_kernel(0, token_rows_kernel<T, NT, U, HELD>, dim3((unsigned)groups), dim3(NT), 0, stream, p);
+}
+
 template <Elem T>
 static hipError_t run_token_rows(const TokenRows& p, int64_t M, hipStream_t stream) {
-    const int64_t groups = M * p.parts;
+    const int64_t groups = M * p.parts, pieces = p.part_len / kVec<T>;
     if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
-    const hipError_t e = groups < 2 * compute_units()
-                             ? launch_kernel(0, token_rows_kernel<T, 1024, 2>, dim3((unsigned)groups), dim3(1024), 0, stream, p)
-                             : launch_kernel(0, token_rows_kernel<T, 256, 4>, dim3((unsigned)groups), dim3(256), 0, stream, p);
+    hipError_t e;
+    if (pieces <= 256 * 2) e = run_token_kernel<T, 256, 2, true>(p, groups, stream);
+    else if (pieces <= 256 * 8) e = run_token_kernel<T, 256, 8, true>(p, groups, stream);
+    else if (M > compute_units() || p.part_len > kHeldLogits) e = run_token_kernel<T, 256, 4, false>(p, groups, stream);
+    else if (pieces <= 1024 * 4) e = run_token_kernel<T, 1024, 4, true>(p, groups, stream);
+    else if (T == Elem::f32 && pieces > 1024 * 9) e = run_token_kernel<T, 1024, T == Elem::f32 ? 16 : 8, true>(p, groups, stream);
+    else e = run_token_kernel<T, 1024, T == Elem::f32 ? 9 : 8, true>(p, groups, stream);
     if (e != hipSuccess || p.parts == 1) return e;
     return launch_kernel(0, token_join_kernel<T>, dim3((unsigned)M), dim3(64), 0, stream, p);
 }
