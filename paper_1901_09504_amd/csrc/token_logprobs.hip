@@ -3,14 +3,14 @@
 // One pass over a row: every lane keeps the running maximum m of what it has seen, s = sum exp(x - m) and
 // w = sum (x - m) exp(x - m); where the maximum grows by d, s -> s e^-d and w -> e^-d (w - d s).  Joined over the row,
 // log p(t) = (x_t - m) - log s and the entropy is log s - w / s (both free of the cancellation of sum p log p).
-// The alternatives come out of the same pass: the k-th largest of 256 lane maxima is a bound that at least k logits
+// The alternatives come out of the same pass: the k-th largest of 64 groups' maxima is a bound that at least k logits
 // reach, only the lanes that reach it hold any of them, and only those lanes' pieces of the row are looked through again.
 // Bound by HBM for many rows, by latency for few.  All sums are in fp32.
 #include "row_types.h"
 
 namespace ocs {
 
-constexpr int kTopGroups = 256;       // lane maxima that the bound is taken from
+constexpr int kTopGroups = 256;       // maxima of lanes, or of quads of them, that are held against the bound
 constexpr int kTopList = 1024;        // logits that may reach it; more (rows of equal values) are selected one by one
 constexpr float kLowest = -3.402823466e+38f;
 constexpr float kLog2e = 1.44269504f;
@@ -124,27 +124,28 @@ __device__ __forceinline__ void write_top(const TokenRows& p, int64_t row, const
 
 constexpr unsigned kFirstFinite = 0x00800000u;      // order_of(kLowest): what is below is -inf or nothing
 
-// The largest number of which at least k of the wave's 256 keys (4 a lane) are no smaller, to its upper 16 bits.
+// A number that at least k of the wave's keys (4 a lane) reach: the k-th largest of the lanes' maxima, to its upper 16 bits.
 __device__ __forceinline__ unsigned bound_of(u32x4 keys, int k) {
+    unsigned most = keys[0];
+#pragma unroll
+    for (int e = 1; e < 4; ++e) most = keys[e] > most ? keys[e] : most;
     unsigned bound = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
         const unsigned next = bound | (1u << bit);
-        int reach = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) reach += (int)__popcll(__ballot(keys[e] >= next));
-        bound = reach >= k ? next : bound;
+        bound = (int)__popcll(__ballot(most >= next)) >= k ? next : bound;
     }
     return bound;
 }
 
-template <int NT>
+template <int NT, bool HELD>
 struct TopShared {
     alignas(16) unsigned group[kTopGroups];
     float wave_m[NT / 64], wave_s[NT / 64], wave_w[NT / 64];
-    unsigned long long list[kTopList + 8];
+    unsigned long long list[kTopList];
     unsigned long long top[32];
     unsigned long long wave_key[NT / 64];
+    int reach[HELD ? 1 : NT / 64][kTopGroups];                     // (a list per wave)
     int list_n;
 };
 
@@ -157,12 +158,12 @@ template <Elem T, int NT, int U, bool HELD>
 __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
     constexpr int VEC = kVec<T>;
     constexpr int GW = NT / kTopGroups;                            // lanes of a group
-    static_assert(GW == 1 || GW == 4, "a lane or a quad");
-    __shared__ TopShared<NT> sh;
+    static_assert(GW == 1 || GW == 2 || GW == 4, "a lane, a pair or a quad");
+    __shared__ TopShared<NT, HELD> sh;
     const int tid = (int)threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = p.parts == 1 ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)p.parts);
-    const int part = p.parts == 1 ? 0 : (int)(blockIdx.x % (unsigned)p.parts);
+    const int part = p.parts == 1 ? 0 : (int)(blockIdx.x - (unsigned)row * (unsigned)p.parts);
     const elem_t<T>* whole = static_cast<const elem_t<T>*>(p.logits) + row * p.ld;
     const int first = part * p.part_len;
     const int n = p.V - first < p.part_len ? p.V - first : p.part_len;
@@ -177,6 +178,8 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
     if (tid < head) edge = tid;
     else if (tid >= VEC && tid - VEC < rest) edge = head + body * VEC + tid - VEC;
 
+    int token = -1;                                                // asked for first: a wait for it is no wait for the row
+    if (p.parts == 1 && p.tokens != nullptr) token = p.tokens[row];
     u32x4 raw[U];
     if constexpr (HELD) {
 #pragma unroll
@@ -187,13 +190,6 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
     }
     float edge_v = -__builtin_inff();
     if (edge >= 0) edge_v = elem_to_float<T>(x[edge]);
-    int token = -1;
-    float given = 0.0f;
-    if (p.parts == 1 && p.tokens != nullptr) {
-        token = p.tokens[row];
-        if (token < 0 || token >= p.V) token = -1;
-        if (token >= 0) given = elem_to_float<T>(whole[token]);
-    }
     if (tid == 0) sh.list_n = 0;
 
     Running r;
@@ -239,14 +235,20 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
         add_logits(r, v);
     }
 
+    if (token < 0 || token >= p.V) token = -1;
+    float given = 0.0f;
+    if (token >= 0) given = elem_to_float<T>(whole[token]);
+
     // each wave's maximum and sums, and the lanes' maxima (0: nothing but -inf)
     const unsigned mine = r.s == 0.0f ? 0u : order_of(r.m);
     {
         unsigned g = mine;
-        if constexpr (GW == 4) {
-            unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0xB1, 0xF, 0xF, false);   // quad_perm [1,0,3,2]
+        if constexpr (GW >= 2) {
+            const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0xB1, 0xF, 0xF, false);   // quad_perm [1,0,3,2]
             g = other > g ? other : g;
-            other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0x4E, 0xF, 0xF, false);            // quad_perm [2,3,0,1]
+        }
+        if constexpr (GW == 4) {
+            const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0x4E, 0xF, 0xF, false);            // quad_perm [2,3,0,1]
             g = other > g ? other : g;
         }
         if (tid % GW == 0) sh.group[tid / GW] = g;
@@ -281,34 +283,50 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
     if (!odd) {
         const u32x4 groups = *reinterpret_cast<const u32x4*>(&sh.group[4 * lane]);
         const unsigned reached = bound_of(groups, p.k), bound = reached > kFirstFinite ? reached : kFirstFinite;
+        const float least = value_of(bound);
         auto offer = [&](float v, int index) {
-            if (order_of(v) >= bound) {
-                const int at = atomicAdd(&sh.list_n, 1);
-                if (at < kTopList) sh.list[at] = key_of(v, first + index);
-            }
+            const int at = atomicAdd(&sh.list_n, 1);
+            if (at < kTopList) sh.list[at] = key_of(v, first + index);
         };
-        if (edge >= 0) offer(edge_v, edge);
+        if (edge >= 0 && edge_v >= least) offer(edge_v, edge);
         if constexpr (HELD) {
+            // which of the lane's logits reach it, then those few once more (short code: a row's is fetched for that row alone)
+            static_assert(U * VEC <= 64, "a bit per logit");
             if (mine >= bound) {
+                unsigned hits[2] = {0u, 0u};
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) offer(piece_elem<T>(raw[u], e), head + (u * NT + tid) * VEC + e);
+                    for (int e = 0; e < VEC; ++e)
+                        hits[(u * VEC + e) / 32] |= piece_elem<T>(raw[u], e) >= least ? 1u << ((u * VEC + e) % 32) : 0u;
+                unsigned long long in = ((unsigned long long)hits[1] << 32) | hits[0];
+                for (; in != 0; in &= in - 1) {
+                    const int b = (int)__ffsll(in) - 1, index = head + (b / VEC * NT + tid) * VEC + b % VEC;
+                    offer(elem_to_float<T>(x[index]), index);
+                }
             }
         } else {
-            // the groups that reach the bound, dealt over the waves: group 4 l + e is lane l's key e
-            int turn = 0;
+            // the groups that reach the bound (group 4 l + e is lane l's key e), listed by every wave alike, then the pieces of them all
+            int reach_n = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                unsigned long long in = __ballot(groups[e] >= bound);
-                for (; in != 0; in &= in - 1) {
-                    if (turn++ % (NT / 64) != wave) continue;
-                    const int t0 = (4 * ((int)__ffsll(in) - 1) + e) * GW + lane % GW;
-                    for (int i = t0 + (lane / GW) * NT; i < body; i += (64 / GW) * NT) {
-                        const u32x4 again = load_piece<T>(xb + (int64_t)i * VEC);
+                const unsigned long long in = __ballot(groups[e] >= bound);
+                if (groups[e] >= bound) sh.reach[wave][reach_n + (int)__popcll(in & ((1ull << lane) - 1ull))] = 4 * lane + e;
+                reach_n += (int)__popcll(in);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            const unsigned each = (unsigned)(body + NT - 1) / NT * GW, all = (unsigned)reach_n * each;
+            for (unsigned j = (unsigned)tid; j < all; j += NT) {
+                const unsigned a = j / each, in = j - a * each, i = in / GW * NT + (unsigned)sh.reach[wave][a] * GW + in % GW;
+                if ((int)i >= body) continue;
+                const u32x4 again = load_piece<T>(xb + (int64_t)i * VEC);
+                unsigned hits = 0;
 #pragma unroll
-                        for (int q = 0; q < VEC; ++q) offer(piece_elem<T>(again, q), head + i * VEC + q);
-                    }
+                for (int e = 0; e < VEC; ++e) hits |= piece_elem<T>(again, e) >= least ? 1u << e : 0u;
+                for (; hits != 0; hits &= hits - 1) {
+                    const int index = head + (int)i * VEC + __ffs((int)hits) - 1;
+                    offer(elem_to_float<T>(x[index]), index);
                 }
             }
         }
@@ -354,9 +372,10 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
             if (wave != 0) return;
             const unsigned long long key = lane < got ? sh.list[lane] : 0ull;
             int ahead = 0;
-            for (int j = 0; j < got; j += 8) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ahead += j + e < got && sh.list[j + e] > key ? 1 : 0;
+            for (int j = 0; j < got; ++j) {
+                const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(key >> 32), j);
+                const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)key, j);
+                ahead += (((unsigned long long)hi << 32) | lo) > key ? 1 : 0;
             }
             if (lane < got && ahead < want) sh.top[ahead] = key;
         }
@@ -449,6 +468,10 @@ static hipError_t run_token_kernel(const TokenRows& p, int64_t groups, hipStream
     return launch_kernel(0, token_rows_kernel<T, NT, U, HELD>, dim3((unsigned)groups), dim3(NT), 0, stream, p);
 }
 
+// Rows of up to 2048 pieces are held by 256 lanes.  Longer ones: while every row can have a compute unit to itself, by 1024 (1 x 33001
+// fp32 8.1 us; passing through 256 lanes, with the row's second look from memory, 19), otherwise they pass through 256 lanes, or 512 where
+// rows come in several rounds and the last one's length counts (us, 256 / 512 lanes: 700 x 33001 fp32 18.7 / 19.2, bf16 14.2 / 14.9; 3000
+// x 33001 fp32 73 / 70; 4096 x 100003 bf16 160 / 155).
 template <Elem T>
 static hipError_t run_token_rows(const TokenRows& p, int64_t M, hipStream_t stream) {
     const int64_t groups = M * p.parts, pieces = p.part_len / kVec<T>;
@@ -456,6 +479,7 @@ static hipError_t run_token_rows(const TokenRows& p, int64_t M, hipStream_t stre
     hipError_t e;
     if (pieces <= 256 * 2) e = run_token_kernel<T, 256, 2, true>(p, groups, stream);
     else if (pieces <= 256 * 8) e = run_token_kernel<T, 256, 8, true>(p, groups, stream);
+    else if (M > 4 * compute_units()) e = run_token_kernel<T, 512, 4, false>(p, groups, stream);
     else if (M > compute_units() || p.part_len > kHeldLogits) e = run_token_kernel<T, 256, 4, false>(p, groups, stream);
     else if (pieces <= 1024 * 4) e = run_token_kernel<T, 1024, 4, true>(p, groups, stream);
     else if (T == Elem::f32 && pieces > 1024 * 9) e = run_token_kernel<T, 1024, T == Elem::f32 ? 16 : 8, true>(p, groups, stream);
