@@ -105,7 +105,9 @@ __device__ __forceinline__ void tile_of(unsigned w, int tiles_m, int tiles_n, in
 }
 
 // A BM x BN tile (tokens x outputs) per workgroup, a ring of NBUF steps in LDS.
-template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT>
+// WIDE: pitches of 2^24 bytes and more, whose offsets inside a tile do not fit 32 bits.
+constexpr int64_t kWidePitch = (int64_t)1 << 24;
+template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool WIDE = false>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsGemm p) {
     constexpr int NW = WAVES_M * WAVES_N;
     constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW, LPS = XL + WL;
@@ -125,18 +127,18 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsG
     const int piece = (lane & 7) ^ (lane >> 3);
     const int8_t* xbase = p.Xq + (int64_t)row0 * p.ldx;
     const int8_t* wbase = p.Wq + (int64_t)col0 * p.ldw;
-    unsigned from[LPS];
+    typename std::conditional<WIDE, int64_t, unsigned>::type from[LPS];
 #pragma unroll
     for (int u = 0; u < XL; ++u) {
         int r = (u * NW + wave) * 8 + (lane >> 3);
         r = row0 + r < p.M ? r : p.M - 1 - row0;
-        from[u] = (unsigned)(r * p.ldx + piece * 16);
+        from[u] = (decltype(from[0] + 0))(r * p.ldx + piece * 16);
     }
 #pragma unroll
     for (int u = 0; u < WL; ++u) {
         int r = column_of<OUT>((u * NW + wave) * 8 + (lane >> 3));
         r = col0 + r < p.N ? r : p.N - 1 - col0;
-        from[XL + u] = (unsigned)(r * p.ldw + piece * 16);
+        from[XL + u] = (decltype(from[0] + 0))(r * p.ldw + piece * 16);
     }
     const unsigned lds0 = lds_address(lds) + (unsigned)wave * 1024;
     const bool cut = p.ldx < (int64_t)p.ksteps * 128 || p.ldw < (int64_t)p.ksteps * 128;   // a pitch that ends inside the last step
@@ -145,6 +147,8 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsG
         const int8_t* base = (u < XL ? xbase : wbase) + (int64_t)kt * 128;
         if (cut && kt == p.ksteps - 1)
             request_1k((int64_t)kt * 128 + piece * 16 < (u < XL ? p.ldx : p.ldw) ? base + from[u] : rows_zero_chunk, to);
+        else if constexpr (WIDE)
+            request_1k(base + from[u], to);
         else
             request_1k(base, from[u], to);
     };
@@ -269,14 +273,28 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsG
     else emit(std::false_type{}, std::true_type{});
 }
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool WIDE = false>
 static hipError_t run_rows_tile(RowsGemm p, hipStream_t stream) {
     p.tiles_m = (int)ceil_div(p.M, BM);
     p.tiles_n = (int)ceil_div(p.N, BN);
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
     if (total > 0x7FFFFFFF || p.ksteps < 1) return hipErrorInvalidValue;
-    return launch_kernel(kTimeGemm, rows_tile_kernel<BM, BN, WAVES_M, WAVES_N, NBUF, OUT>, dim3((unsigned)total),
+    return launch_kernel(kTimeGemm, rows_tile_kernel<BM, BN, WAVES_M, WAVES_N, NBUF, OUT, WIDE>, dim3((unsigned)total),
                          dim3(WAVES_M * WAVES_N * 64), 0, stream, p);
+}
+
+constexpr int kMostLds = 160 * 1024;   // of a compute unit
+
+// Lets a kernel have `bytes` of LDS by its launch, once per device.
+static hipError_t allow_lds(const void* kernel, int bytes, std::atomic<bool>* allowed) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
+    if (allowed[dev].load(std::memory_order_acquire)) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) allowed[dev].store(true, std::memory_order_release);
+    return e;
 }
 
 // Few tiles: 8 XB tokens and 8 WB outputs per workgroup, the steps of K dealt over its NW waves, each with a ring of its own and no
@@ -398,23 +416,15 @@ __global__ __launch_bounds__(NW * 64) void rows_few_kernel(RowsGemm p) {
 template <int XB, int WB, int NW, int NBUF, Elem OUT>
 static hipError_t run_rows_few(RowsGemm p, hipStream_t stream) {
     constexpr int LDS = NW * NBUF * (XB + WB) * 1024;
-    static_assert(LDS <= 160 * 1024, "a compute unit's LDS");
+    static_assert(LDS <= kMostLds, "a compute unit's LDS");
     p.tiles_m = (int)ceil_div(p.M, XB * 8);
     p.tiles_n = (int)ceil_div(p.N, WB * 8);
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
     if (total > 0x7FFFFFFF || p.ksteps < 1) return hipErrorInvalidValue;
-    if constexpr (LDS > 65536) {                            // once per device
+    if constexpr (LDS > 65536) {
         static std::atomic<bool> allowed[kMaxDevices];
-        int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
+        const hipError_t e = allow_lds(reinterpret_cast<const void*>(&rows_few_kernel<XB, WB, NW, NBUF, OUT>), LDS, allowed);
         if (e != hipSuccess) return e;
-        if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
-        if (!allowed[dev].load(std::memory_order_acquire)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&rows_few_kernel<XB, WB, NW, NBUF, OUT>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-            if (e != hipSuccess) return e;
-            allowed[dev].store(true, std::memory_order_release);
-        }
     }
     return launch_kernel(kTimeGemm, rows_few_kernel<XB, WB, NW, NBUF, OUT>, dim3((unsigned)total), dim3(NW * 64),
                          (unsigned)LDS, stream, p);
@@ -434,6 +444,7 @@ static hipError_t run_rows_few(RowsGemm p, hipStream_t stream) {
 // 8192 x 4096 x 4178 256 x 256 132 (256 x 128 153, 128 x 128 177), 700 x 33001 x 1575 256 x 256 65 (192 x 128 75).
 template <Elem OUT>
 static hipError_t run_rows_gemm(const RowsGemm& p, hipStream_t stream) {
+    if (p.ldx >= kWidePitch || p.ldw >= kWidePitch) return run_rows_tile<64, 64, 2, 2, 4, OUT, true>(p, stream);
     const int64_t cus = compute_units(), per_cu = ceil_div(ceil_div(p.N, 8), cus);   // requests of 8 outputs a compute unit
 #define OCS_ROWS_FEW(XB)                                                        \
     (per_cu <= 2   ? run_rows_few<XB, 2, 8, 2, OUT>(p, stream)                  \

@@ -29,6 +29,32 @@ __device__ __forceinline__ int source_column(const RowGrids& p, int k, int* chan
     return p.g == 1 ? src : src * p.g + (k - j * p.g);
 }
 
+// The sources of columns k0 .. k0 + 3, those up to K being their own: four look-ups under way at once, whatever the columns are.
+struct FourSources {
+    int src[4], channel[4];
+};
+__device__ __forceinline__ FourSources four_sources(const RowGrids& p, int k0, int K, int Ke) {
+    FourSources f;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        f.src[b] = k0 + b;
+        f.channel[b] = 0;
+    }
+    if (p.s == 0 || k0 + 3 < K || k0 >= Ke) return f;
+    int looked[4], at[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const int k = k0 + b < Ke ? k0 + b : Ke - 1;
+        looked[b] = source_column(p, k, &at[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        f.src[b] = k0 + b < K ? k0 + b : looked[b];
+        f.channel[b] = at[b];
+    }
+    return f;
+}
+
 __device__ __forceinline__ float depth_factor(const RowGrids& p, int channel) {
     int d = p.chan_depth[channel];
     d = d < 0 ? 0 : (d > 255 ? 255 : d);
@@ -81,6 +107,8 @@ __global__ __launch_bounds__(256) void row_grid_kernel(RowGrids p) {
     int8_t* q = p.Xq + row * p.ldq;
     const int pieces = K / VEC, rest = K % VEC;
 
+    const int tail0 = pieces * VEC;
+    FourSources first = four_sources(p, tail0 + 4 * t, K, Ke);      // of this lane's first word behind the pieces
     u32x4 raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -136,23 +164,20 @@ __global__ __launch_bounds__(256) void row_grid_kernel(RowGrids p) {
         }
     }
     row_barrier<NT>();
-    const int tail0 = pieces * VEC;
     for (int k0 = tail0 + 4 * t; k0 < (int)p.ldq; k0 += 4 * NT) {
+        const FourSources f = k0 == tail0 + 4 * t ? first : four_sources(p, k0, K, Ke);
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (SCALED) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                if (k0 + b >= K && k0 + b < Ke) v[b] = elem_to_float<T>(x[f.src[b]]) * depth_factor(p, f.channel[b]);
+        }
         unsigned word = 0;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const int k = k0 + b;
-            unsigned byte = 0;
-            if (k < K) {
-                byte = (unsigned char)image[k];
-            } else if (k < Ke) {
-                int j;
-                const int src = source_column(p, k, &j);
-                if constexpr (SCALED)
-                    byte = code_bits(elem_to_float<T>(x[src]) * depth_factor(p, j), inv, p.qmax) & 0xFFu;
-                else
-                    byte = (unsigned char)image[src];
-            }
+            if (k0 + b >= Ke) continue;
+            unsigned byte = (unsigned char)image[k0 + b < K || !SCALED ? f.src[b] : 0];
+            if (SCALED && k0 + b >= K) byte = code_bits(v[b], inv, p.qmax) & 0xFFu;
             word |= byte << (8 * b);
         }
         *reinterpret_cast<unsigned*>(q + k0) = word;

@@ -443,6 +443,7 @@ __global__ __launch_bounds__(64) void token_join_kernel(TokenRows p) {
 
 // Logits that 1024 lanes hold, whatever their type: 16 pieces a lane of fp32, 8 of the others.
 constexpr int kHeldLogits = 65536;
+constexpr int64_t kMostPartRows = 2048;   // parts of all rows together: the workspace stays below a megabyte
 
 struct TokenPlan {
     int parts, part_len;
@@ -451,9 +452,10 @@ struct TokenPlan {
 // Rows that fill the chip have a workgroup each.  Fewer ones, longer than a workgroup holds, are cut into parts that it does.
 static TokenPlan plan_token_rows(int64_t M, int64_t V, int k) {
     TokenPlan t{1, (int)V, 0, 0};
-    if (M <= compute_units() && V > kHeldLogits) {
+    if (M <= compute_units() && M <= kMostPartRows / 2 && V > kHeldLogits) {
         int64_t parts = ceil_div(V, kHeldLogits);
-        parts = parts < kMostParts ? parts : kMostParts;
+        const int64_t most = kMostPartRows / M < kMostParts ? kMostPartRows / M : kMostParts;
+        parts = parts < most ? parts : most;
         t.part_len = (int)round_up(ceil_div(V, parts), 64);
         t.parts = (int)ceil_div(V, t.part_len);
         t.keys_off = (size_t)round_up(M * t.parts * 16, 256);

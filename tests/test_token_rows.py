@@ -231,6 +231,22 @@ def test_product_of_extreme_codes(M):
     _check_product(rng, M, 36, K, F32, False, extreme=True)
 
 
+@pytest.mark.parametrize("M,N,ldx,ldw", [(3, 5, 1 << 24, 128), (70, 3, 128, (1 << 24) + 64), (20, 40, (1 << 25) + 64, 192)])
+def test_product_of_pitches_whose_offsets_in_a_tile_pass_32_bits(M, N, ldx, ldw):
+    """A tile of 256 rows at a pitch of 2^24 bytes spans 2^32: 64-bit offsets."""
+    rng = np.random.default_rng(M)
+    K = 100
+    xq, wq = _random_codes(rng, M, K, 128), _random_codes(rng, N, K, 128)
+    big_x, big_w = torch.empty(M * ldx, dtype=torch.int8, device="cuda"), torch.empty(N * ldw, dtype=torch.int8, device="cuda")
+    x, w = big_x.view(M, ldx), big_w.view(N, ldw)
+    x[:, :128], w[:, :128] = G.dev(xq), G.dev(wq)
+    sx, sw = np.full(M, 0.01, np.float32), np.full(N, 0.02, np.float32)
+    y = torch.full((M, N), 7.0, device="cuda")
+    B.ocs_qgemm_rows(x, ldx, w, ldw, M, N, K, 8, 8, G.dev(sx), G.dev(sw), None, y, N)
+    torch.cuda.synchronize()
+    _check_y(y, xq.astype(np.float64) @ wq.astype(np.float64).T, sx, sw, None, F32, M, N)
+
+
 # ---- the layer -------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
