@@ -10,6 +10,8 @@ arithmetic happens here.
       forward(X[, threshold])      per batch: duplicate channels + quantize, GEMM (X1/X2, G1, G2)
   activation OCS (Eq. 4) with the channels chosen on the batch itself (Sec. 5.3):
       forward_act_ocs(W, X)        select on X, duplicate weights, halve + quantize X, GEMM
+  weight OCS with a grid per token and per output channel (TokenLayer), and what a language model's logits come
+      to (token_logprobs): log probabilities of given tokens, entropy, the most likely alternatives
 """
 import torch
 
@@ -297,3 +299,88 @@ class ConvChain:
         for i, L in enumerate(self.layers[1:-1], 1):
             H, W = L.conv_to_codes(Bn, H, W, self.layers[i + 1], thresholds[i + 1], True, None, stream)
         return self.layers[-1].conv(Bn, H, W, acc_out, stream)
+
+
+class TokenLayer:
+    """The layer of Eq. 3 with a grid of its own for every token (row of X) and every output channel (row of W), where
+    ExpandedLayer has one per tensor: an outlier token costs only itself precision.  X and Y in fp32, bf16 or fp16."""
+
+    def __init__(self, N, C, r, g=1, bits_w=8, bits_x=8, clip_ratio_w=1.0, clip_ratio_x=1.0, out_dtype=torch.float32,
+                 max_rows=None, device="cuda"):
+        self.N, self.C, self.g = int(N), int(C), int(g)
+        self.K = self.C * self.g
+        self.s = B.ocs_num_splits(self.C, r)
+        self.Ke = (self.C + self.s) * self.g
+        self.ldq = B.ocs_padded_cols(self.Ke)
+        self.bits_w, self.bits_x = int(bits_w), int(bits_x)
+        self.clip_ratio_w, self.clip_ratio_x = float(clip_ratio_w), float(clip_ratio_x)
+        self.out_dtype, self.device = out_dtype, device
+        E = self.C + self.s
+        i32 = dict(dtype=torch.int32, device=device)
+        self.split_src = torch.empty(max(self.s, 1), **i32)
+        self.chan_src = torch.empty(E, **i32)
+        self.chan_depth = torch.empty(E, **i32)
+        self.Wq = torch.empty((self.N, self.ldq), dtype=torch.int8, device=device)
+        self.step_w = torch.empty(self.N, dtype=torch.float32, device=device)
+        self.bias = None
+        self._rows = 0
+        self.Xq = self.step_x = self.Y = None
+        if max_rows:
+            self._ensure_rows(max_rows)
+
+    def _ensure_rows(self, M):
+        if M > self._rows:
+            self.Xq = torch.empty((M, self.ldq), dtype=torch.int8, device=self.device)
+            self.step_x = torch.empty(M, dtype=torch.float32, device=self.device)
+            self.Y = torch.empty((M, self.N), dtype=self.out_dtype, device=self.device)
+            self._rows = M
+
+    def prepare_weights(self, W, bias=None, stream=None):
+        """W fp32 [N, C*g] on the device -> split lists, Wq, step_w.  The channels are chosen on the whole tensor (Sec. 3.4) and
+        halved (Eq. 3), then every row gets its grid.  bias: fp32 [N] or None, kept by reference."""
+        assert W.dtype == torch.float32 and W.shape == (self.N, self.K) and W.stride(1) == 1
+        assert bias is None or (bias.dtype == torch.float32 and bias.shape == (self.N,) and bias.is_contiguous())
+        self.bias = bias
+        ws = B.alloc_workspace(self.N, self.K, self.device)
+        B.ocs_select_channels(W, self.N, self.C, self.g, W.stride(0), self.s, self.split_src, self.chan_src, self.chan_depth, None,
+                              ws, stream)
+        B.ocs_split_quantize_rows(W, self.N, self.C, self.g, W.stride(0), self.chan_src, self.chan_depth, self.s, self.bits_w,
+                                  self.clip_ratio_w, self.Wq, self.ldq, self.step_w, stream)
+        if stream is not None:
+            ws.record_stream(stream)
+
+    def forward(self, X, stream=None):
+        """X [M, C*g] in fp32, bf16 or fp16 -> Y [M, N] in out_dtype (M = 0 included)."""
+        assert X.dim() == 2 and X.shape[1] == self.K and (X.stride(1) == 1 or X.shape[0] == 0)
+        M = X.shape[0]
+        if M == 0:
+            return torch.empty((0, self.N), dtype=self.out_dtype, device=self.device)
+        self._ensure_rows(M)
+        B.ocs_forward_rows(X, M, self.C, self.g, X.stride(0) if M > 1 else self.K, self.chan_src, self.s, self.bits_x,
+                           self.clip_ratio_x, self.Xq, self.ldq, self.step_x, self.Wq, self.ldq, self.N, self.bits_w, self.step_w,
+                           self.bias, self.Y, self.N, stream)
+        return self.Y[:M]
+
+
+def token_logprobs(logits, tokens=None, top_k=0, stream=None):
+    """logits [M, V] in fp32, bf16 or fp16; tokens int32 [M] or None (a token outside 0 .. V-1: a position without one).
+    -> dict(entropy [M], logprob [M] with tokens, top_ids int32 / top_logprobs [M, top_k] with top_k > 0), all fp32 but the ids."""
+    assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[0] == 0)
+    M, V = logits.shape
+    assert tokens is None or (tokens.dtype == torch.int32 and tokens.shape == (M,) and tokens.is_contiguous())
+    f32 = dict(dtype=torch.float32, device=logits.device)
+    out = dict(entropy=torch.empty(M, **f32))
+    if tokens is not None:
+        out["logprob"] = torch.empty(M, **f32)
+    if top_k:
+        out["top_ids"] = torch.empty((M, top_k), dtype=torch.int32, device=logits.device)
+        out["top_logprobs"] = torch.empty((M, top_k), **f32)
+    need = B.ocs_token_logprobs_workspace_bytes(M, V, top_k)
+    ws = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+    B.ocs_token_logprobs(logits, M, V, logits.stride(0) if M > 1 else V, tokens, top_k, out.get("logprob"), out["entropy"],
+                         out.get("top_ids"), out.get("top_logprobs"), ws, stream)
+    if stream is not None:
+        for t in (*out.values(), ws):
+            if t is not None:
+                t.record_stream(stream)
+    return out

@@ -452,6 +452,73 @@ def test_the_same_bits_every_time():
             assert all(np.array_equal(a, b) for a, b in zip(first, _score(x.cuda(), t.cuda(), 5)))
 
 
+# ---- the layer and the scores as a program uses them -------------------------------------------
+
+def _oracle_layer(W, X, r, bits_w):
+    C = W.shape[1]
+    s = ref.num_splits(C, r)
+    sp = ref.split_weights(W, C, 1, s)
+    xe = X[:, sp["chan_src"]]
+    y = np.zeros((X.shape[0], W.shape[0]))
+    steps_w, rows_w = [], []
+    for n in range(W.shape[0]):
+        q, sc = ref.quantize(sp["T_out"][n:n + 1], bits_w)
+        rows_w.append(q[0].astype(np.float64))
+        steps_w.append(float(sc[1]))
+    for m in range(X.shape[0]):
+        q, sc = ref.quantize(np.ascontiguousarray(xe[m:m + 1]), 8)
+        y[m] = (np.stack(rows_w) @ q[0].astype(np.float64)) * (float(sc[1]) * np.array(steps_w))
+    return y
+
+
+@pytest.mark.parametrize("M,C,N,r,bits_w", [(1, 300, 50, 0.05, 8), (25, 300, 70, 0.05, 5), (70, 128, 33, 0.0, 8), (9, 64, 40, 0.3, 4)])
+def test_token_layer_against_the_oracle(M, C, N, r, bits_w):
+    from paper_1901_09504_amd.layer import TokenLayer, token_logprobs
+
+    rng = np.random.default_rng(C + N)
+    W = (rng.standard_normal((N, C)) * rng.random((N, 1))).astype(np.float32)
+    W[rng.integers(0, N, 5), rng.integers(0, C, 5)] *= 8
+    X = rng.standard_normal((M, C)).astype(np.float32)
+    head = TokenLayer(N, C, r, bits_w=bits_w)
+    head.prepare_weights(G.dev(W))
+    y = head.forward(G.dev(X))
+    torch.cuda.synchronize()
+    want = _oracle_layer(W, X, r, bits_w)
+    assert np.all(np.abs(y.cpu().numpy() - want) <= 4 * U * np.abs(want))
+    t = torch.from_numpy(rng.integers(-1, N, M).astype(np.int32)).cuda()
+    out = token_logprobs(y, t, 3)
+    lp, ent, ids, top = _score(y, t, 3)
+    assert np.array_equal(out["logprob"].cpu().numpy(), lp) and np.array_equal(out["entropy"].cpu().numpy(), ent)
+    assert np.array_equal(out["top_ids"].cpu().numpy(), ids) and np.array_equal(out["top_logprobs"].cpu().numpy(), top)
+    assert set(token_logprobs(y)) == {"entropy"}
+
+
+def test_no_tokens_and_one():
+    from paper_1901_09504_amd.layer import TokenLayer, token_logprobs
+
+    head = TokenLayer(40, 100, 0.05, out_dtype=BF16)
+    head.prepare_weights(torch.randn((40, 100), device="cuda"))
+    y = head.forward(torch.empty((0, 100), dtype=F16, device="cuda"))
+    assert y.shape == (0, 40) and y.dtype == BF16
+    out = token_logprobs(y, torch.empty(0, dtype=torch.int32, device="cuda"), 2)
+    assert [tuple(out[n].shape) for n in ("logprob", "entropy", "top_ids", "top_logprobs")] == [(0,), (0,), (0, 2), (0, 2)]
+    x = torch.randn((5, 100), device="cuda").to(F16)
+    every = head.forward(x).clone()
+    for m in range(5):                                      # a token's outputs do not depend on its company
+        assert torch.equal(head.forward(x[m:m + 1])[0], every[m])
+
+
+def test_scoring_command():
+    from paper_1901_09504_amd import score
+
+    rows = score.run(tokens=300, hidden=256, vocab=1000)
+    exact = rows[0][2]
+    eight = [p for bits, _, p, _ in rows if bits == 8]
+    four = [p for bits, _, p, _ in rows if bits == 4]
+    assert 1 < exact < 1000 and all(abs(p / exact - 1) < 0.05 for p in eight)
+    assert max(abs(p / exact - 1) for p in eight) < max(abs(p / exact - 1) for p in four)
+
+
 # ---- long offsets, streams, graphs -----------------------------------------------------------
 
 def test_offsets_beyond_32_bits():
