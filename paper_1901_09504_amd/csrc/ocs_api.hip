@@ -1012,11 +1012,8 @@ int ocs_forward_rows(const void* X, int type, int64_t M, int C, int g, int64_t l
     rc = check_gemm_operands(Xq, ldq, Wq, ldw, M == 0 ? 1 : M, N, Kexp, bits_x, bits_w, nullptr, 0);
     if (rc) return rc;
     if (M == 0) return OCS_OK;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e = launch_row_grids(X, type, ldx, M, C, g, num_splits, chan_src, nullptr, clip_ratio, qmax_of(bits_x), Xq, ldq,
-                                    step_x_out, st);
-    if (e == hipSuccess)
-        e = launch_qgemm_rows(Xq, ldq, Wq, ldw, M, N, Kexp, step_x_out, step_w, bias, Y, out_type, ldy, st);
+    hipError_t e = launch_forward_rows(X, type, ldx, M, C, g, num_splits, chan_src, clip_ratio, qmax_of(bits_x), Xq, ldq, step_x_out,
+                                       Wq, ldw, N, step_w, bias, Y, out_type, ldy, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? OCS_OK : hip_fail(e);
 }
 

@@ -8,7 +8,7 @@
 #include <atomic>
 #include <type_traits>
 
-#include "row_types.h"
+#include "row_grids.h"
 
 namespace ocs {
 
@@ -49,6 +49,17 @@ __device__ __forceinline__ void request_1k(const int8_t* base, unsigned offset, 
 #else
     (void)base;
     (void)offset;
+    (void)lds_addr;
+#endif
+}
+
+// 64 words, one per lane.
+__device__ __forceinline__ void request_256(const float* from, unsigned lds_addr) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const unsigned m0 = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(m0) : "memory");
+#else
+    (void)from;
     (void)lds_addr;
 #endif
 }
@@ -430,6 +441,264 @@ static hipError_t run_rows_few(RowsGemm p, hipStream_t stream) {
                          (unsigned)LDS, stream, p);
 }
 
+// The layer of few tokens as one launch, codes included.  Every workgroup puts all rows of X on their grids while the first weights are
+// on their way (64 pieces of a row at a time per wave, through LDS between the row's maximum and its codes), keeps the codes in LDS as
+// images of 8 rows x 128 bytes, and the workgroups share the writing of codes and steps to memory.  Then it goes over its shares of 8 WB
+// outputs, its 8 waves with K dealt over them: the weights' requests run two steps ahead of their use, from one share into the next, and
+// the waves' sums of a share meet in LDS (integer adds: any order gives the same bits).
+// What it buys is the second launch, which costs the host more than the work of a few tokens takes (see launch_forward_rows).
+constexpr int kImageWaves = 8, kImageRing = 2, kImageScales = 4, kImageTable = 2048;
+
+// Byte of the image that holds column k of row r.
+__device__ __forceinline__ int image_at(int r, int k, int ksteps) {
+    return ((r >> 3) * ksteps + (k >> 7)) * 1024 + (r & 7) * 128 + ((((k >> 4) & 7) ^ (r & 7)) << 4) + (k & 15);
+}
+
+struct ImageLds {
+    int scales, raw, image, sums, rows, table, total;     // byte offsets behind the ring
+};
+template <int XB, int WB>
+__host__ __device__ inline ImageLds image_lds(int segments, int ksteps, int copies) {
+    ImageLds l;
+    l.scales = kImageWaves * kImageRing * WB * 1024;
+    l.raw = l.scales + kImageScales * 256;
+    l.image = l.raw + segments * 1024;
+    l.sums = l.image + XB * 1024 * ksteps;
+    l.rows = l.sums + 2 * XB * 8 * (WB * 8 + 4) * 4;
+    l.table = l.rows + 3 * XB * 8 * 4;
+    l.total = l.table + (copies * 2 + 15) / 16 * 16;
+    return l;
+}
+
+// The rows of X into the image, by the whole workgroup; sx: their steps.  Ends with a barrier.
+template <Elem T>
+__device__ __forceinline__ void quantize_rows(const RowGrids& g, int ksteps, u32x4* raw, int8_t* image, float* sx, float* inv,
+                                              unsigned* big, unsigned short* table, int wave, int lane) {
+    constexpr int VEC = kVec<T>, NT = kImageWaves * 64, AHEAD = 4;
+    const int K = g.C * g.g, Ke = (g.C + g.s) * g.g, pieces = K / VEC, rest = K % VEC, M = (int)g.M, tid = wave * 64 + lane;
+    const int per_row = (pieces + (rest ? 1 : 0) + 63) / 64, segments = M * per_row, ldq = (int)g.ldq;
+    const auto mine = [&](int r) { return r % (int)gridDim.x == (int)blockIdx.x; };   // rows that this workgroup writes to memory
+    if (tid < M) big[tid] = 0u;
+    for (int k = K + tid; k < Ke; k += NT) {
+        int channel;
+        table[k - K] = (unsigned short)source_column(g, k, &channel);
+    }
+    __syncthreads();
+    for (int s0 = wave; s0 < segments; s0 += kImageWaves * AHEAD) {
+        u32x4 v[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int s = s0 + a * kImageWaves;
+            v[a] = u32x4{0u, 0u, 0u, 0u};
+            if (s < segments) {
+                const int r = s / per_row, i = (s - r * per_row) * 64 + lane;
+                const elem_t<T>* x = static_cast<const elem_t<T>*>(g.X) + (int64_t)r * g.ldx;
+                if (i < pieces) v[a] = load_piece<T>(x + i * VEC);
+                else if (i == pieces && rest) v[a] = load_partial<T>(x + i * VEC, rest);
+            }
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int s = s0 + a * kImageWaves;
+            if (s < segments) {
+                raw[s * 64 + lane] = v[a];
+                unsigned m = 0;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const unsigned q = magnitude(piece_elem<T>(v[a], e));
+                    m = q > m ? q : m;
+                }
+                m = wave_umax32(m);
+                if (lane == 0) atomicMax(&big[s / per_row], m);
+            }
+        }
+    }
+    __syncthreads();
+    if (tid < M) {
+        const float thr = g.clip * __uint_as_float(big[tid]), step = __fdiv_rn(thr, g.qmax);
+        inv[tid] = inv_step_of(thr, g.qmax);
+        sx[tid] = step;
+        if (mine(tid)) g.step[tid] = step;
+    }
+    __syncthreads();
+    for (int s = wave; s < segments; s += kImageWaves) {           // (the segments that this wave stored)
+        const int r = s / per_row, i = (s - r * per_row) * 64 + lane;
+        if (i >= pieces + (rest ? 1 : 0)) continue;
+        const u32x4 v = raw[s * 64 + lane];
+        const float f = inv[r];
+#pragma unroll
+        for (int d = 0; d < VEC / 4; ++d) {
+            const unsigned code = pack4(code_bits(piece_elem<T>(v, 4 * d), f, g.qmax), code_bits(piece_elem<T>(v, 4 * d + 1), f, g.qmax),
+                                        code_bits(piece_elem<T>(v, 4 * d + 2), f, g.qmax), code_bits(piece_elem<T>(v, 4 * d + 3), f, g.qmax));
+            *reinterpret_cast<unsigned*>(image + image_at(r, i * VEC + 4 * d, ksteps)) = code;
+            if (mine(r) && i < pieces) *reinterpret_cast<unsigned*>(g.Xq + r * g.ldq + i * VEC + 4 * d) = code;
+        }
+    }
+    __syncthreads();
+    // left-over columns, copies and padding, from the codes in the image (a word's own left-over bytes are written back as they are)
+    const int tail0 = pieces * VEC, end = ldq > ksteps * 128 ? ldq : ksteps * 128, words = (end - tail0) / 4;
+    for (int o = tid; o < M * words; o += NT) {
+        const int r = o / words, k0 = tail0 + 4 * (o - r * words);
+        unsigned word = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int k = k0 + b;
+            if (k < Ke) word |= (unsigned)(unsigned char)image[image_at(r, k < K ? k : table[k - K], ksteps)] << (8 * b);
+        }
+        if (k0 < ksteps * 128) *reinterpret_cast<unsigned*>(image + image_at(r, k0, ksteps)) = word;
+        if (mine(r) && k0 < ldq) *reinterpret_cast<unsigned*>(g.Xq + r * g.ldq + k0) = word;
+    }
+    __syncthreads();
+}
+
+template <int XB, int WB, Elem OUT>
+__global__ __launch_bounds__(kImageWaves * 64) void rows_image_kernel(RowsGemm p, RowGrids g, int type, int segments) {
+    constexpr int NW = kImageWaves, NT = NW * 64, XT = (XB + 1) / 2, WT = (WB + 1) / 2;
+    constexpr int STEP = WB * 1024, BN = WB * 8, PITCH = BN + 4, SUMS = XB * 8 * PITCH;
+    static_assert(BN <= 32, "the scales of a share are half of a request of 64 words");
+    extern __shared__ __align__(1024) int8_t rings[];
+    const int tid = (int)threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int8_t* ring = rings + wave * (kImageRing * STEP);
+    // the scales of the shares, four in turn (the first wave may ask for those of the share after next while this one's are in use):
+    // 32 of step_w, 32 of the bias
+    const ImageLds l = image_lds<XB, WB>(segments, p.ksteps, g.s * g.g);
+    int8_t* scales = rings + l.scales;
+    int8_t* image = rings + l.image;
+    int32_t* sums = reinterpret_cast<int32_t*>(rings + l.sums);
+    float* sx = reinterpret_cast<float*>(rings + l.rows);
+    const unsigned ring0 = lds_address(ring), scales0 = lds_address(scales);
+
+    const int piece = (lane & 7) ^ (lane >> 3);
+    const bool cut = p.ldw < (int64_t)p.ksteps * 128;
+    const int trips = (p.ksteps - wave + NW - 1) / NW;
+    const int shares = (p.tiles_n - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    // step `it` of this workgroup's share n; with a share's first step go its scales, in the first wave
+    auto fetch = [&](int n, int it, int buf) {
+        const int col0 = ((int)blockIdx.x + n * (int)gridDim.x) * BN, kt = it * NW + wave;
+        const int64_t k = (int64_t)kt * 128;
+        if (it == 0 && wave == 0) {
+            int c = col0 + (lane & 31);
+            c = c < p.N ? c : p.N - 1;
+            request_256(lane < 32 || p.bias == nullptr ? p.step_w + c : p.bias + c, scales0 + (unsigned)(n % kImageScales * 256));
+        }
+        const int8_t* base = p.Wq + (int64_t)col0 * p.ldw + k;
+#pragma unroll
+        for (int u = 0; u < WB; ++u) {
+            int r = u * 8 + (lane >> 3);
+            r = col0 + r < p.N ? r : p.N - 1 - col0;
+            const unsigned from = (unsigned)(r * p.ldw + piece * 16), to = ring0 + (unsigned)(buf * STEP + u * 1024);
+            if (cut && kt == p.ksteps - 1) request_1k(k + piece * 16 < p.ldw ? base + from : rows_zero_chunk, to);
+            else request_1k(base, from, to);
+        }
+    };
+    const int total = trips > 0 ? shares * trips : 0;
+    int next_n = 0, next_it = 0;                                   // what is to be requested next
+    auto fetch_next = [&](int buf) {
+        fetch(next_n, next_it, buf);
+        if (++next_it == trips) {
+            next_it = 0;
+            ++next_n;
+        }
+    };
+    if (0 < total) fetch_next(0);
+    if (1 < total) fetch_next(1);
+    {
+        u32x4* raw = reinterpret_cast<u32x4*>(rings + l.raw);
+        float* inv = sx + XB * 8;
+        unsigned* big = reinterpret_cast<unsigned*>(sx + 2 * XB * 8);
+        unsigned short* table = reinterpret_cast<unsigned short*>(rings + l.table);
+        if (type == (int)Elem::f32) quantize_rows<Elem::f32>(g, p.ksteps, raw, image, sx, inv, big, table, wave, lane);
+        else if (type == (int)Elem::bf16) quantize_rows<Elem::bf16>(g, p.ksteps, raw, image, sx, inv, big, table, wave, lane);
+        else quantize_rows<Elem::f16>(g, p.ksteps, raw, image, sx, inv, big, table, wave, lane);
+    }
+    for (int i = tid; i < 2 * SUMS; i += NT) sums[i] = 0;
+    __syncthreads();
+
+    const int fr = lane & 15, fq = lane >> 4;
+    int done = 0;
+    for (int n = 0; n < shares; ++n) {
+        i32x4 acc[WT][XT];
+#pragma unroll
+        for (int i = 0; i < WT; ++i)
+#pragma unroll
+            for (int j = 0; j < XT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+        for (int it = 0; it < trips; ++it, ++done) {
+            // what may still be under way: the step after this one, with its scales if it begins a share
+            if (done + 1 >= total) wait_requests<0>();
+            else if (it + 1 == trips && wave == 0) wait_requests<WB + 1>();
+            else wait_requests<WB>();
+            const int buf = done & 1;
+            const int8_t* at = ring + buf * STEP;
+            const int8_t* xat = image + (it * NW + wave) * 1024;
+            i32x4 x[2][XT], w[2][WT];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const int slot = ((ks * 4 + fq) ^ (fr & 7)) * 16;
+#pragma unroll
+                for (int j = 0; j < XT; ++j) {                     // (a tile without its last 8 rows reads its first ones twice)
+                    const int xb = 2 * j + (2 * j + 1 < XB ? fr >> 3 : 0);
+                    x[ks][j] = *reinterpret_cast<const i32x4*>(xat + xb * p.ksteps * 1024 + (fr & 7) * 128 + slot);
+                }
+#pragma unroll
+                for (int i = 0; i < WT; ++i)
+                    w[ks][i] = *reinterpret_cast<const i32x4*>(at + (i * 16 + (2 * i + 1 < WB ? fr : fr & 7)) * 128 + slot);
+            }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int i = 0; i < WT; ++i)
+#pragma unroll
+                    for (int j = 0; j < XT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[ks][i], x[ks][j], acc[i][j], 0, 0, 0);
+            if (done + 2 < total) {
+                __builtin_amdgcn_sched_barrier(0);                 // the reads of this buffer have returned: the products took them
+                __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+                fetch_next(buf);
+            }
+        }
+        int32_t* meet = sums + (n & 1) * SUMS;
+#pragma unroll
+        for (int i = 0; i < WT; ++i)
+#pragma unroll
+            for (int j = 0; j < XT; ++j) {
+                const int t = j * 16 + fr, c = i * 16 + fq * 4;
+                if (trips > 0 && t < XB * 8 && c < BN) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) atomicAdd(meet + t * PITCH + c + e, acc[i][j][e]);
+                }
+            }
+        // one barrier a share: who reads and clears this share's sums has done so before it comes to the next one's barrier, and the share
+        // after that is the next to add to them
+        __syncthreads();
+        const int col0 = ((int)blockIdx.x + n * (int)gridDim.x) * BN;
+        const float* sw = reinterpret_cast<const float*>(scales + n % kImageScales * 256);
+        for (int o = tid; o < p.M * BN; o += NT) {
+            const int t = o / BN, c = o - t * BN;
+            const int a = meet[t * PITCH + c];
+            meet[t * PITCH + c] = 0;
+            if (col0 + c >= p.N) continue;
+            float v = (float)a * (sx[t] * sw[c]);
+            if (p.bias) v += sw[32 + c];
+            static_cast<elem_t<OUT>*>(p.Y)[(int64_t)t * p.ldy + col0 + c] = float_to_elem<OUT>(v);
+        }
+    }
+}
+
+template <int XB, int WB, Elem OUT>
+static hipError_t run_rows_image(RowsGemm p, const RowGrids& g, int type, int segments, hipStream_t stream) {
+    const int lds = image_lds<XB, WB>(segments, p.ksteps, g.s * g.g).total;
+    if (lds > kMostLds || p.M > XB * 8 || p.ksteps < 1) return hipErrorInvalidValue;
+    static std::atomic<bool> allowed[kMaxDevices];
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&rows_image_kernel<XB, WB, OUT>), kMostLds, allowed);
+    if (e != hipSuccess) return e;
+    // as many shares for every workgroup as for the busiest
+    p.tiles_n = (int)ceil_div(p.N, WB * 8);
+    const int64_t rounds = ceil_div(p.tiles_n, compute_units());
+    return launch_kernel(kTimeGemm, rows_image_kernel<XB, WB, OUT>, dim3((unsigned)ceil_div(p.tiles_n, rounds)),
+                         dim3(kImageWaves * 64), (unsigned)lds, stream, p, g, type, segments);
+}
+
 // The kernel by shape.
 //
 // Up to 32 tokens: the weights' bytes are what is to be had, and every workgroup takes all tokens and a share of the outputs; the
@@ -475,6 +744,40 @@ static hipError_t run_rows_gemm(const RowsGemm& p, hipStream_t stream) {
     }
 }
 
+// The layer as one launch where that serves (up to 32 tokens whose rows, codes and rings fit LDS) and pays.  Every workgroup repeats the
+// pass over the rows, some 2 us and 0.07 us for each segment of 64 pieces; a launch of its own takes the pass 2.7 us and the host 3.7.
+// Up to 24 segments where the host launches, up to 12, or 24 with a long list of outputs, in a stream that is being captured (calls one
+// after the other / from a graph, us, two launches and one: 1 x 256 -> 256 9.0 / 4.4, 5.4 / 4.4; 20 x 256 -> 256, 20 segments, 9.1 / 5.1, 6.8 /
+// 6.4; 1 x 3000 -> 6000, 12, 9.1 / 8.5, 8.2 / 8.2; 4 x 1500 -> 6000, 24, 9.0 / 6.4, 7.4 / 7.3; 4 x 1500 -> 33001 15.2 / 15.2, 14.4 / 14.4;
+// 20 x 600 -> 2000, 60, 9.2 / 5.3, 9.2 / 8.9; 4 x 3000 -> 6000, 48, 9.0 / 8.8, 11.2 / 11.2).
+template <Elem OUT>
+static hipError_t run_forward_rows(const RowsGemm& p, const RowGrids& g, int type, hipStream_t stream, bool* served) {
+    *served = false;
+    const int64_t K = (int64_t)g.C * g.g, copies = (int64_t)g.s * g.g;
+    if (p.M > 24 || K > 16384 || copies > kImageTable || p.ldw >= kWidePitch || g.ldq > 65536) return hipSuccess;
+    const int segments = p.M * (int)ceil_div(ceil_div(K, type == (int)Elem::f32 ? 4 : 8), 64);
+    if (segments > 24) return hipSuccess;
+    if (segments > 12 && p.N <= 64 * compute_units() && stream != nullptr) {   // (the null stream is never captured)
+        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+        const hipError_t e = hipStreamIsCapturing(stream, &status);
+        if (e != hipSuccess) return e;
+        if (status != hipStreamCaptureStatusNone) return hipSuccess;
+    }
+    const bool narrow = ceil_div(p.N, 16) <= compute_units();
+#define OCS_ROWS_IMAGE(XB)                                                                                             \
+    if (p.M <= XB * 8) {                                                                                               \
+        *served = image_lds<XB, 4>(segments, p.ksteps, (int)copies).total <= kMostLds;                                 \
+        if (!*served) return hipSuccess;                                                                               \
+        return narrow ? run_rows_image<XB, 2, OUT>(p, g, type, segments, stream)                                       \
+                      : run_rows_image<XB, 4, OUT>(p, g, type, segments, stream);                                      \
+    }
+    OCS_ROWS_IMAGE(1)
+    OCS_ROWS_IMAGE(2)
+    OCS_ROWS_IMAGE(3)
+#undef OCS_ROWS_IMAGE
+    return hipSuccess;
+}
+
 hipError_t launch_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, int64_t ldw, int64_t M, int64_t N, int64_t Kexp,
                              const float* step_x, const float* step_w, const float* bias, void* Y, int out_type, int64_t ldy,
                              hipStream_t stream) {
@@ -485,6 +788,26 @@ hipError_t launch_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, in
         case Elem::f16: return run_rows_gemm<Elem::f16>(p, stream);
     }
     return hipErrorInvalidValue;
+}
+
+hipError_t launch_forward_rows(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src,
+                               float clip, float qmax, int8_t* Xq, int64_t ldq, float* step_x, const int8_t* Wq, int64_t ldw,
+                               int64_t N, const float* step_w, const float* bias, void* Y, int out_type, int64_t ldy,
+                               hipStream_t stream) {
+    const int64_t Kexp = (int64_t)(C + s) * g;
+    const RowsGemm p{Xq, ldq, Wq, ldw, (int)M, (int)N, (int)ceil_div(Kexp, 128), step_x, step_w, bias, Y, ldy, 0, 0};
+    const RowGrids rows{X, ldx, M, C, g, s, chan_src, nullptr, clip, qmax, Xq, ldq, step_x};
+    bool served = false;
+    hipError_t e = hipErrorInvalidValue;
+    switch (static_cast<Elem>(out_type)) {
+        case Elem::f32: e = run_forward_rows<Elem::f32>(p, rows, type, stream, &served); break;
+        case Elem::bf16: e = run_forward_rows<Elem::bf16>(p, rows, type, stream, &served); break;
+        case Elem::f16: e = run_forward_rows<Elem::f16>(p, rows, type, stream, &served); break;
+    }
+    if (e != hipSuccess || served) return e;
+    e = launch_row_grids(X, type, ldx, M, C, g, s, chan_src, nullptr, clip, qmax, Xq, ldq, step_x, stream);
+    if (e != hipSuccess) return e;
+    return launch_qgemm_rows(Xq, ldq, Wq, ldw, M, N, Kexp, step_x, step_w, bias, Y, out_type, ldy, stream);
 }
 
 }  // namespace ocs

@@ -291,6 +291,69 @@ def test_layer_call_is_its_two_steps(dtype, M, C, g, s, N):
     assert np.all(np.abs(got - want) <= bound + (HALF_STEP[dtype] + 8 * U) * np.abs(got) + 1e-6)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("M,C,g,s,N", [(1, 1, 1, 0, 1), (1, 5, 1, 2, 17), (3, 100, 1, 0, 33), (24, 60, 1, 6, 40), (20, 256, 1, 13, 256),
+                                       (17, 255, 1, 3, 4097), (9, 130, 1, 7, 4100), (8, 511, 1, 20, 8200), (2, 40, 9, 3, 100),
+                                       (5, 900, 1, 45, 9000), (1, 6000, 1, 300, 300), (1, 1000, 1, 50, 25000), (7, 64, 1, 4, 25001),
+                                       (1, 1029, 1, 0, 8193), (12, 300, 1, 400, 70)])
+def test_layer_of_few_tokens_is_its_two_steps(dtype, M, C, g, s, N):
+    """The layer as one launch: one share of outputs a workgroup or several, waves without a step of K, rows with a last partial
+    piece, more copies than channels, a pitch beyond the steps; from a graph as well."""
+    rng = np.random.default_rng(M * 31 + C + N)
+    src, depth = _lists(rng, C, s)
+    Ke = (C + s) * g
+    x = _strided(torch.from_numpy(rng.standard_normal((M, C * g)).astype(np.float32)).to(dtype), C * g + 1, 3, float("inf"))
+    ldq, ldw = B.ocs_padded_cols(Ke) + 128 * (M % 2), max(B.ocs_padded_cols(Ke), 64)
+    wq = G.dev(_random_codes(rng, N, Ke, ldw))
+    sw = G.dev((rng.random(N) * 0.02 + 1e-4).astype(np.float32))
+    bias = G.dev(rng.standard_normal(N).astype(np.float32)) if N % 2 else None
+    srcd = G.dev(src)
+
+    def outputs():
+        return (torch.full((M, ldq), 77, dtype=torch.int8, device="cuda"), torch.full((M,), -1.0, device="cuda"),
+                _strided(torch.full((M, N), 7.0, dtype=dtype), N + 3, 1, 7.0))
+
+    def layer(o):
+        B.ocs_forward_rows(x, M, C, g, x.stride(0), srcd, s, 8, 0.9, o[0], ldq, o[1], wq, ldw, N, 6, sw, bias, o[2], o[2].stride(0))
+
+    two, one, captured = outputs(), outputs(), outputs()
+    B.ocs_split_quantize_rows(x, M, C, g, x.stride(0), srcd, None, s, 8, 0.9, two[0], ldq, two[1])
+    B.ocs_qgemm_rows(two[0], ldq, wq, ldw, M, N, Ke, 8, 6, two[1], sw, bias, two[2], two[2].stride(0))
+    layer(one)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(two, one))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer(captured)
+    for _ in range(3):
+        for a in captured:
+            a.fill_(5)
+        captured[2][:, N:] = 7.0
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(two, captured))
+
+
+def test_bad_rows_of_few_tokens_stay_alone():
+    rng = np.random.default_rng(3)
+    M, C, N = 6, 300, 50
+    x = torch.from_numpy(rng.standard_normal((M, C)).astype(np.float32))
+    x[1, 7], x[3, 299], x[5] = float("nan"), float("inf"), 0.0
+    src, _ = _lists(rng, C, 9)
+    src[C:C + 2] = [-7, 1 << 20]                             # clamped
+    wq = G.dev(_random_codes(rng, N, C + 9, 384))
+    sw = torch.ones(N, device="cuda")
+    xq, sx = torch.empty((M, 384), dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    y = torch.empty((M, N), device="cuda")
+    B.ocs_forward_rows(x.cuda(), M, C, 1, C, G.dev(src), 9, 8, 1.0, xq, 384, sx, wq, 384, N, 8, sw, None, y, N)
+    y, q = G.host(y), G.host(xq).astype(np.float64)
+    assert not np.isfinite(y[[1, 3]]).any() and (y[5] == 0).all()
+    for m in (0, 2, 4):
+        want = (G.host(wq)[:, :C + 9].astype(np.float64) @ q[m, :C + 9]) * float(G.host(sx)[m])
+        assert np.all(np.abs(y[m] - want) <= 4 * U * np.abs(want))
+        assert q[m, C] == q[m, 0] and q[m, C + 1] == q[m, C - 1]
+
+
 # ---- scoring ---------------------------------------------------------------------------------
 
 def _score(x, tokens, k, want_entropy=True, stream=None):
