@@ -11,6 +11,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libocs.so")
+CALLS_PATH = os.path.join(_HERE, "_rows_call.so")
 
 KALIGN = 64
 MODE_HALVE = 0
@@ -430,30 +431,36 @@ def ocs_qgemm_split_k(Xq, ldx, Wq, ldw, M, N, Kexp, bits_x, bits_w, scale_x, sca
 
 # ---- a grid per row, and the scoring of tokens (element types are the tensors' own) ------------
 
-def _type(t):
-    return -1 if t is None else TYPES.get(t.dtype, -1)
+_rows_call = None
 
 
-def _bias(t):
-    """bias: fp32 [N], or None or False for a layer without."""
-    return None if t is None or t is False else t.data_ptr()
+def _calls():
+    """The module that makes these four calls (csrc/rows_call.cpp), built with libocs.so."""
+    global _rows_call
+    if _rows_call is None:
+        lib()
+        if not os.path.exists(CALLS_PATH):
+            raise FileNotFoundError(f"{CALLS_PATH} is missing: build it with `python -m paper_1901_09504_amd.build`")
+        from . import _rows_call as module
+
+        module.bind(*TYPES, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        _rows_call = module
+    return _rows_call
 
 
 def ocs_split_quantize_rows(X, M, Cn, g, ldx, chan_src, chan_depth, num_splits, bits, clip_ratio, Xq, ldq, step_out, stream=None):
-    _check(lib().ocs_split_quantize_rows(_ptr(X), _type(X), M, Cn, g, ldx, _ptr(chan_src), _ptr(chan_depth), num_splits, bits,
-                                         clip_ratio, _ptr(Xq), ldq, _ptr(step_out), _stream(stream)), "ocs_split_quantize_rows")
+    _check(_calls().split_quantize_rows(X, M, Cn, g, ldx, chan_src, chan_depth, num_splits, bits, clip_ratio, Xq, ldq, step_out,
+                                        stream), "ocs_split_quantize_rows")
 
 
 def ocs_qgemm_rows(Xq, ldx, Wq, ldw, M, N, Kexp, bits_x, bits_w, step_x, step_w, bias, Y, ldy, stream=None):
-    _check(lib().ocs_qgemm_rows(_ptr(Xq), ldx, _ptr(Wq), ldw, M, N, Kexp, bits_x, bits_w, _ptr(step_x), _ptr(step_w), _bias(bias),
-                                _ptr(Y), _type(Y), ldy, _stream(stream)), "ocs_qgemm_rows")
+    _check(_calls().qgemm_rows(Xq, ldx, Wq, ldw, M, N, Kexp, bits_x, bits_w, step_x, step_w, bias, Y, ldy, stream), "ocs_qgemm_rows")
 
 
 def ocs_forward_rows(X, M, Cn, g, ldx, chan_src, num_splits, bits_x, clip_ratio, Xq, ldq, step_x_out, Wq, ldw, N, bits_w, step_w,
                      bias, Y, ldy, stream=None):
-    _check(lib().ocs_forward_rows(_ptr(X), _type(X), M, Cn, g, ldx, _ptr(chan_src), num_splits, bits_x, clip_ratio, _ptr(Xq), ldq,
-                                  _ptr(step_x_out), _ptr(Wq), ldw, N, bits_w, _ptr(step_w), _bias(bias), _ptr(Y), _type(Y), ldy,
-                                  _stream(stream)), "ocs_forward_rows")
+    _check(_calls().forward_rows(X, M, Cn, g, ldx, chan_src, num_splits, bits_x, clip_ratio, Xq, ldq, step_x_out, Wq, ldw, N, bits_w,
+                                 step_w, bias, Y, ldy, stream), "ocs_forward_rows")
 
 
 def ocs_token_logprobs_workspace_bytes(M, V, top_k):
@@ -461,6 +468,5 @@ def ocs_token_logprobs_workspace_bytes(M, V, top_k):
 
 
 def ocs_token_logprobs(logits, M, V, ld, tokens, top_k, logprob, entropy, top_ids, top_logprobs, workspace=None, stream=None):
-    w, wb = _ws(workspace)
-    _check(lib().ocs_token_logprobs(_ptr(logits), _type(logits), M, V, ld, _ptr(tokens), top_k, _ptr(logprob), _ptr(entropy),
-                                    _ptr(top_ids), _ptr(top_logprobs), w, wb, _stream(stream)), "ocs_token_logprobs")
+    _check(_calls().token_logprobs(logits, M, V, ld, tokens, top_k, logprob, entropy, top_ids, top_logprobs, workspace, stream),
+           "ocs_token_logprobs")

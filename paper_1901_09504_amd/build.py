@@ -1,10 +1,12 @@
-"""Builds libocs.so (hand-written HIP for gfx950) in-tree with hipcc."""
+"""Builds libocs.so (hand-written HIP for gfx950) in-tree with hipcc, and the Python side of its most frequent calls with g++."""
 import os
 import subprocess
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libocs.so")
+CALLS = os.path.join(_HERE, "_rows_call.so")
 SOURCES = ["ocs_api.hip", "reduce.hip", "select.hip", "quantize.hip", "qa_split.hip", "clip_search.hip", "qgemm.hip", "row_grids.hip",
            "qgemm_rows.hip", "token_logprobs.hip", "calib.hip"]
 
@@ -30,7 +32,20 @@ def build_library(verbose=False):
         raise RuntimeError("hipcc failed:\n" + out)
     if verbose and out.strip():
         print(out)
+    build_calls(verbose)
     return LIB
+
+
+def build_calls(verbose=False):
+    """Compile paper_1901_09504_amd/_rows_call.so, which finds libocs.so beside itself."""
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I" + sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "rows_call.cpp"), "-o", CALLS, "-L" + _HERE, "-l:libocs.so", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd))
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stdout)
+    return CALLS
 
 
 if __name__ == "__main__":

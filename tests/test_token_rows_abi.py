@@ -113,3 +113,55 @@ def test_binding_refuses_other_element_types(dtype):
     with pytest.raises(B.OcsError) as e:
         B.ocs_token_logprobs(x, 2, 8, 8, None, 0, None, f, None, None, stream=type("S", (), {"cuda_stream": 0}))
     assert e.value.code == -11
+
+
+class _NullStream:
+    cuda_stream = 0
+
+
+def test_binding_refuses_arguments_of_other_kinds():
+    """Python errors, not codes and not crashes; what fits neither 32 nor 64 bits is no smaller number."""
+    x, f, i = torch.zeros((0, 8)), torch.zeros(0), torch.zeros(0, dtype=torch.int32)
+
+    def score(x=x, M=0, V=8, ld=8, tokens=i, k=2, lp=f, ws=None, stream=_NullStream):
+        B.ocs_token_logprobs(x, M, V, ld, tokens, k, lp, f, i, f, ws, stream)
+
+    score()
+    score(ws=torch.zeros(4, dtype=torch.uint8))
+    for bad in (dict(M="0"), dict(V=None), dict(x=3), dict(tokens="x"), dict(k=1.5), dict(ws=7), dict(stream=3)):
+        with pytest.raises((TypeError, AttributeError)):
+            score(**bad)
+    for bad in (dict(k=1 << 31), dict(k=-(1 << 31) - 1), dict(V=1 << 63), dict(M=1 << 70)):
+        with pytest.raises(OverflowError):
+            score(**bad)
+    with pytest.raises(B.OcsError) as e:
+        score(x=None)                                        # nothing has no element type
+    assert e.value.code == -11
+
+
+def test_binding_passes_every_argument_to_its_place():
+    """One wrong argument at a time, and no tokens: the code tells which one arrived where."""
+    x, q, f = torch.zeros((0, 40)), torch.zeros((0, 48), dtype=torch.int8), torch.zeros(0)
+    src, w, sw, y = torch.zeros(43, dtype=torch.int32), torch.zeros((10, 48), dtype=torch.int8), torch.zeros(10), torch.zeros((0, 10))
+    half = torch.zeros((0, 10), dtype=torch.float64)
+
+    def quantize(x=x, M=0, C=40, g=1, ldx=40, src=src, s=3, bits=8, clip=1.0, ldq=48):
+        B.ocs_split_quantize_rows(x, M, C, g, ldx, src, None, s, bits, clip, q, ldq, f, _NullStream)
+
+    def product(ldx=48, w=w, ldw=48, M=0, N=10, K=43, bx=8, bw=8, sw=sw, bias=None, y=y, ldy=10):
+        B.ocs_qgemm_rows(q, ldx, w, ldw, M, N, K, bx, bw, f, sw, bias, y, ldy, _NullStream)
+
+    def forward(x=x, M=0, C=40, g=1, ldx=40, src=src, s=3, bits=8, clip=1.0, ldq=48, w=w, ldw=48, N=10, bw=8, sw=sw, bias=False, y=y, ldy=10):
+        B.ocs_forward_rows(x, M, C, g, ldx, src, s, bits, clip, q, ldq, f, w, ldw, N, bw, sw, bias, y, ldy, _NullStream)
+
+    quantize(), product(), forward(), forward(bias=sw), product(bias=sw)
+    grids = [(dict(x=half), -11), (dict(C=0), -2), (dict(g=0), -2), (dict(ldx=39), -2), (dict(src=None), -1),
+             (dict(s=-1), -5), (dict(bits=9), -4), (dict(clip=0.0), -10), (dict(ldq=32), -2), (dict(ldq=56), -3)]
+    layer = [(dict(w=None), -1), (dict(ldw=32), -2), (dict(N=0), -2), (dict(bw=1), -4), (dict(sw=None), -1), (dict(y=half), -11),
+             (dict(ldy=9), -2), (dict(ldw=56), -3)]
+    own = [(dict(ldx=32), -2), (dict(ldx=56), -3), (dict(K=0), -2), (dict(K=49), -2), (dict(bx=1), -4)]
+    for call, cases in ((quantize, grids), (forward, grids + layer), (product, own + layer)):
+        for bad, code in cases:
+            with pytest.raises(B.OcsError) as e:
+                call(**bad)
+            assert e.value.code == code, (call.__name__, bad, e.value.code)
