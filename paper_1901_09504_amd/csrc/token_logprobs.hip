@@ -79,27 +79,30 @@ __device__ __forceinline__ void join_wave(Running& r) {
     r.w = wave_sum(r.w);
 }
 
-template <int N>
+// KNOWN: r.m is at least every one of the logits already.
+template <bool KNOWN = false, int N>
 __device__ __forceinline__ void add_logits(Running& r, const float (&v)[N]) {
-    float top = r.m;
+    if constexpr (!KNOWN) {
+        float top = r.m;
 #pragma unroll
-    for (int e = 0; e < N; ++e) top = fmaxf(top, v[e]);
-    if (top > r.m) raise(r, top);
+        for (int e = 0; e < N; ++e) top = fmaxf(top, v[e]);
+        if (top > r.m) raise(r, top);
+    }
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        const float d = v[e] - top;                 // -inf for a token ruled out, NaN stays NaN
+        const float d = v[e] - r.m;                 // -inf for a token ruled out, NaN stays NaN
         const float x = exp_of(d);
         r.s += x;
         r.w = __builtin_fmaf(fmaxf(d, -150.0f), x, r.w);
     }
 }
 
-template <Elem T>
+template <Elem T, bool KNOWN = false>
 __device__ __forceinline__ void add_piece(Running& r, u32x4 raw) {
     float v[kVec<T>];
 #pragma unroll
     for (int e = 0; e < kVec<T>; ++e) v[e] = piece_elem<T>(raw, e);
-    add_logits(r, v);
+    add_logits<KNOWN>(r, v);
 }
 
 // What a row comes to.
@@ -138,11 +141,13 @@ __device__ __forceinline__ unsigned bound_of(u32x4 keys, int k) {
     return bound;
 }
 
+typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+
 template <int NT, bool HELD>
 struct TopShared {
     alignas(16) unsigned group[kTopGroups];
     float wave_m[NT / 64], wave_s[NT / 64], wave_w[NT / 64];
-    unsigned long long list[kTopList];
+    alignas(16) unsigned long long list[kTopList];
     unsigned long long top[32];
     unsigned long long wave_key[NT / 64];
     int reach[HELD ? 1 : NT / 64][kTopGroups];                     // (a list per wave)
@@ -201,7 +206,7 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
             for (int e = 0; e < VEC; ++e) top = fmaxf(top, piece_elem<T>(raw[u], e));
         r.m = top;
 #pragma unroll
-        for (int u = 0; u < U; ++u) add_piece<T>(r, raw[u]);
+        for (int u = 0; u < U; ++u) add_piece<T, true>(r, raw[u]);
     } else {
         int i0 = 0;
         if (NT * U <= body) {
@@ -370,12 +375,19 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(TokenRows p) {
             if (wave != 0) return;
         } else {
             if (wave != 0) return;
-            const unsigned long long key = lane < got ? sh.list[lane] : 0ull;
+            // every lane counts the keys above its own, eight at a time from LDS (k = 20, some 50 keys: 1.5 us less than one by one out of
+            // the lanes); what follows the list reads as zero
+            if (lane >= got) sh.list[lane] = 0ull;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            const unsigned long long key = sh.list[lane];
             int ahead = 0;
-            for (int j = 0; j < got; ++j) {
-                const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(key >> 32), j);
-                const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)key, j);
-                ahead += (((unsigned long long)hi << 32) | lo) > key ? 1 : 0;
+            for (int j = 0; j < got; j += 8) {
+                u64x2 other[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) other[q] = *reinterpret_cast<const u64x2*>(&sh.list[j + 2 * q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) ahead += (other[q][0] > key ? 1 : 0) + (other[q][1] > key ? 1 : 0);
             }
             if (lane < got && ahead < want) sh.top[ahead] = key;
         }
