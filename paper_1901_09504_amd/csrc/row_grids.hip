@@ -205,7 +205,7 @@ static hipError_t run_row_grids(const RowGrids& p, hipStream_t stream) {
 template <Elem T>
 static hipError_t run_row_grids_of(const RowGrids& p, hipStream_t stream) {
     const int64_t K = (int64_t)p.C * p.g, pieces = ceil_div(K, kVec<T>);
-    if (p.ldq <= 0x7FFFFFFF) {
+    if (p.ldq <= 0x7FFFF000) {                            // (a row's 32-bit column passes its end by one round of the workgroup)
         // a wave per row while two pieces a lane hold it, then a workgroup
         if (pieces <= 64) return run_row_grids<T, 64, 1>(p, stream);
         if (pieces <= 128) return run_row_grids<T, 64, 2>(p, stream);

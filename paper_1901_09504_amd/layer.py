@@ -350,7 +350,8 @@ class TokenLayer:
             ws.record_stream(stream)
 
     def forward(self, X, stream=None):
-        """X [M, C*g] in fp32, bf16 or fp16 -> Y [M, N] in out_dtype (M = 0 included)."""
+        """X [M, C*g] in fp32, bf16 or fp16 -> Y [M, N] in out_dtype (M = 0 included), the layer's own buffer: the next call
+        writes to it again."""
         assert X.dim() == 2 and X.shape[1] == self.K and (X.stride(1) == 1 or X.shape[0] == 0)
         M = X.shape[0]
         if M == 0:
@@ -359,13 +360,16 @@ class TokenLayer:
         B.ocs_forward_rows(X, M, self.C, self.g, X.stride(0) if M > 1 else self.K, self.chan_src, self.s, self.bits_x,
                            self.clip_ratio_x, self.Xq, self.ldq, self.step_x, self.Wq, self.ldq, self.N, self.bits_w, self.step_w,
                            self.bias, self.Y, self.N, stream)
+        if stream is not None:                              # a larger batch may replace them while that stream still works
+            for t in (self.Xq, self.step_x, self.Y):
+                t.record_stream(stream)
         return self.Y[:M]
 
 
 def token_logprobs(logits, tokens=None, top_k=0, stream=None):
     """logits [M, V] in fp32, bf16 or fp16; tokens int32 [M] or None (a token outside 0 .. V-1: a position without one).
     -> dict(entropy [M], logprob [M] with tokens, top_ids int32 / top_logprobs [M, top_k] with top_k > 0), all fp32 but the ids."""
-    assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[0] == 0)
+    assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[0] == 0 or logits.shape[1] == 1)
     M, V = logits.shape
     assert tokens is None or (tokens.dtype == torch.int32 and tokens.shape == (M,) and tokens.is_contiguous())
     f32 = dict(dtype=torch.float32, device=logits.device)

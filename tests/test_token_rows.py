@@ -571,6 +571,36 @@ def test_no_tokens_and_one():
         assert torch.equal(head.forward(x[m:m + 1])[0], every[m])
 
 
+def test_layer_that_grows_while_another_stream_works():
+    """The buffers that a larger batch replaces are still the other stream's: what is allocated meanwhile does not land on them."""
+    from paper_1901_09504_amd.layer import TokenLayer
+
+    head = TokenLayer(6000, 1000, 0.05, max_rows=256)
+    head.prepare_weights(torch.randn((6000, 1000), device="cuda"))
+    small, large = torch.randn((256, 1000), device="cuda"), torch.randn((300, 1000), device="cuda")
+    want = head.forward(small).clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(20):
+        y = head.forward(small, side)
+    with torch.cuda.stream(side):
+        kept = y.clone()
+    del y
+    head.forward(large)                                     # replaces codes, steps and outputs
+    filler = [torch.full((256, 6000), 7.0, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(kept, want) and all(bool((f == 7.0).all()) for f in filler)
+
+
+def test_logits_of_one_token_in_any_layout():
+    from paper_1901_09504_amd.layer import token_logprobs
+
+    x = torch.randn((5, 3), device="cuda")
+    for col in (x[:, 1:2], x.t().contiguous().t()[:, 2:]):  # a column: its second stride means nothing
+        out = token_logprobs(col, torch.zeros(5, dtype=torch.int32, device="cuda"), 1)
+        assert not out["entropy"].any() and not out["logprob"].any() and not out["top_ids"].any()
+
+
 def test_scoring_command():
     from paper_1901_09504_amd import score
 
@@ -602,6 +632,18 @@ def test_offsets_beyond_32_bits():
     B.ocs_qgemm_rows(G.dev(xq), 256, G.dev(wq), 256, 3, 100, 200, 8, 8, G.dev(sx), G.dev(sw), None, y, ld)
     torch.cuda.synchronize()
     _check_y(y, xq[:, :200].astype(np.float64) @ wq[:, :200].astype(np.float64).T, sx, sw, None, BF16, 3, 100)
+
+
+def test_codes_into_rows_whose_end_is_near_2_to_31():
+    """The padding of such a row is walked past its end by less than a round; a 32-bit column would not hold that."""
+    x = torch.randn((1, 100), generator=torch.Generator().manual_seed(2)).cuda()
+    ldq = (1 << 31) - 16
+    big = torch.full((ldq,), 77, dtype=torch.int8, device="cuda")
+    step = torch.empty(1, device="cuda")
+    B.ocs_split_quantize_rows(x, 1, 100, 1, 100, None, None, 0, 8, 1.0, big, ldq, step)
+    q, want = _codes(x, 100, 1, None, None, 0, 8)
+    assert np.array_equal(G.host(big[:100]), q[0, :100]) and G.host(step)[0] == want[0]
+    assert not any(bool(part.any()) for part in big[100:].split(1 << 28))
 
 
 def _chain_state(M=20, C=500, s=25, V=40001, k=5):
