@@ -279,6 +279,57 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void rows_tile_kernel(RowsG
             }
         }
     };
+    if constexpr (OUT != Elem::f32) {
+        // Rows that begin between two words (every second one of an odd pitch): a store of 16 bytes there takes the time of several.  Such a
+        // row's lanes store one output further on, with the first of the next lane (the next tiles', behind the last lane), and what that
+        // leaves of the wave's columns, the first output and the last, goes by itself (256 x 256 tiles, us without / with: 333 x 2049 x 1052
+        // 28.4 / 19.7, 4000 x 6001 x 500 37.0 / 30.8, 8192 x 4097 x 4178 188 / 170; of 4098 outputs 160).
+        const bool odd_rows = (((unsigned)(uintptr_t)p.Y >> 1 | (unsigned)p.ldy) & 1) != 0;
+        if (odd_rows && col0 + BN <= p.N) {
+            constexpr int G = TN / 2;                                  // 16-byte pieces of a lane's outputs of a token
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                const int m = m0 + j * 16;
+                unsigned short* y = static_cast<unsigned short*>(p.Y) + (int64_t)m * p.ldy + n0;
+                const unsigned odd = ((unsigned)(uintptr_t)y >> 1) & 1;
+                unsigned w[G][5];
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        float a = (float)acc[i][j][e] * (sx[j] * sw[i][e]), b = (float)acc[i][j][e + 1] * (sx[j] * sw[i][e + 1]);
+                        if (p.bias) {
+                            a += bias[i][e];
+                            b += bias[i][e + 1];
+                        }
+                        w[i / 2][i % 2 * 2 + e / 2] = (unsigned)__builtin_bit_cast(unsigned short, float_to_elem<OUT>(a)) |
+                                                      (unsigned)__builtin_bit_cast(unsigned short, float_to_elem<OUT>(b)) << 16;
+                    }
+#pragma unroll
+                for (int i = 0; i < G; ++i)                            // (by all lanes, whatever their rows)
+                    w[i][4] = (unsigned)__builtin_amdgcn_ds_bpermute(((lane + 16) & 63) * 4, (int)(fq == 0 && i + 1 < G ? w[i + 1 < G ? i + 1 : i][0] : w[i][0]));
+                if (m >= p.M) continue;
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    u32x4 r;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) r[d] = __builtin_amdgcn_alignbit(w[i][d + 1], w[i][d], odd * 16);
+                    unsigned short* to = y + i * 32 + odd;
+                    if (i + 1 < G || fq != 3 || odd == 0) {
+                        *reinterpret_cast<u32x4_a4*>(to) = r;
+                    } else {
+                        *reinterpret_cast<u32x2_a4*>(to) = u32x2{r[0], r[1]};
+                        *reinterpret_cast<unsigned*>(to + 4) = r[2];
+                    }
+                }
+                if (odd != 0 && (fq == 0 || fq == 3)) {
+                    if (fq == 0) y[0] = (unsigned short)w[0][0];
+                    else y[(G - 1) * 32 + 7] = (unsigned short)(w[G - 1][3] >> 16);
+                }
+            }
+            return;
+        }
+    }
     if (whole && p.bias == nullptr) emit(std::true_type{}, std::false_type{});
     else if (whole) emit(std::true_type{}, std::true_type{});
     else emit(std::false_type{}, std::true_type{});
@@ -708,7 +759,9 @@ static hipError_t run_rows_image(RowsGemm p, const RowGrids& g, int type, int se
 // Beyond, while 64 x 16 (64 x 32) tiles are no more than the compute units, K is dealt over a workgroup's waves all the same (100 x 500 x
 // 3150 5.0 against 11.1 in 64 x 64 tiles, 1000 x 256 x 2000 5.6 / 7.9, 300 x 500 x 5000 7.9 / 15.7; 64 x 6000 x 3150 8.6 / 11.0).
 // Then tiles: rounds of the chip times what a tile takes, a constant and a cost per step in 10 ns, fitted to tiles of every size alone
-// and under load.  It finds the fastest of the five on all 19 shapes that were measured (us): 333 x 2049 x 1052 64 x 64 6.7 (128 x
+// and under load.  128 x 128 comes twice: a ring of three steps, and where there are more tiles than compute units one of two, of which a
+// unit holds two workgroups whose ends and starts hide behind each other (300 x 33001 x 1575 42.7 us in 192 x 128, 37.3 this way).  It
+// found the fastest of the first five on all 19 shapes that were measured (us): 333 x 2049 x 1052 64 x 64 6.7 (128 x
 // 128 10.7), 400 x 8000 x 3150 128 x 128 17.2 (64 x 64 24, 256 x 128 25.5), 700 x 6000 x 3150 192 x 128 23 (256 x 128 28, 128 x 128 33),
 // 8192 x 4096 x 4178 256 x 256 132 (256 x 128 153, 128 x 128 177), 700 x 33001 x 1575 256 x 256 65 (192 x 128 75).
 template <Elem OUT>
@@ -730,17 +783,19 @@ static hipError_t run_rows_gemm(const RowsGemm& p, hipStream_t stream) {
     const auto cost = [&](int64_t bm, int64_t bn, int64_t fixed, int64_t step) {
         return ceil_div(ceil_div(p.M, bm) * ceil_div(p.N, bn), cus) * (fixed + step * p.ksteps);
     };
-    const int64_t by_tile[5] = {cost(64, 64, 50, 26), cost(128, 128, 150, 58), cost(192, 128, 250, 72), cost(256, 128, 350, 92),
-                                cost(256, 256, 600, 150)};
+    const int64_t by_tile[6] = {cost(64, 64, 50, 26),    cost(128, 128, 150, 58),  cost(192, 128, 250, 72),
+                                cost(256, 128, 350, 92), cost(256, 256, 600, 150),
+                                ceil_div(ceil_div(p.M, 128) * ceil_div(p.N, 128), 2 * cus) * (450 + 95 * (int64_t)p.ksteps)};
     int best = 0;
-    for (int i = 1; i < 5; ++i)
+    for (int i = 1; i < 6; ++i)
         if (by_tile[i] < by_tile[best]) best = i;
     switch (best) {
         case 0: return run_rows_tile<64, 64, 2, 2, 4, OUT>(p, stream);
         case 1: return run_rows_tile<128, 128, 2, 4, 3, OUT>(p, stream);
         case 2: return run_rows_tile<192, 128, 2, 4, 3, OUT>(p, stream);
         case 3: return run_rows_tile<256, 128, 4, 2, 3, OUT>(p, stream);
-        default: return run_rows_tile<256, 256, 2, 4, 2, OUT>(p, stream);
+        case 4: return run_rows_tile<256, 256, 2, 4, 2, OUT>(p, stream);
+        default: return run_rows_tile<128, 128, 2, 4, 2, OUT>(p, stream);
     }
 }
 

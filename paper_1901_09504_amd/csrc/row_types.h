@@ -31,6 +31,7 @@ constexpr int kVec = 16 / (int)sizeof(elem_t<T>);   // elements of a 16-byte pie
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned u32x2_a4 __attribute__((ext_vector_type(2), aligned(4)));
 typedef unsigned u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 
 template <Elem T>

@@ -213,6 +213,20 @@ def test_product_into_any_pitch_and_alignment(M, dtype):
         _check_product(rng, M, N, 200, dtype, True, ld_extra=extra, off=off)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("M,N,K", [(333, 2049, 1052), (1500, 2049, 1000), (1000, 4099, 600), (2000, 4001, 1000), (2000, 8001, 500),
+                                   (300, 20001, 900)])
+def test_product_into_rows_that_begin_between_two_words(dtype, M, N, K):
+    """Tiles of every size: every second row of an odd pitch, and every row of an even one from an odd base; with a last column of
+    tiles that is not whole."""
+    rng = np.random.default_rng(M + N)
+    _check_product(rng, M, N, K, dtype, True)
+    _check_product(rng, M, N - 1, K, dtype, False, ld_extra=3, off=1)
+    if M == 333:
+        for off in (0, 1):
+            _check_product(rng, M, 2048, K, dtype, True, ld_extra=off * 2, off=1)
+
+
 @pytest.mark.parametrize("M,N", [(1, 40), (7, 50), (20, 70), (64, 33), (130, 140), (300, 260)])
 def test_product_of_pitches_that_end_inside_a_step(M, N):
     rng = np.random.default_rng(N)
