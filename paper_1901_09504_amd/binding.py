@@ -1,4 +1,4 @@
-"""Thin Python binding of libocs.so (ctypes): argument marshalling only.
+"""Thin Python binding of libocs.so (ctypes; _rows_call.so for the calls of generation): argument marshalling only.
 
 Every step of the path runs in the HIP kernels behind the C ABI declared in include/ocs.h;
 PyTorch supplies device memory and the stream, nothing else.  There is no fallback: if the

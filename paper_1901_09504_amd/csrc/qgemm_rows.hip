@@ -799,20 +799,24 @@ static hipError_t run_rows_gemm(const RowsGemm& p, hipStream_t stream) {
     }
 }
 
-// The layer as one launch where that serves (up to 32 tokens whose rows, codes and rings fit LDS) and pays.  Every workgroup repeats the
-// pass over the rows, some 2 us and 0.07 us for each segment of 64 pieces; a launch of its own takes the pass 2.7 us and the host 3.7.
-// Up to 24 segments where the host launches, up to 12, or 24 with a long list of outputs, in a stream that is being captured (calls one
-// after the other / from a graph, us, two launches and one: 1 x 256 -> 256 9.0 / 4.4, 5.4 / 4.4; 20 x 256 -> 256, 20 segments, 9.1 / 5.1, 6.8 /
-// 6.4; 1 x 3000 -> 6000, 12, 9.1 / 8.5, 8.2 / 8.2; 4 x 1500 -> 6000, 24, 9.0 / 6.4, 7.4 / 7.3; 4 x 1500 -> 33001 15.2 / 15.2, 14.4 / 14.4;
-// 20 x 600 -> 2000, 60, 9.2 / 5.3, 9.2 / 8.9; 4 x 3000 -> 6000, 48, 9.0 / 8.8, 11.2 / 11.2).
+// The layer as one launch where that serves (up to 16 tokens whose rows, codes and rings fit LDS) and pays.  Every workgroup repeats the
+// pass over the rows, some 2 us and 0.07 us for each segment of 64 pieces; a launch of its own takes the pass 2.7 us and the host 3.2.
+// Outputs that a compute unit has one share of: up to 16 segments where the host launches, up to 8 in a stream that is being captured,
+// rows of up to 20 steps (calls one after the other / from a graph, us, two launches and one, weights rotating: 1 x 250 -> 4000 6.9 / 4.7,
+// 4.6 / 4.4; 8 x 250 -> 4000, 8 segments, 6.9 / 5.4, 5.0 / 4.8; 4 x 1000 -> 4000, 16, 6.9 / 6.1; 20 x 250 -> 4000, 20, 6.9 / 7.1; 1 x 2000 ->
+// 4000 6.9 / 6.0, 6.0 / 5.8; 2 x 3000 -> 4000 7.2 / 7.9).  More shares a unit: not until there are so many that the next share's weights,
+// asked for while this one's are summed up, make good for the pass (1 x 1000 -> 12000 6.8 / 7.5; 1 x 500 -> 33001 9.2 / 8.4, 1 x 3000 -> 33001
+// 24.6 / 22.7, 4 x 1000 -> 33001, 16 segments, 12.0 / 12.5; rows of two steps 1 x 250 -> 33001 7.7 / 8.1).
 template <Elem OUT>
 static hipError_t run_forward_rows(const RowsGemm& p, const RowGrids& g, int type, hipStream_t stream, bool* served) {
     *served = false;
     const int64_t K = (int64_t)g.C * g.g, copies = (int64_t)g.s * g.g;
-    if (p.M > 24 || K > 16384 || copies > kImageTable || p.ldw >= kWidePitch || g.ldq > 65536) return hipSuccess;
-    const int segments = p.M * (int)ceil_div(ceil_div(K, type == (int)Elem::f32 ? 4 : 8), 64);
-    if (segments > 24) return hipSuccess;
-    if (segments > 12 && p.N <= 64 * compute_units() && stream != nullptr) {   // (the null stream is never captured)
+    if (p.M > 16 || copies > kImageTable || p.ldw >= kWidePitch || g.ldq > 65536) return hipSuccess;
+    const int64_t segments = p.M * ceil_div(ceil_div(K, type == (int)Elem::f32 ? 4 : 8), 64), cus = compute_units();
+    const bool one_share = p.N <= 32 * cus && p.ksteps <= 20 && segments <= 16;
+    const bool many_shares = p.N > 128 * cus && p.ksteps >= 4 && segments <= 12;
+    if (!one_share && !many_shares) return hipSuccess;
+    if (one_share && segments > 8 && stream != nullptr) {          // (the null stream is never captured)
         hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
         const hipError_t e = hipStreamIsCapturing(stream, &status);
         if (e != hipSuccess) return e;
@@ -821,14 +825,13 @@ static hipError_t run_forward_rows(const RowsGemm& p, const RowGrids& g, int typ
     const bool narrow = ceil_div(p.N, 16) <= compute_units();
 #define OCS_ROWS_IMAGE(XB)                                                                                             \
     if (p.M <= XB * 8) {                                                                                               \
-        *served = image_lds<XB, 4>(segments, p.ksteps, (int)copies).total <= kMostLds;                                 \
+        *served = image_lds<XB, 4>((int)segments, p.ksteps, (int)copies).total <= kMostLds;                             \
         if (!*served) return hipSuccess;                                                                               \
-        return narrow ? run_rows_image<XB, 2, OUT>(p, g, type, segments, stream)                                       \
-                      : run_rows_image<XB, 4, OUT>(p, g, type, segments, stream);                                      \
+        return narrow ? run_rows_image<XB, 2, OUT>(p, g, type, (int)segments, stream)                                  \
+                      : run_rows_image<XB, 4, OUT>(p, g, type, (int)segments, stream);                                 \
     }
     OCS_ROWS_IMAGE(1)
     OCS_ROWS_IMAGE(2)
-    OCS_ROWS_IMAGE(3)
 #undef OCS_ROWS_IMAGE
     return hipSuccess;
 }
