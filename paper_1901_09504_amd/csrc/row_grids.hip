@@ -8,7 +8,7 @@
 
 namespace ocs {
 
-// The largest word over the NT lanes of a row (64: the wave, 256: the workgroup).
+// The largest word over the NT lanes of a row (64: the wave, otherwise the workgroup).
 template <int NT>
 __device__ __forceinline__ unsigned row_max(unsigned v, unsigned* red) {
     v = wave_umax32(v);
@@ -34,18 +34,22 @@ __device__ __forceinline__ void row_barrier() {
 // Bytes of LDS for a row's codes: whole pieces.
 static int64_t image_bytes(int64_t K) { return round_up(K, 16); }
 
+// Lanes of a workgroup: of four rows or of one.
+template <int NT>
+constexpr int kRowLanes = NT == 64 ? 256 : NT;
+
 // NT lanes per row, U 16-byte pieces per lane: rows of up to NT * U pieces.  SCALED: 2^-chan_depth applies.
 // Codes of whole pieces go straight to memory and into the row's image in LDS; what lies behind them (a last partial
 // piece, the copies, the padding) is put together from the image, or with SCALED from the row again.
 template <Elem T, int NT, int U, bool SCALED>
-__global__ __launch_bounds__(256) void row_grid_kernel(RowGrids p) {
-    constexpr int VEC = kVec<T>;
-    __shared__ unsigned red[4];
+__global__ __launch_bounds__(kRowLanes<NT>) void row_grid_kernel(RowGrids p) {
+    constexpr int VEC = kVec<T>, ROWS = kRowLanes<NT> / NT;
+    __shared__ unsigned red[kRowLanes<NT> / 64];
     extern __shared__ __align__(16) int8_t images[];
     const int K = p.C * p.g, Ke = (p.C + p.s) * p.g;
     const int t = (int)threadIdx.x % NT;
-    const int64_t row = (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT;
-    if (row >= p.M) return;                               // NT == 64: whole waves; NT == 256: never
+    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / NT;
+    if (row >= p.M) return;                               // NT == 64: whole waves; otherwise never
     int8_t* image = images + (threadIdx.x / NT) * ((K + 15) & ~15);
     const elem_t<T>* x = static_cast<const elem_t<T>*>(p.X) + row * p.ldx;
     int8_t* q = p.Xq + row * p.ldq;
@@ -195,24 +199,32 @@ __global__ __launch_bounds__(256) void row_grid_long_kernel(RowGrids p) {
 
 template <Elem T, int NT, int U>
 static hipError_t run_row_grids(const RowGrids& p, hipStream_t stream) {
-    const int64_t groups = ceil_div(p.M, 256 / NT);
+    const int64_t groups = ceil_div(p.M, kRowLanes<NT> / NT);
     if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
-    const unsigned lds = (unsigned)(image_bytes((int64_t)p.C * p.g) * (256 / NT));
+    const unsigned lds = (unsigned)(image_bytes((int64_t)p.C * p.g) * (kRowLanes<NT> / NT));
     return launch_kernel(kTimeSplitQuantize, p.chan_depth ? row_grid_kernel<T, NT, U, true> : row_grid_kernel<T, NT, U, false>,
-                         dim3((unsigned)groups), dim3(256), lds, stream, p);
+                         dim3((unsigned)groups), dim3(kRowLanes<NT>), lds, stream, p);
 }
 
 template <Elem T>
 static hipError_t run_row_grids_of(const RowGrids& p, hipStream_t stream) {
     const int64_t K = (int64_t)p.C * p.g, pieces = ceil_div(K, kVec<T>);
     if (p.ldq <= 0x7FFFF000) {                            // (a row's 32-bit column passes its end by one round of the workgroup)
-        // a wave per row while two pieces a lane hold it, then a workgroup
+        // A wave per row while two pieces a lane hold it, then a workgroup.  While every row can have a compute unit to itself, with as
+        // many lanes as its pieces ask for: a lane's pieces are the latency (us, fp32, 256 lanes / 512 / 1024: 20 x 1500 2.8 / 2.55 / 2.56,
+        // 20 x 3000 3.0 / 2.8 / 2.6, 256 x 6000 5.4 / 4.3 / 4.1).  With more rows, several workgroups a unit hide it instead, and fewer
+        // lanes wait at a barrier (700 x 3000 4.75 / 4.7 / 5.8, 700 x 4096 6.5 / 5.8 / 7.1, 4096 x 1500 8.2 / 10.1 / 16.8, 4096 x 3000 12.5 / 13.7 /
+        // 18.1, 4096 x 6000 27.1 / 24.9 / 30.9).
+        const int64_t cus = compute_units();
         if (pieces <= 64) return run_row_grids<T, 64, 1>(p, stream);
         if (pieces <= 128) return run_row_grids<T, 64, 2>(p, stream);
         if (pieces <= 256) return run_row_grids<T, 256, 1>(p, stream);
-        if (pieces <= 512) return run_row_grids<T, 256, 2>(p, stream);
-        if (pieces <= 1024) return run_row_grids<T, 256, 4>(p, stream);
-        if (pieces <= 2048) return run_row_grids<T, 256, 8>(p, stream);
+        if (pieces <= 512) return p.M <= cus ? run_row_grids<T, 512, 1>(p, stream) : run_row_grids<T, 256, 2>(p, stream);
+        if (pieces <= 1024) {
+            if (p.M <= cus) return run_row_grids<T, 1024, 1>(p, stream);
+            return p.M <= 4 * cus ? run_row_grids<T, 512, 2>(p, stream) : run_row_grids<T, 256, 4>(p, stream);
+        }
+        if (pieces <= 2048) return p.M <= cus ? run_row_grids<T, 1024, 2>(p, stream) : run_row_grids<T, 512, 4>(p, stream);
     }
     if (p.M > 0x7FFFFFFF) return hipErrorInvalidValue;
     return launch_kernel(kTimeSplitQuantize, p.chan_depth ? row_grid_long_kernel<T, true> : row_grid_long_kernel<T, false>,

@@ -87,6 +87,26 @@ def test_codes_and_steps_are_those_of_each_row_alone(dtype, M, C, g, s, halved):
     _check_codes(x.to(dtype).cuda(), C, g, src, depth if halved else None, s, 8)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M", [256, 300, 1030])
+@pytest.mark.parametrize("C", [1030, 2051, 2500, 4102, 7003])
+def test_codes_of_many_long_rows(dtype, M, C):
+    """Lanes per row change with the count of rows; s copies and a last partial piece behind them."""
+    rng = np.random.default_rng(M + C)
+    src, depth = _lists(rng, C, 40)
+    x = torch.randn((M, C), generator=torch.Generator().manual_seed(C)).to(dtype).cuda() * torch.rand((M, 1), device="cuda").to(dtype)
+    for halved in (None, depth):
+        q, step = _codes(x, C, 1, src, halved, 40, 8)
+        for m in (0, 1, 255, M - 1):
+            want, scale = ref.quantize(_expanded(x[m:m + 1], C, 1, src, halved), 8, ldq=q.shape[1])
+            assert np.array_equal(q[m], want[0]) and step[m].view(np.uint32) == scale.view(np.uint32)[1], m
+        if halved is None:                                  # every row: the grid's definition on the device, row by row
+            v = x.float()[:, torch.from_numpy(src).long().cuda()]
+            t = v.abs().amax(1, keepdim=True)
+            code = (v * (torch.full_like(t, 127) / t)).clamp(-127, 127).round()
+            assert np.array_equal(q[:, :C + 40], G.host(code.to(torch.int8))) and not q[:, C + 40:].any()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("C", [40, 333, 1200])
 def test_codes_of_any_pitch_and_alignment(dtype, C):
