@@ -462,11 +462,14 @@ struct TokenPlan {
     int parts, part_len;
     size_t keys_off, total;
 };
-// Rows that fill the chip have a workgroup each.  Fewer ones, longer than a workgroup holds, are cut into parts that it does.
+// Rows that fill the chip have a workgroup each.  Fewer ones, longer than a workgroup holds, are cut into parts of half of what it does: the
+// exponentials of a lane's logits are what a part takes longest over (bf16, us from a graph, parts of 65536 / 32768 / 16384 / 8192: 1 x 100003
+// 11.7 / 9.8 / 9.6 / 9.7, 64 x 100003 13.8 / 11.4 / 11.9 / 14.6, 250 x 70001 22.6 / 18.0 / 16.7 / 20.4, 64 x 250001 15.4 / 15.2 / 15.7 / 20.9).
+constexpr int kPartLogits = 32768;
 static TokenPlan plan_token_rows(int64_t M, int64_t V, int k) {
     TokenPlan t{1, (int)V, 0, 0};
     if (M <= compute_units() && M <= kMostPartRows / 2 && V > kHeldLogits) {
-        int64_t parts = ceil_div(V, kHeldLogits);
+        int64_t parts = ceil_div(V, kPartLogits);
         const int64_t most = kMostPartRows / M < kMostParts ? kMostPartRows / M : kMostParts;
         parts = parts < most ? parts : most;
         t.part_len = (int)round_up(ceil_div(V, parts), 64);

@@ -464,6 +464,14 @@ def test_scores(dtype, M, V, k):
     _check_scores(x.cuda(), t, k)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,V,k", [(1, 65537, 32), (5, 70001, 1), (64, 98305, 5), (250, 66001, 8), (2, 2200000, 20), (1, 5000001, 3)])
+def test_scores_of_few_long_rows(dtype, M, V, k):
+    """Rows in parts: one logit more than a workgroup holds, as many rows as take part in it, more parts asked for than there may be."""
+    x, t = _logits(M, V, dtype, V)
+    _check_scores(x.cuda(), t, k)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("M,V", [(3, 999), (2, 40000), (700, 130)])
 def test_scores_of_any_pitch_and_alignment(dtype, M, V):
