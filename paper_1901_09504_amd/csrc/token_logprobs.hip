@@ -31,9 +31,10 @@ struct TokenRows {
     unsigned long long* keys;
 };
 
-// Logits as whole numbers that order like them: -0 with +0, NaN above everything, 0 below everything.
+// Logits as whole numbers that order like them: -0 with +0, NaN above everything, 0 below everything.  Nothing is 0xFFFFFFFF: every key
+// is below ~0, which is what a selection begins below.
 __device__ __forceinline__ unsigned order_of(float v) {
-    if (v != v) return 0xFFFFFFFFu;
+    if (v != v) return 0xFFFFFFFEu;
     const unsigned b = __float_as_uint(v + 0.0f);
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
