@@ -266,9 +266,15 @@ struct KernelTimer {
 };
 KernelTimer& kernel_timer();
 
+// HIP takes fewer than 2^32 lanes a launch in each direction.  It does not refuse more: the launch succeeds and runs the workgroups that
+// are left of the count modulo 2^32.
+constexpr int64_t kMostLanes = 0xFFFFFFFF;
+
 template <typename F, typename... Args>
 inline hipError_t launch_kernel(int family, F kernel, dim3 grid, dim3 block, unsigned lds,
                                 hipStream_t stream, Args... args) {
+    if ((int64_t)grid.x * block.x > kMostLanes || (int64_t)grid.y * block.y > kMostLanes || (int64_t)grid.z * block.z > kMostLanes)
+        return hipErrorInvalidConfiguration;
     KernelTimer& t = kernel_timer();
     if (family > 0 && family < kTimeFamilies && t.start[family] != nullptr) {
         hipEvent_t a = t.start[family], b = t.stop[family];

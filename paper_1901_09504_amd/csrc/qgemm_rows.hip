@@ -838,14 +838,39 @@ static hipError_t run_forward_rows(const RowsGemm& p, const RowGrids& g, int typ
     return hipSuccess;
 }
 
+// Outputs by the launch: as a rule all of them.  2^28 rows, 2^26 columns and 2^35 outputs are at most 2^23 + 2^22 + 2^20 + 1 tiles of 64 x 64 on 256
+// lanes, 2^22 + 2^19 + 1 of 128 x 128 on 512, or 2^21 shares of 32 outputs on 512 where there are few tokens: fewer than kMostLanes.
+template <Elem OUT>
+static hipError_t run_rows_ranges(const RowsGemm& p, hipStream_t stream) {
+    constexpr int64_t kMostRows = (int64_t)1 << 28, kMostColumns = (int64_t)1 << 26, kMostOutputs = (int64_t)1 << 35;
+    for (int64_t n0 = 0; n0 < p.N; n0 += kMostColumns) {
+        const int64_t cols = p.N - n0 < kMostColumns ? p.N - n0 : kMostColumns;
+        const int64_t most = kMostOutputs / cols < kMostRows ? kMostOutputs / cols : kMostRows;
+        for (int64_t m0 = 0; m0 < p.M; m0 += most) {
+            RowsGemm q = p;
+            q.M = (int)(p.M - m0 < most ? p.M - m0 : most);
+            q.N = (int)cols;
+            q.Xq += m0 * p.ldx;
+            q.Wq += n0 * p.ldw;
+            q.step_x += m0;
+            q.step_w += n0;
+            if (p.bias) q.bias += n0;
+            q.Y = static_cast<elem_t<OUT>*>(p.Y) + m0 * p.ldy + n0;
+            const hipError_t e = run_rows_gemm<OUT>(q, stream);
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
 hipError_t launch_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, int64_t ldw, int64_t M, int64_t N, int64_t Kexp,
                              const float* step_x, const float* step_w, const float* bias, void* Y, int out_type, int64_t ldy,
                              hipStream_t stream) {
     const RowsGemm p{Xq, ldx, Wq, ldw, (int)M, (int)N, (int)ceil_div(Kexp, 128), step_x, step_w, bias, Y, ldy, 0, 0};
     switch (static_cast<Elem>(out_type)) {
-        case Elem::f32: return run_rows_gemm<Elem::f32>(p, stream);
-        case Elem::bf16: return run_rows_gemm<Elem::bf16>(p, stream);
-        case Elem::f16: return run_rows_gemm<Elem::f16>(p, stream);
+        case Elem::f32: return run_rows_ranges<Elem::f32>(p, stream);
+        case Elem::bf16: return run_rows_ranges<Elem::bf16>(p, stream);
+        case Elem::f16: return run_rows_ranges<Elem::f16>(p, stream);
     }
     return hipErrorInvalidValue;
 }

@@ -197,13 +197,27 @@ __global__ __launch_bounds__(256) void row_grid_long_kernel(RowGrids p) {
     }
 }
 
+// One launch for every `lanes` lanes' worth of rows, `rows` rows a workgroup: as a rule all of them.
+template <Elem T, typename F>
+static hipError_t launch_by_rows(RowGrids p, int lanes, int rows, F kernel, unsigned lds, hipStream_t stream) {
+    const int64_t most = kMostLanes / lanes * rows;
+    for (int64_t left = p.M; left > 0;) {
+        p.M = left < most ? left : most;
+        const hipError_t e = launch_kernel(kTimeSplitQuantize, kernel, dim3((unsigned)ceil_div(p.M, rows)), dim3((unsigned)lanes), lds, stream, p);
+        if (e != hipSuccess) return e;
+        left -= p.M;
+        p.X = static_cast<const elem_t<T>*>(p.X) + p.M * p.ldx;
+        p.Xq += p.M * p.ldq;
+        p.step += p.M;
+    }
+    return hipSuccess;
+}
+
 template <Elem T, int NT, int U>
 static hipError_t run_row_grids(const RowGrids& p, hipStream_t stream) {
-    const int64_t groups = ceil_div(p.M, kRowLanes<NT> / NT);
-    if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
-    const unsigned lds = (unsigned)(image_bytes((int64_t)p.C * p.g) * (kRowLanes<NT> / NT));
-    return launch_kernel(kTimeSplitQuantize, p.chan_depth ? row_grid_kernel<T, NT, U, true> : row_grid_kernel<T, NT, U, false>,
-                         dim3((unsigned)groups), dim3(kRowLanes<NT>), lds, stream, p);
+    constexpr int LANES = kRowLanes<NT>, ROWS = LANES / NT;
+    const unsigned lds = (unsigned)(image_bytes((int64_t)p.C * p.g) * ROWS);
+    return launch_by_rows<T>(p, LANES, ROWS, p.chan_depth ? row_grid_kernel<T, NT, U, true> : row_grid_kernel<T, NT, U, false>, lds, stream);
 }
 
 template <Elem T>
@@ -226,9 +240,7 @@ static hipError_t run_row_grids_of(const RowGrids& p, hipStream_t stream) {
         }
         if (pieces <= 2048) return p.M <= cus ? run_row_grids<T, 1024, 2>(p, stream) : run_row_grids<T, 512, 4>(p, stream);
     }
-    if (p.M > 0x7FFFFFFF) return hipErrorInvalidValue;
-    return launch_kernel(kTimeSplitQuantize, p.chan_depth ? row_grid_long_kernel<T, true> : row_grid_long_kernel<T, false>,
-                         dim3((unsigned)p.M), dim3(256), 0, stream, p);
+    return launch_by_rows<T>(p, 256, 1, p.chan_depth ? row_grid_long_kernel<T, true> : row_grid_long_kernel<T, false>, 0, stream);
 }
 
 hipError_t launch_row_grids(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src,

@@ -482,9 +482,25 @@ static TokenPlan plan_token_rows(int64_t M, int64_t V, int k) {
 }
 size_t token_logprobs_workspace_bytes(int64_t M, int64_t V, int k) { return plan_token_rows(M, V, k).total; }
 
+// One launch for every kMostLanes lanes' worth of rows: as a rule all of them, rows in parts always (there are few).
 template <Elem T, int NT, int U, bool HELD>
-static hipError_t run_token_kernel(const TokenRows& p, int64_t groups, hipStream_t stream) {
-    return launch_kernel(0, token_rows_kernel<T, NT, U, HELD>, dim3((unsigned)groups), dim3(NT), 0, stream, p);
+static hipError_t run_token_kernel(TokenRows p, int64_t M, hipStream_t stream) {
+    const int64_t most = kMostLanes / NT / p.parts;
+    for (int64_t left = M; left > 0;) {
+        const int64_t rows = left < most ? left : most;
+        const hipError_t e = launch_kernel(0, token_rows_kernel<T, NT, U, HELD>, dim3((unsigned)(rows * p.parts)), dim3(NT), 0, stream, p);
+        if (e != hipSuccess) return e;
+        left -= rows;
+        p.logits = static_cast<const elem_t<T>*>(p.logits) + rows * p.ld;
+        if (p.tokens) p.tokens += rows;
+        if (p.logprob) p.logprob += rows;
+        if (p.entropy) p.entropy += rows;
+        if (p.k) {
+            p.top_ids += rows * p.k;
+            p.top_logprobs += rows * p.k;
+        }
+    }
+    return hipSuccess;
 }
 
 // Rows of up to 2048 pieces are held by 256 lanes.  Longer ones: while every row can have a compute unit to itself, by 1024 (1 x 33001
@@ -493,16 +509,15 @@ static hipError_t run_token_kernel(const TokenRows& p, int64_t groups, hipStream
 // x 33001 fp32 73 / 70; 4096 x 100003 bf16 160 / 155).
 template <Elem T>
 static hipError_t run_token_rows(const TokenRows& p, int64_t M, hipStream_t stream) {
-    const int64_t groups = M * p.parts, pieces = p.part_len / kVec<T>;
-    if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
+    const int64_t pieces = p.part_len / kVec<T>;
     hipError_t e;
-    if (pieces <= 256 * 2) e = run_token_kernel<T, 256, 2, true>(p, groups, stream);
-    else if (pieces <= 256 * 8) e = run_token_kernel<T, 256, 8, true>(p, groups, stream);
-    else if (M > 4 * compute_units()) e = run_token_kernel<T, 512, 4, false>(p, groups, stream);
-    else if (M > compute_units() || p.part_len > kHeldLogits) e = run_token_kernel<T, 256, 4, false>(p, groups, stream);
-    else if (pieces <= 1024 * 4) e = run_token_kernel<T, 1024, 4, true>(p, groups, stream);
-    else if (T == Elem::f32 && pieces > 1024 * 9) e = run_token_kernel<T, 1024, T == Elem::f32 ? 16 : 8, true>(p, groups, stream);
-    else e = run_token_kernel<T, 1024, T == Elem::f32 ? 9 : 8, true>(p, groups, stream);
+    if (pieces <= 256 * 2) e = run_token_kernel<T, 256, 2, true>(p, M, stream);
+    else if (pieces <= 256 * 8) e = run_token_kernel<T, 256, 8, true>(p, M, stream);
+    else if (M > 4 * compute_units()) e = run_token_kernel<T, 512, 4, false>(p, M, stream);
+    else if (M > compute_units() || p.part_len > kHeldLogits) e = run_token_kernel<T, 256, 4, false>(p, M, stream);
+    else if (pieces <= 1024 * 4) e = run_token_kernel<T, 1024, 4, true>(p, M, stream);
+    else if (T == Elem::f32 && pieces > 1024 * 9) e = run_token_kernel<T, 1024, T == Elem::f32 ? 16 : 8, true>(p, M, stream);
+    else e = run_token_kernel<T, 1024, T == Elem::f32 ? 9 : 8, true>(p, M, stream);
     if (e != hipSuccess || p.parts == 1) return e;
     return launch_kernel(0, token_join_kernel<T>, dim3((unsigned)M), dim3(64), 0, stream, p);
 }

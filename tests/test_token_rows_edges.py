@@ -49,3 +49,69 @@ def test_nan_at_any_token_comes_first(dtype, V, k):
         assert np.array_equal(ids[m], order), (m, ids[m], order)
     assert ids.min() >= 0 and ids.max() < V
     assert np.isnan(G.host(top)).all() and np.isnan(G.host(lp)).all() and np.isnan(G.host(ent)).all()
+
+
+# ---- more rows and outputs than a launch takes ---------------------------------------------------
+# A launch has fewer than 2^32 lanes.  Every output is one row's (or one row's and one column's), so calls on ranges give the same bits.
+
+def _same_in_ranges(whole, part, n, step):
+    """whole: tensors of n rows (or columns) from one call; part(a, b): those of rows a .. b-1 alone."""
+    for a in range(0, n, step):
+        b = min(a + step, n)
+        for got, want in zip(whole, part(a, b)):
+            assert torch.equal(got[a:b], want), (a, b)
+
+
+@pytest.mark.parametrize("M", [(1 << 24) - 1, 1 << 24, (1 << 25) + 7])
+def test_scores_of_more_rows_than_a_launch_takes(M):
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.randint(-40, 41, (M, 2), dtype=torch.int8, device="cuda", generator=gen).to(BF16)
+    t = torch.randint(-1, 3, (M,), dtype=torch.int32, device="cuda", generator=gen)
+
+    def score(a, b):
+        n = b - a
+        out = [torch.full((n,), -7.0, device="cuda"), torch.full((n,), -7.0, device="cuda"),
+               torch.full((n, 1), -7, dtype=torch.int32, device="cuda"), torch.full((n, 1), -7.0, device="cuda")]
+        lp, ent, ids, top = out
+        B.ocs_token_logprobs(x[a:b], n, 2, 2, t[a:b], 1, lp, ent, ids, top)
+        return out
+
+    whole = score(0, M)
+    assert bool((whole[2][:, 0] == (x[:, 1] > x[:, 0])).all()) and bool((whole[1] >= 0).all())
+    _same_in_ranges(whole, score, M, 1 << 22)
+    only = torch.full((M,), -7.0, device="cuda")           # one output, and no token
+    B.ocs_token_logprobs(x, M, 2, 2, None, 0, None, only, None, None)
+    assert torch.equal(only, whole[1])
+
+
+@pytest.mark.parametrize("dtype,M", [(F32, 1 << 26), (BF16, (1 << 26) + 5)])
+def test_codes_of_more_rows_than_a_launch_takes(dtype, M):
+    x = torch.randint(-9, 10, (M, 2), dtype=torch.int8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(M)).to(dtype)
+
+    def codes(a, b):
+        q, step = torch.full((b - a, 16), 77, dtype=torch.int8, device="cuda"), torch.full((b - a,), -7.0, device="cuda")
+        B.ocs_split_quantize_rows(x[a:b], b - a, 2, 1, 2, None, None, 0, 8, 1.0, q, 16, step)
+        return q, step
+
+    whole = codes(0, M)
+    assert bool((whole[1] == x.float().abs().amax(1) / torch.full((1,), 127.0, device="cuda")).all())
+    _same_in_ranges(whole, codes, M, 1 << 24)
+
+
+@pytest.mark.parametrize("M,N", [(1, (1 << 28) + 5), ((1 << 28) + 5, 1)])
+def test_product_of_more_outputs_than_a_launch_takes(M, N):
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randint(-127, 128, (M, 16), dtype=torch.int8, device="cuda", generator=gen)
+    w = torch.randint(-127, 128, (N, 16), dtype=torch.int8, device="cuda", generator=gen)
+    sx, sw, bias = (torch.rand(n, device="cuda", generator=gen) for n in (M, N, N))
+    many = max(M, N)
+
+    def product(a, b):
+        m, n = (slice(a, b), slice(0, 1)) if M > N else (slice(0, 1), slice(a, b))
+        y = torch.full((b - a,), float("nan"), dtype=BF16, device="cuda")   # (no product of finite factors)
+        B.ocs_qgemm_rows(x[m], 16, w[n], 16, x[m].shape[0], w[n].shape[0], 16, 8, 8, sx[m], sw[n], bias[n], y, w[n].shape[0])
+        return (y,)
+
+    whole = product(0, many)
+    assert not bool(whole[0].isnan().any())
+    _same_in_ranges(whole, product, many, 1 << 25)
