@@ -517,7 +517,8 @@ int ocs_fold_weights(const int8_t *Wq, int64_t ldq, int64_t N, int C, int g, int
  *   Codes: pitches as for ocs_qgemm.  Y: any ldy >= N, base aligned to its element.
  *
  * ocs_forward_rows: the two as one call (weight OCS, Eq. 3: activations' copies un-scaled), Xq and step_x_out left
- *   as ocs_split_quantize_rows leaves them, Y as ocs_qgemm_rows does, bit for bit; `type` is X's and Y's is `out_type`.
+ *   as ocs_split_quantize_rows leaves them, Y as ocs_qgemm_rows does, bit for bit; `type` is X's and Y's is `out_type`.  Few tokens
+ *   run as one launch, but where Y, Xq or step_x_out share memory with X, chan_src, Wq, step_w or bias.
  */
 int ocs_split_quantize_rows(const void *X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t *chan_src,
                             const int32_t *chan_depth, int num_splits, int bits, float clip_ratio, int8_t *Xq,

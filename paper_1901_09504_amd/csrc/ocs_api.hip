@@ -1012,8 +1012,17 @@ int ocs_forward_rows(const void* X, int type, int64_t M, int C, int g, int64_t l
     rc = check_gemm_operands(Xq, ldq, Wq, ldw, M == 0 ? 1 : M, N, Kexp, bits_x, bits_w, nullptr, 0);
     if (rc) return rc;
     if (M == 0) return OCS_OK;
+    // As in ocs_forward: an output that shares memory with what is read (a layer applied in place, rows of X against each other) keeps
+    // the two launches, the first of which has read or written it all before the second begins.
+    const int64_t K = (int64_t)C * g, xb = (int64_t)type_bytes(type) * ((M - 1) * ldx + K),
+                  yb = (int64_t)type_bytes(out_type) * ((M - 1) * ldy + N);
+    auto clear_of_outputs = [&](const void* in, int64_t bytes) {
+        return !overlap(in, bytes, Y, yb) && !overlap(in, bytes, Xq, M * ldq) && !overlap(in, bytes, step_x_out, 4 * M);
+    };
+    const bool apart = clear_of_outputs(X, xb) && clear_of_outputs(num_splits > 0 ? chan_src : nullptr, 4 * (int64_t)(C + num_splits)) &&
+                       clear_of_outputs(Wq, N * ldw) && clear_of_outputs(step_w, 4 * N) && clear_of_outputs(bias, 4 * N);
     hipError_t e = launch_forward_rows(X, type, ldx, M, C, g, num_splits, chan_src, clip_ratio, qmax_of(bits_x), Xq, ldq, step_x_out,
-                                       Wq, ldw, N, step_w, bias, Y, out_type, ldy, static_cast<hipStream_t>(stream));
+                                       Wq, ldw, N, step_w, bias, Y, out_type, ldy, apart, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? OCS_OK : hip_fail(e);
 }
 

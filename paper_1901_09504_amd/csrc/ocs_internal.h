@@ -237,7 +237,7 @@ hipError_t launch_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, in
 hipError_t launch_forward_rows(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src,
                                float clip, float qmax, int8_t* Xq, int64_t ldq, float* step_x, const int8_t* Wq, int64_t ldw,
                                int64_t N, const float* step_w, const float* bias, void* Y, int out_type, int64_t ldy,
-                               hipStream_t stream);
+                               bool apart, hipStream_t stream);
 size_t token_logprobs_workspace_bytes(int64_t M, int64_t V, int k);
 hipError_t launch_token_logprobs(const void* logits, int type, int64_t M, int64_t V, int64_t ld, const int32_t* tokens, int k,
                                  float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,

@@ -878,19 +878,21 @@ hipError_t launch_qgemm_rows(const int8_t* Xq, int64_t ldx, const int8_t* Wq, in
 hipError_t launch_forward_rows(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src,
                                float clip, float qmax, int8_t* Xq, int64_t ldq, float* step_x, const int8_t* Wq, int64_t ldw,
                                int64_t N, const float* step_w, const float* bias, void* Y, int out_type, int64_t ldy,
-                               hipStream_t stream) {
+                               bool apart, hipStream_t stream) {
     const int64_t Kexp = (int64_t)(C + s) * g;
     const RowsGemm p{Xq, ldq, Wq, ldw, (int)M, (int)N, (int)ceil_div(Kexp, 128), step_x, step_w, bias, Y, ldy, 0, 0};
     const RowGrids rows{X, ldx, M, C, g, s, chan_src, nullptr, clip, qmax, Xq, ldq, step_x};
-    bool served = false;
-    hipError_t e = hipErrorInvalidValue;
-    switch (static_cast<Elem>(out_type)) {
-        case Elem::f32: e = run_forward_rows<Elem::f32>(p, rows, type, stream, &served); break;
-        case Elem::bf16: e = run_forward_rows<Elem::bf16>(p, rows, type, stream, &served); break;
-        case Elem::f16: e = run_forward_rows<Elem::f16>(p, rows, type, stream, &served); break;
+    if (apart) {                                                   // (one launch reads X and W while outputs are being written)
+        bool served = false;
+        hipError_t e = hipErrorInvalidValue;
+        switch (static_cast<Elem>(out_type)) {
+            case Elem::f32: e = run_forward_rows<Elem::f32>(p, rows, type, stream, &served); break;
+            case Elem::bf16: e = run_forward_rows<Elem::bf16>(p, rows, type, stream, &served); break;
+            case Elem::f16: e = run_forward_rows<Elem::f16>(p, rows, type, stream, &served); break;
+        }
+        if (e != hipSuccess || served) return e;
     }
-    if (e != hipSuccess || served) return e;
-    e = launch_row_grids(X, type, ldx, M, C, g, s, chan_src, nullptr, clip, qmax, Xq, ldq, step_x, stream);
+    const hipError_t e = launch_row_grids(X, type, ldx, M, C, g, s, chan_src, nullptr, clip, qmax, Xq, ldq, step_x, stream);
     if (e != hipSuccess) return e;
     return launch_qgemm_rows(Xq, ldq, Wq, ldw, M, N, Kexp, step_x, step_w, bias, Y, out_type, ldy, stream);
 }

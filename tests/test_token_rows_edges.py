@@ -115,3 +115,48 @@ def test_product_of_more_outputs_than_a_launch_takes(M, N):
     whole = product(0, many)
     assert not bool(whole[0].isnan().any())
     _same_in_ranges(whole, product, many, 1 << 25)
+
+
+# ---- operands that share memory ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("M", [1, 5, 8, 16])
+@pytest.mark.parametrize("C,N", [(64, 64), (500, 500), (1000, 40), (256, 4000)])
+def test_layer_whose_outputs_take_the_place_of_its_inputs(dtype, M, C, N):
+    """Y over X: the call is its two steps, the first of which has read all of X before the second writes."""
+    gen = torch.Generator(device="cuda").manual_seed(M + C)
+    ld, pitch = max(C, N), B.ocs_padded_cols(C)
+    x = torch.randn((M, ld), device="cuda", generator=gen).to(dtype)
+    w = torch.zeros((N, pitch), dtype=torch.int8, device="cuda")
+    w[:, :C] = torch.randint(-127, 128, (N, C), device="cuda", generator=gen)
+    sw = torch.rand(N, device="cuda", generator=gen)
+    want = []
+    for one in (False, True):
+        a = x.clone()
+        q, step = torch.empty((M, pitch), dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+        if one:
+            B.ocs_forward_rows(a, M, C, 1, ld, None, 0, 8, 1.0, q, pitch, step, w, pitch, N, 8, sw, None, a, ld)
+        else:
+            B.ocs_split_quantize_rows(a, M, C, 1, ld, None, None, 0, 8, 1.0, q, pitch, step)
+            B.ocs_qgemm_rows(q, pitch, w, pitch, M, N, C, 8, 8, step, sw, None, a, ld)
+        want.append((a, q, step))
+    assert all(torch.equal(a, b) for a, b in zip(*want))
+
+
+@pytest.mark.parametrize("M,C", [(1, 64), (8, 300), (16, 300), (16, 1000)])
+def test_rows_against_each_other(M, C):
+    """The weights are the codes that the call itself writes, with the steps that it writes."""
+    x = torch.randn((M, C), device="cuda", generator=torch.Generator(device="cuda").manual_seed(C))
+    pitch = B.ocs_padded_cols(C)
+    want = []
+    for one in (False, True):
+        q, step = torch.full((M, pitch), 77, dtype=torch.int8, device="cuda"), torch.full((M,), 7.0, device="cuda")
+        y = torch.full((M, M), 7.0, device="cuda")
+        if one:
+            B.ocs_forward_rows(x, M, C, 1, C, None, 0, 8, 1.0, q, pitch, step, q, pitch, M, 8, step, None, y, M)
+        else:
+            B.ocs_split_quantize_rows(x, M, C, 1, C, None, None, 0, 8, 1.0, q, pitch, step)
+            B.ocs_qgemm_rows(q, pitch, q, pitch, M, M, C, 8, 8, step, step, None, y, M)
+        want.append((y, q, step))
+    assert all(torch.equal(a, b) for a, b in zip(*want))
+    assert torch.equal(want[0][0], want[0][0].t())
