@@ -532,7 +532,8 @@ int ocs_forward_rows(const void *X, int type, int64_t M, int C, int g, int64_t l
                      int64_t ldy, void *stream);
 
 /*
- * Scoring of tokens: what a language model is judged by (perplexity is exp of the mean of -logprob).
+ * Scoring of tokens: what a language model is judged by (perplexity is exp of the mean of -logprob over the positions that have a
+ * token: the others' logprob is 0 and no part of that mean).
  *   logits [M, V] of element type `type`, any ld >= V, base aligned to its element; p = softmax of a row in fp32.
  *   tokens [M] int32 (may be NULL): logprob[m] = log p[tokens[m]]; a token outside 0 .. V-1 marks a position
  *        without one (padding) and gets logprob 0.

@@ -26,9 +26,10 @@ def synthetic(tokens, hidden, vocab, seed=190109504, device="cuda"):
 
 
 def perplexity(logits, tokens):
-    """(exp of the mean of -log p, the most likely token of every position)"""
+    """(exp of the mean of -log p over the positions that have a token, NaN where none has; the most likely token of every position)"""
     out = token_logprobs(logits, tokens, 1)
-    return float(torch.exp(-out["logprob"].mean())), out["top_ids"][:, 0]
+    has = (tokens >= 0) & (tokens < logits.shape[1])
+    return float(torch.exp(-out["logprob"][has].mean())), out["top_ids"][:, 0]
 
 
 def run(tokens=700, hidden=1500, vocab=10000, widths=(8, 6, 5, 4), ratios=(0.0, 0.05), seed=190109504):

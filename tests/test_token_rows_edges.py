@@ -160,3 +160,21 @@ def test_rows_against_each_other(M, C):
         want.append((y, q, step))
     assert all(torch.equal(a, b) for a, b in zip(*want))
     assert torch.equal(want[0][0], want[0][0].t())
+
+
+# ---- perplexity of padded batches ----------------------------------------------------------------
+
+def test_padding_is_no_part_of_a_perplexity():
+    from paper_1901_09504_amd import score
+
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    x = torch.randn((40, 100), device="cuda", generator=gen)
+    t = torch.randint(100, (40,), dtype=torch.int32, device="cuda", generator=gen)
+    alone, best = score.perplexity(x, t)
+    want = float(torch.exp(-torch.log_softmax(x.double(), 1).gather(1, t.long()[:, None]).mean()))
+    assert abs(alone / want - 1) < 1e-5
+    pad = torch.tensor([-1, 100, 1 << 30, -(1 << 31)] * 20, dtype=torch.int32, device="cuda")
+    padded, top = score.perplexity(torch.cat([x, x, x]), torch.cat([t, pad]))
+    assert padded == alone and torch.equal(top[:40], best) and torch.equal(top[40:80], best)
+    assert np.isnan(score.perplexity(x, pad[:40])[0])
+    assert np.isnan(score.perplexity(x[:0], t[:0])[0])
