@@ -303,7 +303,10 @@ class ConvChain:
 
 class TokenLayer:
     """The layer of Eq. 3 with a grid of its own for every token (row of X) and every output channel (row of W), where
-    ExpandedLayer has one per tensor: an outlier token costs only itself precision.  X and Y in fp32, bf16 or fp16."""
+    ExpandedLayer has one per tensor: an outlier token costs only itself precision.  X and Y in fp32, bf16 or fp16.
+
+    A call runs on `stream`, or on the current one.  Whatever streams a layer is used on, its buffers are not handed out again before
+    their work is done; that one stream's call comes before another's (they share the buffers) is the caller's to see to."""
 
     def __init__(self, N, C, r, g=1, bits_w=8, bits_x=8, clip_ratio_w=1.0, clip_ratio_x=1.0, out_dtype=torch.float32,
                  max_rows=None, device="cuda"):
@@ -323,6 +326,9 @@ class TokenLayer:
         self.Wq = torch.empty((self.N, self.ldq), dtype=torch.int8, device=device)
         self.step_w = torch.empty(self.N, dtype=torch.float32, device=device)
         self.bias = None
+        self._weights_from = torch.cuda.current_stream()    # the streams whose memory the buffers are
+        self._rows_from = self._weights_from
+        self._streams = set()                               # those that they may be used on
         self._rows = 0
         self.Xq = self.step_x = self.Y = None
         if max_rows:
@@ -334,41 +340,69 @@ class TokenLayer:
             self.step_x = torch.empty(M, dtype=torch.float32, device=self.device)
             self.Y = torch.empty((M, self.N), dtype=self.out_dtype, device=self.device)
             self._rows = M
+            self._rows_from = torch.cuda.current_stream()
+            self._streams.clear()
+
+    def _use_on_current_stream(self):
+        """Before work on the current stream: the buffers may be memory that another stream's earlier work is not done with, and may be
+        dropped on the host before this stream's work is done.  Once per stream and set of buffers."""
+        raw = B._stream(None)
+        if raw in self._streams:
+            return
+        stream = torch.cuda.current_stream()
+        if not torch.cuda.is_current_stream_capturing():    # (a capture begins with the device idle)
+            for other in {self._weights_from, self._rows_from} - {stream}:
+                stream.wait_stream(other)
+        for t in (self.split_src, self.chan_src, self.chan_depth, self.Wq, self.step_w, self.bias, self.Xq, self.step_x, self.Y):
+            if t is not None:
+                t.record_stream(stream)
+        self._streams.add(raw)
 
     def prepare_weights(self, W, bias=None, stream=None):
         """W fp32 [N, C*g] on the device -> split lists, Wq, step_w.  The channels are chosen on the whole tensor (Sec. 3.4) and
         halved (Eq. 3), then every row gets its grid.  bias: fp32 [N] or None, kept by reference."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.prepare_weights(W, bias)
         assert W.dtype == torch.float32 and W.shape == (self.N, self.K) and W.stride(1) == 1
         assert bias is None or (bias.dtype == torch.float32 and bias.shape == (self.N,) and bias.is_contiguous())
         self.bias = bias
+        self._streams.clear()
+        self._use_on_current_stream()
         ws = B.alloc_workspace(self.N, self.K, self.device)
-        B.ocs_select_channels(W, self.N, self.C, self.g, W.stride(0), self.s, self.split_src, self.chan_src, self.chan_depth, None,
-                              ws, stream)
+        B.ocs_select_channels(W, self.N, self.C, self.g, W.stride(0), self.s, self.split_src, self.chan_src, self.chan_depth, None, ws)
         B.ocs_split_quantize_rows(W, self.N, self.C, self.g, W.stride(0), self.chan_src, self.chan_depth, self.s, self.bits_w,
-                                  self.clip_ratio_w, self.Wq, self.ldq, self.step_w, stream)
-        if stream is not None:
-            ws.record_stream(stream)
+                                  self.clip_ratio_w, self.Wq, self.ldq, self.step_w)
 
     def forward(self, X, stream=None):
         """X [M, C*g] in fp32, bf16 or fp16 -> Y [M, N] in out_dtype (M = 0 included), the layer's own buffer: the next call
         writes to it again."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                Y = self.forward(X)
+            Y.record_stream(torch.cuda.current_stream())    # the caller reads it on its own
+            return Y
         assert X.dim() == 2 and X.shape[1] == self.K and (X.stride(1) == 1 or X.shape[0] == 0)
         M = X.shape[0]
         if M == 0:
             return torch.empty((0, self.N), dtype=self.out_dtype, device=self.device)
         self._ensure_rows(M)
+        self._use_on_current_stream()
         B.ocs_forward_rows(X, M, self.C, self.g, X.stride(0) if M > 1 else self.K, self.chan_src, self.s, self.bits_x,
                            self.clip_ratio_x, self.Xq, self.ldq, self.step_x, self.Wq, self.ldq, self.N, self.bits_w, self.step_w,
-                           self.bias, self.Y, self.N, stream)
-        if stream is not None:                              # a larger batch may replace them while that stream still works
-            for t in (self.Xq, self.step_x, self.Y):
-                t.record_stream(stream)
+                           self.bias, self.Y, self.N)
         return self.Y[:M]
 
 
 def token_logprobs(logits, tokens=None, top_k=0, stream=None):
     """logits [M, V] in fp32, bf16 or fp16; tokens int32 [M] or None (a token outside 0 .. V-1: a position without one).
     -> dict(entropy [M], logprob [M] with tokens, top_ids int32 / top_logprobs [M, top_k] with top_k > 0), all fp32 but the ids."""
+    if stream is not None:                                  # results and workspace are that stream's memory, which the caller reads on its own
+        with torch.cuda.stream(stream):
+            out = token_logprobs(logits, tokens, top_k)
+        for t in out.values():
+            t.record_stream(torch.cuda.current_stream())
+        return out
     assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[0] == 0 or logits.shape[1] == 1)
     M, V = logits.shape
     assert tokens is None or (tokens.dtype == torch.int32 and tokens.shape == (M,) and tokens.is_contiguous())
@@ -382,9 +416,5 @@ def token_logprobs(logits, tokens=None, top_k=0, stream=None):
     need = B.ocs_token_logprobs_workspace_bytes(M, V, top_k)
     ws = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
     B.ocs_token_logprobs(logits, M, V, logits.stride(0) if M > 1 else V, tokens, top_k, out.get("logprob"), out["entropy"],
-                         out.get("top_ids"), out.get("top_logprobs"), ws, stream)
-    if stream is not None:
-        for t in (*out.values(), ws):
-            if t is not None:
-                t.record_stream(stream)
+                         out.get("top_ids"), out.get("top_logprobs"), ws)
     return out

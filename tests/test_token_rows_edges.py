@@ -178,3 +178,112 @@ def test_padding_is_no_part_of_a_perplexity():
     assert padded == alone and torch.equal(top[:40], best) and torch.equal(top[40:80], best)
     assert np.isnan(score.perplexity(x, pad[:40])[0])
     assert np.isnan(score.perplexity(x[:0], t[:0])[0])
+
+
+# ---- buffers and streams -------------------------------------------------------------------------
+# Memory that a stream has freed on the host is handed out again on that stream at once, while its kernels are still queued: what is
+# used on another stream is that one's own memory, or waits, and is not handed out before its work is done.
+
+def _behind_long_work(*sizes):
+    """Tensors of these sizes in bytes that the current stream overwrites with sevens, behind some 20 ms of other work, and then frees."""
+    a = torch.randn((4096, 4096), device="cuda")
+    out = torch.empty_like(a)
+    doomed = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        torch.mm(a, a, out=out)
+    for d in doomed:
+        d.fill_(7)
+
+
+def _head(N=600, C=300, max_rows=None, seed=3):
+    from paper_1901_09504_amd.layer import TokenLayer
+
+    return TokenLayer(N, C, 0.05, max_rows=max_rows), torch.randn((N, C), device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+def _rows(M, C=300):
+    return torch.randn((M, C), device="cuda", generator=torch.Generator(device="cuda").manual_seed(M))
+
+
+@pytest.mark.parametrize("M,V", [(64, 500), (4, 70001)])
+def test_scores_on_another_stream_while_the_current_one_is_busy(M, V):
+    from paper_1901_09504_amd.layer import token_logprobs
+
+    x = _rows(M, V)
+    t = torch.zeros(M, dtype=torch.int32, device="cuda")
+    want = {n: v.clone() for n, v in token_logprobs(x, t, 5).items()}
+    side = torch.cuda.Stream()
+    _behind_long_work(4 * M, 20 * M, B.ocs_token_logprobs_workspace_bytes(M, V, 5))
+    got = token_logprobs(x, t, 5, side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("grows", [False, True])
+@pytest.mark.parametrize("explicit", [False, True])
+def test_layer_on_another_stream_while_the_current_one_is_busy(grows, explicit):
+    """The buffers of a layer made, or outgrown, while what the current stream freed is still being written."""
+    M, x = 40, _rows(40)
+    head, W = _head(max_rows=M)
+    head.prepare_weights(W)
+    want = head.forward(x).clone()
+    side = torch.cuda.Stream()
+    sizes = [t.nbytes for t in (head.Xq, head.step_x, head.Y)]
+    if grows:
+        head, _ = _head(max_rows=8)
+        head.prepare_weights(W)
+    _behind_long_work(*sizes)
+    if not grows:
+        other, _ = _head(max_rows=M)                        # takes the memory that was freed
+        for n in ("chan_src", "chan_depth", "Wq", "step_w"):
+            setattr(other, n, getattr(head, n))
+        head = other
+    if explicit:
+        y = head.forward(x, side)
+    else:
+        with torch.cuda.stream(side):
+            y = head.forward(x)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_weights_prepared_on_another_stream_while_the_current_one_is_busy():
+    bias = torch.randn(600, device="cuda")
+    first, W = _head()
+    first.prepare_weights(W, bias)
+    want = first.forward(_rows(9)).clone()
+    side = torch.cuda.Stream()
+    _behind_long_work(first.Wq.nbytes, first.step_w.nbytes, first.chan_src.nbytes, B.alloc_workspace(600, 300).nbytes)
+    head, _ = _head(seed=3)
+    head.prepare_weights(W, bias, side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(head.Wq, first.Wq) and torch.equal(head.step_w, first.step_w) and torch.equal(head.chan_src, first.chan_src)
+    assert torch.equal(head.forward(_rows(9)), want)
+
+
+@pytest.mark.parametrize("drop", [False, True])
+def test_buffers_are_not_handed_out_while_a_stream_that_is_current_works(drop):
+    """A layer used within torch.cuda.stream(), then outgrown or dropped from outside: what is allocated meanwhile lands elsewhere."""
+    head, W = _head(6000, 1000, max_rows=256)
+    W = torch.randn((6000, 1000), device="cuda")
+    bias = torch.randn(6000, device="cuda")
+    head.prepare_weights(W, bias)
+    small, large = _rows(256, 1000), _rows(300, 1000)
+    want = head.forward(small).clone()
+    a, out = torch.randn((4096, 4096), device="cuda"), torch.empty((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            torch.mm(a, a, out=out)
+        kept = head.forward(small).clone()
+    sizes = [(t.shape, t.dtype) for t in (head.Xq, head.step_x, head.Y, head.Wq, head.step_w, head.chan_src, head.chan_depth, bias)]
+    if drop:
+        del head, bias
+    else:
+        head.forward(large)
+    filler = [torch.full(shape, 7, dtype=dtype, device="cuda") for shape, dtype in sizes for _ in range(2)]
+    torch.cuda.synchronize()
+    assert torch.equal(kept, want) and all(bool((f == 7).all()) for f in filler)
