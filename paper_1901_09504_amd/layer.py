@@ -306,7 +306,9 @@ class TokenLayer:
     ExpandedLayer has one per tensor: an outlier token costs only itself precision.  X and Y in fp32, bf16 or fp16.
 
     A call runs on `stream`, or on the current one.  Whatever streams a layer is used on, its buffers are not handed out again before
-    their work is done; that one stream's call comes before another's (they share the buffers) is the caller's to see to."""
+    their work is done; that one stream's call comes before another's (they share the buffers) is the caller's to see to.
+    A call captured into a graph keeps the buffers and the bias that it was captured with for as long as the layer lives: the graph
+    goes on writing to them when a larger batch has outgrown them.  The layer has to outlive the graph."""
 
     def __init__(self, N, C, r, g=1, bits_w=8, bits_x=8, clip_ratio_w=1.0, clip_ratio_x=1.0, out_dtype=torch.float32,
                  max_rows=None, device="cuda"):
@@ -329,6 +331,7 @@ class TokenLayer:
         self._weights_from = torch.cuda.current_stream()    # the streams whose memory the buffers are
         self._rows_from = self._weights_from
         self._streams = set()                               # those that they may be used on
+        self._in_graphs = []                                # what captured calls read and write
         self._rows = 0
         self.Xq = self.step_x = self.Y = None
         if max_rows:
@@ -388,6 +391,8 @@ class TokenLayer:
             return torch.empty((0, self.N), dtype=self.out_dtype, device=self.device)
         self._ensure_rows(M)
         self._use_on_current_stream()
+        if torch.cuda.is_current_stream_capturing() and not any(held[2] is self.Y and held[3] is self.bias for held in self._in_graphs):
+            self._in_graphs.append((self.Xq, self.step_x, self.Y, self.bias))
         B.ocs_forward_rows(X, M, self.C, self.g, X.stride(0) if M > 1 else self.K, self.chan_src, self.s, self.bits_x,
                            self.clip_ratio_x, self.Xq, self.ldq, self.step_x, self.Wq, self.ldq, self.N, self.bits_w, self.step_w,
                            self.bias, self.Y, self.N)

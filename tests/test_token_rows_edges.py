@@ -287,3 +287,31 @@ def test_buffers_are_not_handed_out_while_a_stream_that_is_current_works(drop):
     filler = [torch.full(shape, 7, dtype=dtype, device="cuda") for shape, dtype in sizes for _ in range(2)]
     torch.cuda.synchronize()
     assert torch.equal(kept, want) and all(bool((f == 7).all()) for f in filler)
+
+
+def test_a_graph_keeps_its_buffers_when_the_layer_grows():
+    """A captured step of generation, then a longer prompt and another bias: replays write to nobody else's memory."""
+    bias = [torch.randn(600, device="cuda") for _ in range(2)]
+    head, W = _head()
+    head.prepare_weights(W, bias[0])
+    x = _rows(20)
+    want = head.forward(x).clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = head.forward(x)
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):          # the same buffers once more: held once
+        head.forward(x[:3])
+    assert len(head._in_graphs) == 1
+    sizes = [(t.shape, t.dtype) for t in (head.Xq, head.step_x, head.Y, bias[0])]
+    where = y.data_ptr()
+    del y
+    bias.pop(0)
+    head.prepare_weights(W, bias[0])
+    large = head.forward(_rows(300)).clone()
+    filler = [torch.full(shape, 7, dtype=dtype, device="cuda") for shape, dtype in sizes for _ in range(3)]
+    assert where not in [f.data_ptr() for f in filler]
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(head._in_graphs[0][2][:20], want) and all(bool((f == 7).all()) for f in filler)
+        assert torch.equal(head.forward(_rows(300)), large)
