@@ -349,9 +349,6 @@ class TokenLayer:
     def _use_on_current_stream(self):
         """Before work on the current stream: the buffers may be memory that another stream's earlier work is not done with, and may be
         dropped on the host before this stream's work is done.  Once per stream and set of buffers."""
-        raw = B._stream(None)
-        if raw in self._streams:
-            return
         stream = torch.cuda.current_stream()
         if not torch.cuda.is_current_stream_capturing():    # (a capture begins with the device idle)
             for other in {self._weights_from, self._rows_from} - {stream}:
@@ -359,7 +356,11 @@ class TokenLayer:
         for t in (self.split_src, self.chan_src, self.chan_depth, self.Wq, self.step_w, self.bias, self.Xq, self.step_x, self.Y):
             if t is not None:
                 t.record_stream(stream)
-        self._streams.add(raw)
+        self._streams.add(stream.cuda_stream)
+
+    def _hold_for_graph(self):
+        if not any(held[2] is self.Y and held[3] is self.bias for held in self._in_graphs):
+            self._in_graphs.append((self.Xq, self.step_x, self.Y, self.bias))
 
     def prepare_weights(self, W, bias=None, stream=None):
         """W fp32 [N, C*g] on the device -> split lists, Wq, step_w.  The channels are chosen on the whole tensor (Sec. 3.4) and
@@ -390,9 +391,11 @@ class TokenLayer:
         if M == 0:
             return torch.empty((0, self.N), dtype=self.out_dtype, device=self.device)
         self._ensure_rows(M)
-        self._use_on_current_stream()
-        if torch.cuda.is_current_stream_capturing() and not any(held[2] is self.Y and held[3] is self.bias for held in self._in_graphs):
-            self._in_graphs.append((self.Xq, self.step_x, self.Y, self.bias))
+        raw = torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if raw not in self._streams:
+            self._use_on_current_stream()
+        if raw and torch._C._cuda_isCurrentStreamCapturing():   # (the null stream is never captured)
+            self._hold_for_graph()
         B.ocs_forward_rows(X, M, self.C, self.g, X.stride(0) if M > 1 else self.K, self.chan_src, self.s, self.bits_x,
                            self.clip_ratio_x, self.Xq, self.ldq, self.step_x, self.Wq, self.ldq, self.N, self.bits_w, self.step_w,
                            self.bias, self.Y, self.N)
@@ -405,8 +408,9 @@ def token_logprobs(logits, tokens=None, top_k=0, stream=None):
     if stream is not None:                                  # results and workspace are that stream's memory, which the caller reads on its own
         with torch.cuda.stream(stream):
             out = token_logprobs(logits, tokens, top_k)
+        caller = torch.cuda.current_stream()
         for t in out.values():
-            t.record_stream(torch.cuda.current_stream())
+            t.record_stream(caller)
         return out
     assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[0] == 0 or logits.shape[1] == 1)
     M, V = logits.shape
