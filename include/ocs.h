@@ -80,7 +80,7 @@ extern "C" {
 
 #define OCS_MAX_TOP 32 /* most alternatives per row of ocs_token_logprobs                       */
 
-#define OCS_MAX_EXPANDED_CHANNELS 8000  /* C + num_splits may not exceed this                */
+#define OCS_MAX_EXPANDED_CHANNELS 8000  /* C + num_splits may not exceed this (the _rows calls: where num_splits > 0) */
 
 /* Text for an OCS_E_* code (static storage, never NULL). */
 const char *ocs_strerror(int code);
@@ -507,8 +507,9 @@ int ocs_fold_weights(const int8_t *Wq, int64_t ldq, int64_t N, int C, int g, int
  *        Xq[m, .] = Eq. 1's code of x' on the grid of T_m, pad columns zero
  *   with the arithmetic of ocs_quantize on that row alone (a row of zeros: step 0, codes 0).
  *   chan_src [C + num_splits] as the selection writes it: its first C entries are 0 .. C-1 (NULL with
- *   num_splits = 0).  Activations of Eq. 3 take chan_depth = NULL; weights [N, C*g] take the selection's
- *   chan_src and chan_depth and give codes with a step per output channel.
+ *   num_splits = 0: then C is bounded by C*g <= 2^30 alone, not by the selection's OCS_MAX_EXPANDED_CHANNELS).  Activations of
+ *   Eq. 3 take chan_depth = NULL; weights [N, C*g] take the selection's chan_src and chan_depth and give codes with a step per
+ *   output channel.
  *   A row with NaN or an infinity: its step is not finite and its codes are unspecified, other rows are as without.
  *   Xq: ldq >= (C + num_splits)*g, a multiple of OCS_CALIGN, 16-byte aligned base.  step_out: M floats.
  *

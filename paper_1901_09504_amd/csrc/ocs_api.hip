@@ -47,12 +47,13 @@ static int check_workspace(const void* ws, size_t ws_bytes, int64_t rows, int64_
     return OCS_OK;
 }
 
-static int check_layer(int64_t rows, int C, int g, int64_t ld, int num_splits) {
+// selected: the channels come from a selection, which C + num_splits have to fit.
+static int check_layer(int64_t rows, int C, int g, int64_t ld, int num_splits, bool selected = true) {
     if (rows <= 0 || C <= 0 || g <= 0) return OCS_E_SHAPE;
     if ((int64_t)C * g > (int64_t)1 << 30 || rows > (int64_t)1 << 31) return OCS_E_SHAPE;
     if (ld < (int64_t)C * g) return OCS_E_SHAPE;
     if (num_splits < 0) return OCS_E_SPLITS;
-    if ((int64_t)C + num_splits > OCS_MAX_EXPANDED_CHANNELS) return OCS_E_SPLITS;
+    if (selected && (int64_t)C + num_splits > OCS_MAX_EXPANDED_CHANNELS) return OCS_E_SPLITS;
     return OCS_OK;
 }
 
@@ -953,7 +954,7 @@ static int check_row_grids(const void* X, int type, int64_t M, int C, int g, int
                            int bits, float clip_ratio, const int8_t* Xq, int64_t ldq, const float* step) {
     if ((M != 0 && (!X || !Xq || !step)) || (num_splits > 0 && !chan_src)) return OCS_E_NULL;
     if (!type_ok(type)) return OCS_E_TYPE;
-    int rc = check_layer(M == 0 ? 1 : M, C, g, ldx, num_splits);
+    int rc = check_layer(M == 0 ? 1 : M, C, g, ldx, num_splits, num_splits > 0);
     if (rc) return rc;
     const int64_t Ke = (int64_t)(C + num_splits) * g;
     if (Ke > (int64_t)1 << 30) return OCS_E_SHAPE;

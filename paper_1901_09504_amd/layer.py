@@ -304,6 +304,7 @@ class ConvChain:
 class TokenLayer:
     """The layer of Eq. 3 with a grid of its own for every token (row of X) and every output channel (row of W), where
     ExpandedLayer has one per tensor: an outlier token costs only itself precision.  X and Y in fp32, bf16 or fp16.
+    Channels are selected among up to 8000 with their copies; without splits (r = 0) there is no selection and no such bound.
 
     A call runs on `stream`, or on the current one.  Whatever streams a layer is used on, its buffers are not handed out again before
     their work is done; that one stream's call comes before another's (they share the buffers) is the caller's to see to.
@@ -328,6 +329,9 @@ class TokenLayer:
         self.Wq = torch.empty((self.N, self.ldq), dtype=torch.int8, device=device)
         self.step_w = torch.empty(self.N, dtype=torch.float32, device=device)
         self.bias = None
+        if self.s == 0:                                     # what a selection of none would write
+            torch.arange(E, out=self.chan_src)
+            self.chan_depth.zero_()
         self._weights_from = torch.cuda.current_stream()    # the streams whose memory the buffers are
         self._rows_from = self._weights_from
         self._streams = set()                               # those that they may be used on
@@ -373,10 +377,11 @@ class TokenLayer:
         self.bias = bias
         self._streams.clear()
         self._use_on_current_stream()
-        ws = B.alloc_workspace(self.N, self.K, self.device)
-        B.ocs_select_channels(W, self.N, self.C, self.g, W.stride(0), self.s, self.split_src, self.chan_src, self.chan_depth, None, ws)
-        B.ocs_split_quantize_rows(W, self.N, self.C, self.g, W.stride(0), self.chan_src, self.chan_depth, self.s, self.bits_w,
-                                  self.clip_ratio_w, self.Wq, self.ldq, self.step_w)
+        if self.s:
+            ws = B.alloc_workspace(self.N, self.K, self.device)
+            B.ocs_select_channels(W, self.N, self.C, self.g, W.stride(0), self.s, self.split_src, self.chan_src, self.chan_depth, None, ws)
+        B.ocs_split_quantize_rows(W, self.N, self.C, self.g, W.stride(0), self.chan_src, self.chan_depth if self.s else None, self.s,
+                                  self.bits_w, self.clip_ratio_w, self.Wq, self.ldq, self.step_w)
 
     def forward(self, X, stream=None):
         """X [M, C*g] in fp32, bf16 or fp16 -> Y [M, N] in out_dtype (M = 0 included), the layer's own buffer: the next call
