@@ -372,8 +372,8 @@ class TokenLayer:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.prepare_weights(W, bias)
-        assert W.dtype == torch.float32 and W.shape == (self.N, self.K) and W.stride(1) == 1
-        assert bias is None or (bias.dtype == torch.float32 and bias.shape == (self.N,) and bias.is_contiguous())
+        assert W.is_cuda and W.dtype == torch.float32 and W.shape == (self.N, self.K) and W.stride(1) == 1
+        assert bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.shape == (self.N,) and bias.is_contiguous())
         self.bias = bias
         self._streams.clear()
         self._use_on_current_stream()
@@ -391,7 +391,7 @@ class TokenLayer:
                 Y = self.forward(X)
             Y.record_stream(torch.cuda.current_stream())    # the caller reads it on its own
             return Y
-        assert X.dim() == 2 and X.shape[1] == self.K and (X.stride(1) == 1 or X.shape[0] == 0)
+        assert X.is_cuda and X.dim() == 2 and X.shape[1] == self.K and (X.stride(1) == 1 or X.shape[0] == 0)
         M = X.shape[0]
         if M == 0:
             return torch.empty((0, self.N), dtype=self.out_dtype, device=self.device)
@@ -417,9 +417,9 @@ def token_logprobs(logits, tokens=None, top_k=0, stream=None):
         for t in out.values():
             t.record_stream(caller)
         return out
-    assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[0] == 0 or logits.shape[1] == 1)
+    assert logits.is_cuda and logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[0] == 0 or logits.shape[1] == 1)
     M, V = logits.shape
-    assert tokens is None or (tokens.dtype == torch.int32 and tokens.shape == (M,) and tokens.is_contiguous())
+    assert tokens is None or (tokens.is_cuda and tokens.dtype == torch.int32 and tokens.shape == (M,) and tokens.is_contiguous())
     f32 = dict(dtype=torch.float32, device=logits.device)
     out = dict(entropy=torch.empty(M, **f32))
     if tokens is not None:

@@ -33,3 +33,25 @@ def test_with_splits_it_does():
 def test_other_bounds_hold_without_splits():
     assert _quantize(1 << 30, 0) == 0 and _quantize((1 << 30) + 1, 0) == -2 and _quantize(1 << 20, 0, g=1 << 11) == -2
     assert _forward(140000, 0) == -6                         # 140000 x 127 x 127 does not fit an accumulator
+
+
+# ---- tensors of the host -------------------------------------------------------------------------
+
+def test_tensors_of_the_host_are_refused_before_any_call(monkeypatch):
+    """Their addresses mean nothing to the GPU: no call may be made with them."""
+    from paper_1901_09504_amd import layer
+
+    called = []
+    for n in ("ocs_select_channels", "ocs_split_quantize_rows", "ocs_forward_rows", "ocs_token_logprobs", "alloc_workspace"):
+        monkeypatch.setattr(layer.B, n, lambda *a, **k: called.append(a))
+    head = object.__new__(layer.TokenLayer)
+    head.N, head.K, head.C, head.g, head.s = 4, 8, 8, 1, 0
+    with pytest.raises(AssertionError):
+        head.prepare_weights(torch.zeros(4, 8))
+    with pytest.raises(AssertionError):
+        head.forward(torch.zeros(2, 8))
+    with pytest.raises(AssertionError):
+        layer.token_logprobs(torch.zeros(2, 8))
+    with pytest.raises(AssertionError):
+        layer.token_logprobs(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int32), 3)
+    assert not called
