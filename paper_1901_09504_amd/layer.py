@@ -372,15 +372,16 @@ class TokenLayer:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.prepare_weights(W, bias)
-        assert W.is_cuda and W.dtype == torch.float32 and W.shape == (self.N, self.K) and W.stride(1) == 1
+        assert W.is_cuda and W.dtype == torch.float32 and W.shape == (self.N, self.K) and (W.stride(1) == 1 or self.K == 1)
         assert bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.shape == (self.N,) and bias.is_contiguous())
+        ldw = W.stride(0) if self.N > 1 else self.K         # (a single row's or column's own stride means nothing)
         self.bias = bias
         self._streams.clear()
         self._use_on_current_stream()
         if self.s:
             ws = B.alloc_workspace(self.N, self.K, self.device)
-            B.ocs_select_channels(W, self.N, self.C, self.g, W.stride(0), self.s, self.split_src, self.chan_src, self.chan_depth, None, ws)
-        B.ocs_split_quantize_rows(W, self.N, self.C, self.g, W.stride(0), self.chan_src, self.chan_depth if self.s else None, self.s,
+            B.ocs_select_channels(W, self.N, self.C, self.g, ldw, self.s, self.split_src, self.chan_src, self.chan_depth, None, ws)
+        B.ocs_split_quantize_rows(W, self.N, self.C, self.g, ldw, self.chan_src, self.chan_depth if self.s else None, self.s,
                                   self.bits_w, self.clip_ratio_w, self.Wq, self.ldq, self.step_w)
 
     def forward(self, X, stream=None):
@@ -391,7 +392,7 @@ class TokenLayer:
                 Y = self.forward(X)
             Y.record_stream(torch.cuda.current_stream())    # the caller reads it on its own
             return Y
-        assert X.is_cuda and X.dim() == 2 and X.shape[1] == self.K and (X.stride(1) == 1 or X.shape[0] == 0)
+        assert X.is_cuda and X.dim() == 2 and X.shape[1] == self.K and (X.stride(1) == 1 or X.shape[0] == 0 or self.K == 1)
         M = X.shape[0]
         if M == 0:
             return torch.empty((0, self.N), dtype=self.out_dtype, device=self.device)

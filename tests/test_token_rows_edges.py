@@ -351,3 +351,27 @@ def test_wide_layer_without_splits(M, C, N):
     code = (W * (torch.full_like(t, 127) / t)).clamp(-127, 127).round()
     assert torch.equal(head.Wq[:, :C], code.to(torch.int8))
     assert torch.equal(head.chan_src, torch.arange(C, dtype=torch.int32, device="cuda")) and not head.chan_depth.any()
+
+
+# ---- layouts of one row and of one column --------------------------------------------------------
+
+def test_layers_of_one_input_and_of_one_output_in_any_layout():
+    """The stride along a dimension of one element means nothing."""
+    from paper_1901_09504_amd.layer import TokenLayer
+
+    for r in (0.0, 1.0):
+        x = torch.randn((5, 3), device="cuda").t().contiguous().t()      # strides 1, 5
+        w = torch.randn((4, 2), device="cuda").t().contiguous().t()
+        head = TokenLayer(4, 1, r)
+        head.prepare_weights(w[:, 1:])
+        y = head.forward(x[:, 2:]).clone()
+        head.prepare_weights(w[:, 1:].contiguous())
+        assert torch.equal(y, head.forward(x[:, 2:].contiguous())) and bool(y.any())
+        x = torch.randn((6, 40), device="cuda")
+        w = torch.randn((40, 1), device="cuda").t()                      # one row, strides 1, 1
+        assert w.stride() == (1, 1)
+        head = TokenLayer(1, 40, r)
+        head.prepare_weights(w)
+        y = head.forward(x).clone()
+        head.prepare_weights(w.clone(memory_format=torch.contiguous_format))
+        assert torch.equal(y, head.forward(x)) and bool(y.any())
