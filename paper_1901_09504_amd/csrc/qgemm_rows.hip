@@ -5,7 +5,7 @@
 // holds four consecutive outputs of one token and stores them as they are, without a detour through LDS.
 // Codes go from memory straight into LDS, 128 bytes (one line) of 8 rows per request, 16-byte chunks XOR-ed with the row so that
 // the matrix cores' reads of consecutive rows fall into different banks.
-// Many tokens: 8192 x 4096 x 4178 bf16 116 us, 2.4 POPS, where a bare loop of these instructions on random codes sustains 4.1; a step's requests, LDS
+// Many tokens: 8192 x 4096 x 4178 bf16 118 us, 2.4 POPS, where a bare loop of these instructions on random codes sustains 4.1; a step's requests, LDS
 // reads and products add up more than they hide (768 x 8192 -> 6016: 32 us of requests and 32 of products make 49).  Few tokens: the weights' bytes.
 #include <atomic>
 #include <type_traits>
@@ -762,10 +762,15 @@ static hipError_t run_rows_image(RowsGemm p, const RowGrids& g, int type, int se
 // 3150 5.0 against 11.1 in 64 x 64 tiles, 1000 x 256 x 2000 5.6 / 7.9, 300 x 500 x 5000 7.9 / 15.7; 64 x 6000 x 3150 8.6 / 11.0).
 // Then tiles: rounds of the chip times what a tile takes, a constant and a cost per step in 10 ns, fitted to tiles of every size alone
 // and under load.  128 x 128 comes twice: a ring of three steps, and where there are more tiles than compute units one of two, of which a
-// unit holds two workgroups whose ends and starts hide behind each other (300 x 33001 x 1575 42.7 us in 192 x 128, 37.3 this way).  It
-// found the fastest of the first five on all 19 shapes that were measured (us): 333 x 2049 x 1052 64 x 64 6.7 (128 x
-// 128 10.7), 400 x 8000 x 3150 128 x 128 17.2 (64 x 64 24, 256 x 128 25.5), 700 x 6000 x 3150 192 x 128 23 (256 x 128 28, 128 x 128 33),
-// 8192 x 4096 x 4178 256 x 256 132 (256 x 128 153, 128 x 128 177), 700 x 33001 x 1575 256 x 256 65 (192 x 128 75).
+// unit holds two workgroups whose ends and starts hide behind each other.  It finds the fastest of the six on these (us, from a graph,
+// three sets of operands in turn, 64 x 64 / 128 x 128 / 192 x 128 / 256 x 128 / 256 x 256 / two to a unit):
+//   333 x 2049 x 1052 fp16      6.6 /   8.6 /  10.9 /  12.9 /  19.9 /   8.6
+//   400 x 8000 x 3150 fp32     25.6 /  19.5 /  24.1 /  28.5 /  43.1 /  22.7
+//   700 x 6000 x 3150 fp32     31.7 /  31.8 /  23.3 /  27.9 /  41.5 /  28.1
+//   8192 x 4096 x 4178 bf16     227 /   180 /   160 /   145 /   118 /   155
+//   700 x 33001 x 1575 fp32     104 /  81.4 /  81.2 /  74.6 /  68.8 /  73.7
+//   300 x 33001 x 1575 fp32    49.4 /  41.1 /  43.4 /  51.9 /  53.2 /  39.3
+// It knows nothing of the outputs' bytes: the model's 51 us for 700 x 33001 x 1575 are 69.
 template <Elem OUT>
 static hipError_t run_rows_gemm(const RowsGemm& p, hipStream_t stream) {
     if (p.ldx >= kWidePitch || p.ldw >= kWidePitch) return run_rows_tile<64, 64, 2, 2, 4, OUT, true>(p, stream);

@@ -12,7 +12,8 @@
 namespace ocs {
 
 constexpr int kTopGroups = 256;       // maxima of lanes, or of quads of them, that are held against the bound
-constexpr int kTopList = 1024;        // logits that may reach it; more (rows of equal values) are selected one by one
+constexpr int kTopList = 1024;        // logits that may reach it; more are selected one by one, each a pass over the row:
+                                      // rows of equal values, and few rows of logits that fall from token to token (see bound_of)
 constexpr float kLowest = -3.402823466e+38f;
 constexpr float kLog2e = 1.44269504f;
 
@@ -129,7 +130,10 @@ __device__ __forceinline__ void write_top(const TokenRows& p, int64_t row, const
 
 constexpr unsigned kFirstFinite = 0x00800000u;      // order_of(kLowest): what is below is -inf or nothing
 
-// A number that at least k of the wave's keys (4 a lane) reach: the k-th largest of the lanes' maxima, to its upper 16 bits.
+// A number that at least k of the wave's keys (4 a lane) reach: the k-th largest of the lanes' maxima, to its upper 16 bits.  A lane's four
+// groups are neighbours in the row, so it is a weak bound where large logits are (us, k = 5 / 20 / 32, of shuffled logits, of -log rank + N(0, 1)
+// in order of rank, of -log rank alone, of equal ones: 1 x 33001 fp32 6.4 / 6.9 / 7.2, 6.6 / 8.2 / 11.0, 9.7 / 114 / 178, 40 / 121 / 186;
+// 700 x 33001 bf16 12.9 / 14.2 / 15.7, 14.2 / 20.4 / 25.2, 17.8 / 53 / 100, 290 / 933 / 1441).
 __device__ __forceinline__ unsigned bound_of(u32x4 keys, int k) {
     unsigned most = keys[0];
 #pragma unroll
@@ -503,6 +507,13 @@ static hipError_t run_token_kernel(TokenRows p, int64_t M, hipStream_t stream) {
     return hipSuccess;
 }
 
+// fp32 rows that 1024 lanes hold: 4, 9 or 16 pieces a lane.  A piece costs its exponentials whether the row fills it or not, 0.2-0.3 us.  9
+// serves rows of 16385 to 36864 logits; 8 would save 0.3-0.4 us up to 32768 and send those above to 16 pieces, 2 us more; 12 would cost
+// 0.6-0.8 us up to 36864 and save 1 us from there to 49152 (us, 20 alternatives, 1 row / 250 rows, by pieces a lane):
+//   32000 logits   8: 6.5 / 8.1    9: 6.8 / 8.5   10: 7.1 / 8.7    12: 7.6 / 9.2
+//   33001                          9: 6.8 / 8.9   10: 7.3 / 9.1    12: 7.4 / 9.6    16: 9.2 / 11.0
+//   40000                                         10: 7.2 / 10.5   12: 7.7 / 10.8   16: 8.9 / 11.7
+//
 // Rows of up to 2048 pieces are held by 256 lanes.  Longer ones: while every row can have a compute unit to itself, by 1024 (1 x 33001
 // fp32 7.0 us with 20 alternatives, 6.2 with 5; passing through 256 lanes, with the row's second look from memory, 19 where this took 8.1), otherwise they pass through 256 lanes, or 512 where
 // rows come in several rounds and the last one's length counts (us, 256 / 512 lanes: 700 x 33001 fp32 18.7 / 19.2, bf16 14.2 / 14.9; 3000
