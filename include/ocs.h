@@ -71,12 +71,18 @@ extern "C" {
 #define OCS_E_TYPE (-11)     /* unknown element type                                         */
 #define OCS_E_TOP (-12)      /* top_k negative, above OCS_MAX_TOP or above the row's length   */
 
+#define OCS_E_SCALE (-13)    /* scale is not a finite number                                 */
+
 #define OCS_MODE_HALVE 0 /* choose channels on this tensor and halve both copies (Eq. 3)     */
 #define OCS_MODE_DUP 1   /* channel choice given; copy channels un-halved (Eq. 4, weights)   */
 
 #define OCS_F32 0  /* element types of the calls with a grid per row and of token scoring      */
 #define OCS_BF16 1
 #define OCS_F16 2
+
+#define OCS_MX_BLOCK 32  /* columns that share a scale on microscaled 4-bit grids                */
+#define OCS_CACHE_INT8 0 /* formats of a quantized cache                                          */
+#define OCS_CACHE_MX4 1
 
 #define OCS_MAX_TOP 32 /* most alternatives per row of ocs_token_logprobs                       */
 
@@ -531,6 +537,81 @@ int ocs_forward_rows(const void *X, int type, int64_t M, int C, int g, int64_t l
                      int bits_x, float clip_ratio, int8_t *Xq, int64_t ldq, float *step_x_out, const int8_t *Wq,
                      int64_t ldw, int64_t N, int bits_w, const float *step_w, const float *bias, void *Y, int out_type,
                      int64_t ldy, void *stream);
+
+/*
+ * Microscaled 4-bit grids: a row's columns in blocks of OCS_MX_BLOCK, each block on a grid of its own.  A code is a 4-bit floating-point
+ * number (e2m1: magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes 0 .. 7, bit 3 the sign), a scale a byte b for 2^(b - 127) (e8m0; 255 for
+ * NaN).  Weights and activations take 17 bits for 4 values, and the matrix cores multiply them as they are.  M = 0 is OCS_OK and
+ * launches nothing.
+ *
+ * Codes [M, ldq] bytes, two columns a byte, the even one in the low half; ldq >= half the columns.  Scales [M, lds] bytes, one per block;
+ *   lds >= the blocks.  Pitches are multiples of OCS_CALIGN, bases 16-byte aligned; what lies behind the last column or block is zero:
+ *   the producer writes it, the product relies on it.  ocs_mx_code_pitch and ocs_mx_scale_pitch give pitches for `cols` columns.
+ *
+ * ocs_split_quantize_mx: X and the channels' lists as for ocs_split_quantize_rows.  For a block of the expanded row
+ *        x' = X[m, chan_src[j]*g + t] * 2^-chan_depth[j] (fp32; chan_depth NULL: no factor),  a = max |x'|,
+ *        scale 2^e with e = floor(log2 a) - 2 (at least -127; a = 0: -127),  code = the number nearest to x' * 2^-e, halves to the even
+ *        code, at most 6.  A block with NaN or an infinity: scale 255, codes 0.
+ * ocs_dequantize_mx: Y[m, k] = the number that column k's code and scale stand for, k < cols, rounded to out_type (bf16 and fp32 hold it
+ *   exactly).
+ * ocs_qgemm_mx: Y[m, n] = sum over k of x w + bias[n], products exact, sums in fp32, rounded once to out_type; bias [N] fp32 or NULL.
+ * ocs_forward_mx: the two as one call (weight OCS, Eq. 3: activations' copies un-scaled), Xq and Xs left as ocs_split_quantize_mx leaves
+ *   them.  Few tokens run as one launch, but where Y, Xq or Xs share memory with what is read; sums may be taken in another order then.
+ */
+int64_t ocs_mx_code_pitch(int64_t cols);
+int64_t ocs_mx_scale_pitch(int64_t cols);
+int ocs_split_quantize_mx(const void *X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t *chan_src,
+                          const int32_t *chan_depth, int num_splits, uint8_t *codes, int64_t ldq, uint8_t *scales, int64_t lds,
+                          void *stream);
+int ocs_dequantize_mx(const uint8_t *codes, int64_t ldq, const uint8_t *scales, int64_t lds, int64_t M, int64_t cols, void *Y,
+                      int out_type, int64_t ldy, void *stream);
+int ocs_qgemm_mx(const uint8_t *Xq, int64_t ldx, const uint8_t *Xs, int64_t ldxs, const uint8_t *Wq, int64_t ldw, const uint8_t *Ws,
+                 int64_t ldws, int64_t M, int64_t N, int64_t Kexp, const float *bias, void *Y, int out_type, int64_t ldy, void *stream);
+int ocs_forward_mx(const void *X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t *chan_src, int num_splits, uint8_t *Xq,
+                   int64_t ldq, uint8_t *Xs, int64_t ldxs, const uint8_t *Wq, int64_t ldw, const uint8_t *Ws, int64_t ldws, int64_t N,
+                   const float *bias, void *Y, int out_type, int64_t ldy, void *stream);
+
+/*
+ * A quantized key/value cache in pages, and the attention that reads it.
+ *
+ * The pool: `pages` pages of page_rows positions (a multiple of 16) for each of `heads` heads of D columns (a multiple of 32, up to 256).
+ *   OCS_CACHE_INT8: codes int8 [pages, heads, page_rows, D], steps fp32 [pages, heads, page_rows]: Eq. 1 with 8 bits on each row's grid.
+ *   OCS_CACHE_MX4: codes [pages, heads, page_rows, D / 2] bytes, scales [pages, heads, page_rows, D / 32] bytes: blocks as above.
+ *   Keys and values have codes and scales each; 16-byte aligned bases.
+ * Channels with outliers (keys have them): key_depth, value_depth [heads, D] (NULL: none) say how often a channel is halved before
+ *   its row's grid is laid, 0 .. 126; what reads the cache doubles it as often.  That is splitting (Eq. 3) with the equal copies kept once.
+ * Sequences: tokens cu[b] .. cu[b+1] - 1 of the call's T are positions starts[b], starts[b] + 1, ... of sequence b; cu [B + 1]
+ *   ascending from 0, starts [B].  Tokens from cu[B] on belong to none: nothing is read or written for them.  Position j lies in row
+ *   j % page_rows of page table[b, j / page_rows] (table [B, ldt], table_cols columns used); a page outside 0 .. pages - 1 is not there.
+ *
+ * ocs_cache_write: keys and values [T, heads, D] of element type `type`, ld elements between tokens and hd between heads -> their rows
+ *   of the pool; positions without a page are left out.  Two tokens of a call must not be the same row of the pool.
+ *   A row with NaN or an infinity: 8 bits: a step that is not finite, 4 bits: scales 255.
+ * ocs_cache_read: the rows as numbers, rounded once to `type`; positions without a page read as 0.
+ * ocs_cache_attention: queries Q [T, query_heads, D] of the tokens, whose own rows the pool holds already; query head i reads
+ *   head i / (query_heads / heads).  Over the positions j that a token at position p sees, j <= p, j > p - window (window 0: all),
+ *   j < most, with a page that is there:
+ *        s_j = scale * q . k_j,   Y[t, i] = sum exp(s_j) v_j / sum exp(s_j),   lse[t, i] = log sum exp(s_j)   (dense fp32, may be NULL).
+ *   A token that sees none: Y 0, lse -inf.  What other positions' rows hold does not matter.  `most` is at least the longest sequence's
+ *   positions, this call's among them.  Scores and sums in fp32; bf16 queries meet weights rounded to bf16, others finer ones.
+ *   workspace: at least ocs_cache_attention_workspace_bytes() bytes, 256-byte aligned; it may be NULL where that is 0.  Needs no
+ *   initialisation.
+ * T = 0 or B = 0 is OCS_OK and launches nothing.
+ */
+int ocs_cache_write(const void *K, int64_t ldk, int64_t hdk, const void *V, int64_t ldv, int64_t hdv, int type, int64_t T,
+                    const int32_t *cu, const int32_t *starts, int64_t B, const int32_t *table, int64_t table_cols, int64_t ldt, int format,
+                    void *keys, void *key_scales, void *values, void *value_scales, int64_t pages, int page_rows, int heads, int D,
+                    const int32_t *key_depth, const int32_t *value_depth, void *stream);
+int ocs_cache_read(void *K, int64_t ldk, int64_t hdk, void *V, int64_t ldv, int64_t hdv, int type, int64_t T, const int32_t *cu,
+                   const int32_t *starts, int64_t B, const int32_t *table, int64_t table_cols, int64_t ldt, int format, const void *keys,
+                   const void *key_scales, const void *values, const void *value_scales, int64_t pages, int page_rows, int heads, int D,
+                   const int32_t *key_depth, const int32_t *value_depth, void *stream);
+size_t ocs_cache_attention_workspace_bytes(int64_t T, int64_t B, int heads, int query_heads, int D, int64_t most, int64_t window);
+int ocs_cache_attention(const void *Q, int type, int64_t ldq, int64_t hdq, int query_heads, int64_t T, const int32_t *cu,
+                        const int32_t *starts, int64_t B, int64_t most, const int32_t *table, int64_t table_cols, int64_t ldt, int format,
+                        const void *keys, const void *key_scales, const void *values, const void *value_scales, int64_t pages,
+                        int page_rows, int heads, int D, const int32_t *key_depth, const int32_t *value_depth, float scale, int64_t window,
+                        void *Y, int64_t ldy, int64_t hdy, float *lse, void *workspace, size_t ws_bytes, void *stream);
 
 /*
  * Scoring of tokens: what a language model is judged by (perplexity is exp of the mean of -logprob over the positions that have a

@@ -18,6 +18,9 @@ MODE_HALVE = 0
 MODE_DUP = 1
 MAX_EXPANDED_CHANNELS = 8000
 MAX_TOP = 32
+MX_BLOCK = 32
+CACHE_INT8 = 0
+CACHE_MX4 = 1
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # OCS_F32, OCS_BF16, OCS_F16
 
 
@@ -129,6 +132,28 @@ def lib():
     L.ocs_forward_rows.restype = _i32
     L.ocs_forward_rows.argtypes = [_vp, _i32, _i64, _i32, _i32, _i64, _vp, _i32, _i32, _f32, _vp, _i64, _vp, _vp, _i64, _i64,
                                    _i32, _vp, _vp, _vp, _i32, _i64, _vp]
+    L.ocs_mx_code_pitch.restype = _i64
+    L.ocs_mx_code_pitch.argtypes = [_i64]
+    L.ocs_mx_scale_pitch.restype = _i64
+    L.ocs_mx_scale_pitch.argtypes = [_i64]
+    L.ocs_split_quantize_mx.restype = _i32
+    L.ocs_split_quantize_mx.argtypes = [_vp, _i32, _i64, _i32, _i32, _i64, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp]
+    L.ocs_dequantize_mx.restype = _i32
+    L.ocs_dequantize_mx.argtypes = [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _i32, _i64, _vp]
+    L.ocs_qgemm_mx.restype = _i32
+    L.ocs_qgemm_mx.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _i32, _i64, _vp]
+    L.ocs_forward_mx.restype = _i32
+    L.ocs_forward_mx.argtypes = [_vp, _i32, _i64, _i32, _i32, _i64, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp,
+                                 _i32, _i64, _vp]
+    pool = [_vp, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _vp, _vp]
+    for call in (L.ocs_cache_write, L.ocs_cache_read):
+        call.restype = _i32
+        call.argtypes = [_vp, _i64, _i64, _vp, _i64, _i64, _i32, _i64, _vp, _vp, _i64, *pool, _vp]
+    L.ocs_cache_attention_workspace_bytes.restype = _sz
+    L.ocs_cache_attention_workspace_bytes.argtypes = [_i64, _i64, _i32, _i32, _i32, _i64, _i64]
+    L.ocs_cache_attention.restype = _i32
+    L.ocs_cache_attention.argtypes = [_vp, _i32, _i64, _i64, _i32, _i64, _vp, _vp, _i64, _i64, *pool, _f32, _i64, _vp, _i64, _i64, _vp, _vp,
+                                      _sz, _vp]
     L.ocs_token_logprobs_workspace_bytes.restype = _sz
     L.ocs_token_logprobs_workspace_bytes.argtypes = [_i64, _i64, _i32]
     L.ocs_token_logprobs.restype = _i32
@@ -429,13 +454,13 @@ def ocs_qgemm_split_k(Xq, ldx, Wq, ldw, M, N, Kexp, bits_x, bits_w, scale_x, sca
                                    _stream(stream)), "ocs_qgemm_split_k")
 
 
-# ---- a grid per row, and the scoring of tokens (element types are the tensors' own) ------------
+# ---- a grid per row or per block, a quantized cache, the scoring of tokens (element types are the tensors' own) ------------
 
 _rows_call = None
 
 
 def _calls():
-    """The module that makes these four calls (csrc/rows_call.cpp), built with libocs.so."""
+    """The module that makes these calls (csrc/rows_call.cpp), built with libocs.so."""
     global _rows_call
     if _rows_call is None:
         lib()
@@ -461,6 +486,52 @@ def ocs_forward_rows(X, M, Cn, g, ldx, chan_src, num_splits, bits_x, clip_ratio,
                      bias, Y, ldy, stream=None):
     _check(_calls().forward_rows(X, M, Cn, g, ldx, chan_src, num_splits, bits_x, clip_ratio, Xq, ldq, step_x_out, Wq, ldw, N, bits_w,
                                  step_w, bias, Y, ldy, stream), "ocs_forward_rows")
+
+
+def ocs_mx_code_pitch(cols):
+    return int(lib().ocs_mx_code_pitch(int(cols)))
+
+
+def ocs_mx_scale_pitch(cols):
+    return int(lib().ocs_mx_scale_pitch(int(cols)))
+
+
+def ocs_split_quantize_mx(X, M, Cn, g, ldx, chan_src, chan_depth, num_splits, codes, ldq, scales, lds, stream=None):
+    _check(_calls().split_quantize_mx(X, M, Cn, g, ldx, chan_src, chan_depth, num_splits, codes, ldq, scales, lds, stream),
+           "ocs_split_quantize_mx")
+
+
+def ocs_dequantize_mx(codes, ldq, scales, lds, M, cols, Y, ldy, stream=None):
+    _check(_calls().dequantize_mx(codes, ldq, scales, lds, M, cols, Y, ldy, stream), "ocs_dequantize_mx")
+
+
+def ocs_qgemm_mx(Xq, ldx, Xs, ldxs, Wq, ldw, Ws, ldws, M, N, Kexp, bias, Y, ldy, stream=None):
+    _check(_calls().qgemm_mx(Xq, ldx, Xs, ldxs, Wq, ldw, Ws, ldws, M, N, Kexp, bias, Y, ldy, stream), "ocs_qgemm_mx")
+
+
+def ocs_forward_mx(X, M, Cn, g, ldx, chan_src, num_splits, Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, N, bias, Y, ldy, stream=None):
+    _check(_calls().forward_mx(X, M, Cn, g, ldx, chan_src, num_splits, Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, N, bias, Y, ldy, stream),
+           "ocs_forward_mx")
+
+
+# The pool of a quantized cache is fourteen arguments of each call: table, its columns and pitch, the format, codes and scales of keys, of
+# values, pages, positions a page, heads, columns of a head, the channels' halvings of keys, of values.
+
+def ocs_cache_write(K, ldk, hdk, V, ldv, hdv, T, cu, starts, Bn, *pool, stream=None):
+    _check(_calls().cache_write(K, ldk, hdk, V, ldv, hdv, T, cu, starts, Bn, *pool, stream), "ocs_cache_write")
+
+
+def ocs_cache_read(K, ldk, hdk, V, ldv, hdv, T, cu, starts, Bn, *pool, stream=None):
+    _check(_calls().cache_read(K, ldk, hdk, V, ldv, hdv, T, cu, starts, Bn, *pool, stream), "ocs_cache_read")
+
+
+def ocs_cache_attention_workspace_bytes(T, Bn, heads, query_heads, D, most, window=0):
+    return int(lib().ocs_cache_attention_workspace_bytes(int(T), int(Bn), int(heads), int(query_heads), int(D), int(most), int(window)))
+
+
+def ocs_cache_attention(Q, ldq, hdq, query_heads, T, cu, starts, Bn, most, *pool_and_output, stream=None):
+    """pool_and_output: the pool, then scale, window, Y, ldy, hdy, lse, workspace."""
+    _check(_calls().cache_attention(Q, ldq, hdq, query_heads, T, cu, starts, Bn, most, *pool_and_output, stream), "ocs_cache_attention")
 
 
 def ocs_token_logprobs_workspace_bytes(M, V, top_k):

@@ -8,7 +8,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libocs.so")
 CALLS = os.path.join(_HERE, "_rows_call.so")
 SOURCES = ["ocs_api.hip", "reduce.hip", "select.hip", "quantize.hip", "qa_split.hip", "clip_search.hip", "qgemm.hip", "row_grids.hip",
-           "qgemm_rows.hip", "token_logprobs.hip", "calib.hip"]
+           "qgemm_rows.hip", "mx_grids.hip", "qgemm_mx.hip", "cache_rows.hip", "cache_attention.hip", "token_logprobs.hip", "calib.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -6,7 +6,7 @@
 #include <string>
 
 #include "../../include/ocs.h"
-#include "ocs_internal.h"
+#include "cache.h"
 
 namespace ocs {
 
@@ -119,6 +119,7 @@ const char* ocs_strerror(int code) {
         case OCS_E_CLIP: return "clip_ratio is not a positive finite number";
         case OCS_E_TYPE: return "unknown element type";
         case OCS_E_TOP: return "top_k negative, above OCS_MAX_TOP or above the row's length";
+        case OCS_E_SCALE: return "scale is not a finite number";
         default: return "unknown error code";
     }
 }
@@ -1024,6 +1025,196 @@ int ocs_forward_rows(const void* X, int type, int64_t M, int C, int g, int64_t l
                        clear_of_outputs(Wq, N * ldw) && clear_of_outputs(step_w, 4 * N) && clear_of_outputs(bias, 4 * N);
     hipError_t e = launch_forward_rows(X, type, ldx, M, C, g, num_splits, chan_src, clip_ratio, qmax_of(bits_x), Xq, ldq, step_x_out,
                                        Wq, ldw, N, step_w, bias, Y, out_type, ldy, apart, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+// ---- grids per block -------------------------------------------------------------------------
+
+int64_t ocs_mx_code_pitch(int64_t cols) { return cols <= 0 ? 0 : round_up(ceil_div(cols, 2), OCS_ROWALIGN); }
+
+int64_t ocs_mx_scale_pitch(int64_t cols) { return cols <= 0 ? 0 : round_up(ceil_div(cols, OCS_MX_BLOCK), OCS_CALIGN); }
+
+// Codes and scales of rows of `cols` columns.
+static int check_mx(const void* q, int64_t ldq, const void* scale, int64_t lds, int64_t cols) {
+    if (cols <= 0 || cols > (int64_t)1 << 30) return OCS_E_SHAPE;
+    if (ldq < ceil_div(cols, 2) || lds < ceil_div(cols, OCS_MX_BLOCK) || ldq > (int64_t)1 << 31 || lds > (int64_t)1 << 30) return OCS_E_SHAPE;
+    if (ldq % OCS_CALIGN != 0 || lds % OCS_CALIGN != 0 || !aligned(q, 16) || !aligned(scale, 16)) return OCS_E_ALIGN;
+    return OCS_OK;
+}
+
+static int check_mx_rows(const void* X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t* chan_src, int num_splits,
+                         const void* q, int64_t ldq, const void* scale, int64_t lds) {
+    if ((M != 0 && (!X || !q || !scale)) || (num_splits > 0 && !chan_src)) return OCS_E_NULL;
+    if (!type_ok(type)) return OCS_E_TYPE;
+    int rc = check_layer(M == 0 ? 1 : M, C, g, ldx, num_splits, num_splits > 0);
+    if (rc) return rc;
+    rc = check_mx(q, ldq, scale, lds, (int64_t)(C + num_splits) * g);
+    if (rc) return rc;
+    return aligned(X, type_bytes(type)) ? OCS_OK : OCS_E_ALIGN;
+}
+
+int ocs_split_quantize_mx(const void* X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t* chan_src,
+                          const int32_t* chan_depth, int num_splits, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds,
+                          void* stream) {
+    int rc = check_mx_rows(X, type, M, C, g, ldx, chan_src, num_splits, codes, ldq, scales, lds);
+    if (rc) return rc;
+    if (M == 0) return OCS_OK;
+    hipError_t e = launch_mx_quantize(X, type, ldx, M, C, g, num_splits, chan_src, chan_depth, codes, ldq, scales, lds,
+                                      static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+int ocs_dequantize_mx(const uint8_t* codes, int64_t ldq, const uint8_t* scales, int64_t lds, int64_t M, int64_t cols, void* Y,
+                      int out_type, int64_t ldy, void* stream) {
+    if (M != 0 && (!codes || !scales || !Y)) return OCS_E_NULL;
+    if (!type_ok(out_type)) return OCS_E_TYPE;
+    if (M < 0 || M > (int64_t)1 << 31 || ldy < cols) return OCS_E_SHAPE;
+    int rc = check_mx(codes, ldq, scales, lds, cols);
+    if (rc) return rc;
+    if (!aligned(Y, type_bytes(out_type))) return OCS_E_ALIGN;
+    if (M == 0) return OCS_OK;
+    hipError_t e = launch_mx_values(codes, ldq, scales, lds, M, cols, Y, out_type, ldy, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+// The product's weights and outputs.
+static int check_mx_product(const uint8_t* Wq, int64_t ldw, const uint8_t* Ws, int64_t ldws, int64_t M, int64_t N, int64_t Kexp,
+                            const float* bias, const void* Y, int out_type, int64_t ldy) {
+    if (!Wq || !Ws || (M != 0 && !Y)) return OCS_E_NULL;
+    if (!type_ok(out_type)) return OCS_E_TYPE;
+    if (M < 0 || N <= 0 || M > (int64_t)1 << 30 || N > (int64_t)1 << 30 || ldy < N) return OCS_E_SHAPE;
+    int rc = check_mx(Wq, ldw, Ws, ldws, Kexp);
+    if (rc) return rc;
+    return aligned(Y, type_bytes(out_type)) && aligned(bias, 4) ? OCS_OK : OCS_E_ALIGN;
+}
+
+int ocs_qgemm_mx(const uint8_t* Xq, int64_t ldx, const uint8_t* Xs, int64_t ldxs, const uint8_t* Wq, int64_t ldw, const uint8_t* Ws,
+                 int64_t ldws, int64_t M, int64_t N, int64_t Kexp, const float* bias, void* Y, int out_type, int64_t ldy, void* stream) {
+    if (M != 0 && (!Xq || !Xs)) return OCS_E_NULL;
+    int rc = check_mx_product(Wq, ldw, Ws, ldws, M, N, Kexp, bias, Y, out_type, ldy);
+    if (rc) return rc;
+    rc = check_mx(Xq, ldx, Xs, ldxs, Kexp);
+    if (rc) return rc;
+    if (M == 0) return OCS_OK;
+    hipError_t e = launch_qgemm_mx(Xq, ldx, Xs, ldxs, Wq, ldw, Ws, ldws, M, N, Kexp, bias, Y, out_type, ldy, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+int ocs_forward_mx(const void* X, int type, int64_t M, int C, int g, int64_t ldx, const int32_t* chan_src, int num_splits, uint8_t* Xq,
+                   int64_t ldq, uint8_t* Xs, int64_t ldxs, const uint8_t* Wq, int64_t ldw, const uint8_t* Ws, int64_t ldws, int64_t N,
+                   const float* bias, void* Y, int out_type, int64_t ldy, void* stream) {
+    int rc = check_mx_rows(X, type, M, C, g, ldx, chan_src, num_splits, Xq, ldq, Xs, ldxs);
+    if (rc) return rc;
+    const int64_t Kexp = (int64_t)(C + num_splits) * g, K = (int64_t)C * g;
+    rc = check_mx_product(Wq, ldw, Ws, ldws, M, N, Kexp, bias, Y, out_type, ldy);
+    if (rc) return rc;
+    if (M == 0) return OCS_OK;
+    // as in ocs_forward_rows: outputs that share memory with what is read keep the two launches
+    const int64_t xb = (int64_t)type_bytes(type) * ((M - 1) * ldx + K), yb = (int64_t)type_bytes(out_type) * ((M - 1) * ldy + N);
+    auto clear_of_outputs = [&](const void* in, int64_t bytes) {
+        return !overlap(in, bytes, Y, yb) && !overlap(in, bytes, Xq, M * ldq) && !overlap(in, bytes, Xs, M * ldxs);
+    };
+    const bool apart = clear_of_outputs(X, xb) && clear_of_outputs(num_splits > 0 ? chan_src : nullptr, 4 * (int64_t)(C + num_splits)) &&
+                       clear_of_outputs(Wq, N * ldw) && clear_of_outputs(Ws, N * ldws) && clear_of_outputs(bias, 4 * N);
+    hipError_t e = launch_forward_mx(X, type, ldx, M, C, g, num_splits, chan_src, Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, N, bias, Y, out_type,
+                                     ldy, apart, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+// ---- a quantized cache -----------------------------------------------------------------------
+
+static int check_cache(int64_t T, const int32_t* cu, const int32_t* starts, int64_t B, int format, const Cache& c) {
+    if (T < 0 || B < 0 || T > (int64_t)1 << 30 || B > (int64_t)1 << 30) return OCS_E_SHAPE;
+    if (T != 0 && B != 0 && (!cu || !starts || !c.table || !c.keys || !c.kscales || !c.values || !c.vscales)) return OCS_E_NULL;
+    if (format != OCS_CACHE_INT8 && format != OCS_CACHE_MX4) return OCS_E_MODE;
+    if (c.cols < 1 || c.ldt < c.cols || c.cols > (int64_t)1 << 31 || c.ldt > (int64_t)1 << 31) return OCS_E_SHAPE;
+    if (c.pages < 1 || c.pages > (int64_t)1 << 31 || c.P < 16 || c.P % 16 != 0 || c.P > 1 << 24 || c.H < 1 || c.H > 65535) return OCS_E_SHAPE;
+    if (c.D < 32 || c.D > 256 || c.D % 32 != 0) return OCS_E_SHAPE;
+    if ((double)c.pages * c.H * c.P > 1e15) return OCS_E_SHAPE;
+    if (!aligned(cu, 4) || !aligned(starts, 4) || !aligned(c.table, 4) || !aligned(c.kdepth, 4) || !aligned(c.vdepth, 4) ||
+        !aligned(c.keys, 16) || !aligned(c.kscales, 16) || !aligned(c.values, 16) || !aligned(c.vscales, 16))
+        return OCS_E_ALIGN;
+    return OCS_OK;
+}
+
+// Rows [T, heads, D] at a pitch of `ld` elements between tokens and `hd` between heads.
+static int check_head_rows(const void* x, int type, int64_t T, int64_t heads, int D, int64_t ld, int64_t hd, bool written) {
+    const int64_t least = written ? D : 0;
+    if (T > 0 && !x) return OCS_E_NULL;
+    if ((T > 1 && ld < least) || (heads > 1 && hd < least) || ld < 0 || hd < 0) return OCS_E_SHAPE;
+    return aligned(x, type_bytes(type)) ? OCS_OK : OCS_E_ALIGN;
+}
+
+static int cache_rows(bool write, void* K, int64_t ldk, int64_t hdk, void* V, int64_t ldv, int64_t hdv, int type, int64_t T,
+                      const int32_t* cu, const int32_t* starts, int64_t B, int format, const Cache& c, void* stream) {
+    if (!type_ok(type)) return OCS_E_TYPE;
+    int rc = check_cache(T, cu, starts, B, format, c);
+    if (rc) return rc;
+    if (B == 0) T = 0;
+    rc = check_head_rows(K, type, T, c.H, c.D, ldk, hdk, !write);
+    if (rc) return rc;
+    rc = check_head_rows(V, type, T, c.H, c.D, ldv, hdv, !write);
+    if (rc) return rc;
+    if (T == 0) return OCS_OK;
+    hipError_t e = launch_cache_rows(write, K, ldk, hdk, V, ldv, hdv, type, Sequences{(int)T, (int)B, cu, starts}, format, c,
+                                     static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? OCS_OK : hip_fail(e);
+}
+
+int ocs_cache_write(const void* K, int64_t ldk, int64_t hdk, const void* V, int64_t ldv, int64_t hdv, int type, int64_t T,
+                    const int32_t* cu, const int32_t* starts, int64_t B, const int32_t* table, int64_t table_cols, int64_t ldt, int format,
+                    void* keys, void* key_scales, void* values, void* value_scales, int64_t pages, int page_rows, int heads, int D,
+                    const int32_t* key_depth, const int32_t* value_depth, void* stream) {
+    const Cache c{table, table_cols, ldt, keys, key_scales, values, value_scales, pages, page_rows, heads, D, key_depth, value_depth};
+    return cache_rows(true, const_cast<void*>(K), ldk, hdk, const_cast<void*>(V), ldv, hdv, type, T, cu, starts, B, format, c, stream);
+}
+
+int ocs_cache_read(void* K, int64_t ldk, int64_t hdk, void* V, int64_t ldv, int64_t hdv, int type, int64_t T, const int32_t* cu,
+                   const int32_t* starts, int64_t B, const int32_t* table, int64_t table_cols, int64_t ldt, int format, const void* keys,
+                   const void* key_scales, const void* values, const void* value_scales, int64_t pages, int page_rows, int heads, int D,
+                   const int32_t* key_depth, const int32_t* value_depth, void* stream) {
+    const Cache c{table, table_cols, ldt, const_cast<void*>(keys), const_cast<void*>(key_scales), const_cast<void*>(values),
+                  const_cast<void*>(value_scales), pages, page_rows, heads, D, key_depth, value_depth};
+    return cache_rows(false, K, ldk, hdk, V, ldv, hdv, type, T, cu, starts, B, format, c, stream);
+}
+
+// What bounds the tiles of a launch: 256 lanes for every 16 rows of a head.
+static bool attention_fits(int64_t T, int64_t B, int64_t heads, int64_t query_heads) {
+    return heads >= 1 && query_heads >= heads && query_heads % heads == 0 && query_heads <= 1 << 20 &&
+           (double)T * (query_heads / heads) / 16 + B < 1 << 23;
+}
+
+size_t ocs_cache_attention_workspace_bytes(int64_t T, int64_t B, int heads, int query_heads, int D, int64_t most, int64_t window) {
+    if (T <= 0 || B <= 0 || T > (int64_t)1 << 30 || B > (int64_t)1 << 30 || !attention_fits(T, B, heads, query_heads) || D <= 0 || most < 0 ||
+        most > 0x7FFFFFFF || window < 0)
+        return 0;
+    return cache_attention_workspace_bytes(T, B, heads, query_heads, D, most, window);
+}
+
+int ocs_cache_attention(const void* Q, int type, int64_t ldq, int64_t hdq, int query_heads, int64_t T, const int32_t* cu,
+                        const int32_t* starts, int64_t B, int64_t most, const int32_t* table, int64_t table_cols, int64_t ldt, int format,
+                        const void* keys, const void* key_scales, const void* values, const void* value_scales, int64_t pages,
+                        int page_rows, int heads, int D, const int32_t* key_depth, const int32_t* value_depth, float scale, int64_t window,
+                        void* Y, int64_t ldy, int64_t hdy, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+    if (!type_ok(type)) return OCS_E_TYPE;
+    const Cache c{table, table_cols, ldt, const_cast<void*>(keys), const_cast<void*>(key_scales), const_cast<void*>(values),
+                  const_cast<void*>(value_scales), pages, page_rows, heads, D, key_depth, value_depth};
+    int rc = check_cache(T, cu, starts, B, format, c);
+    if (rc) return rc;
+    if (!attention_fits(T, B, heads, query_heads) || most < 0 || most > 0x7FFFFFFF || window < 0 || window > (int64_t)1 << 40) return OCS_E_SHAPE;
+    if (B == 0) T = 0;
+    rc = check_head_rows(Q, type, T, query_heads, D, ldq, hdq, false);
+    if (rc) return rc;
+    rc = check_head_rows(Y, type, T, query_heads, D, ldy, hdy, true);
+    if (rc) return rc;
+    if (!aligned(lse, 4)) return OCS_E_ALIGN;
+    if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return OCS_E_SCALE;
+    if (T == 0) return OCS_OK;
+    const size_t need = cache_attention_workspace_bytes(T, B, heads, query_heads, D, most, window);
+    if (need > 0 && (workspace == nullptr || ws_bytes < need)) return OCS_E_WORKSPACE;
+    if (need > 0 && !aligned(workspace, 256)) return OCS_E_ALIGN;
+    hipError_t e = launch_cache_attention(Q, type, ldq, hdq, query_heads, Sequences{(int)T, (int)B, cu, starts}, most, format, c, scale, window,
+                                          Y, ldy, hdy, lse, workspace, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? OCS_OK : hip_fail(e);
 }
 

@@ -238,6 +238,26 @@ hipError_t launch_forward_rows(const void* X, int type, int64_t ldx, int64_t M, 
                                float clip, float qmax, int8_t* Xq, int64_t ldq, float* step_x, const int8_t* Wq, int64_t ldw,
                                int64_t N, const float* step_w, const float* bias, void* Y, int out_type, int64_t ldy,
                                bool apart, hipStream_t stream);
+// Grids per block of 32 columns (csrc/mx_grids.hip) and their product (csrc/qgemm_mx.hip).
+hipError_t launch_mx_quantize(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src,
+                              const int32_t* chan_depth, uint8_t* q, int64_t ldq, uint8_t* scale, int64_t lds, hipStream_t stream);
+hipError_t launch_mx_values(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, int64_t M, int64_t cols, void* Y, int out_type,
+                            int64_t ldy, hipStream_t stream);
+hipError_t launch_qgemm_mx(const uint8_t* Xq, int64_t ldx, const uint8_t* Xs, int64_t ldxs, const uint8_t* Wq, int64_t ldw,
+                           const uint8_t* Ws, int64_t ldws, int64_t M, int64_t N, int64_t Kexp, const float* bias, void* Y, int out_type,
+                           int64_t ldy, hipStream_t stream);
+hipError_t launch_forward_mx(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src, uint8_t* Xq,
+                             int64_t ldq, uint8_t* Xs, int64_t ldxs, const uint8_t* Wq, int64_t ldw, const uint8_t* Ws, int64_t ldws,
+                             int64_t N, const float* bias, void* Y, int out_type, int64_t ldy, bool apart, hipStream_t stream);
+// A quantized cache (csrc/cache_rows.hip, csrc/cache_attention.hip).
+struct Cache;
+struct Sequences;
+hipError_t launch_cache_rows(bool write, void* K, int64_t ldk, int64_t hdk, void* V, int64_t ldv, int64_t hdv, int type, const Sequences& s,
+                             int format, const Cache& c, hipStream_t stream);
+size_t cache_attention_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hq, int64_t D, int64_t most, int64_t window);
+hipError_t launch_cache_attention(const void* Q, int type, int64_t ldq, int64_t hdq, int Hq, const Sequences& s, int64_t most, int format,
+                                  const Cache& c, float scale, int64_t window, void* Y, int64_t ldy, int64_t hdy, float* lse,
+                                  void* workspace, hipStream_t stream);
 size_t token_logprobs_workspace_bytes(int64_t M, int64_t V, int k);
 hipError_t launch_token_logprobs(const void* logits, int type, int64_t M, int64_t V, int64_t ld, const int32_t* tokens, int k,
                                  float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,

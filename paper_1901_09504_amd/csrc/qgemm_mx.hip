@@ -1,0 +1,479 @@
+// Product of operands on microscaled 4-bit grids: Y[m,n] = sum over k of x[m,k] w[n,k] + bias[n], where a block of 32 codes shares a power
+// of two, on the matrix cores (v_mfma_scale_f32_16x16x128_f8f6f4, which takes codes and scale bytes as they are and adds in fp32).
+//
+// As in the int8 product with a scale per row the weights run down an accumulator tile and the tokens across it, and codes go from memory
+// straight into LDS, 128 bytes (256 columns) of 8 rows per request, 16-byte chunks XOR-ed with the row.  A chunk is a block.  A row's 16
+// scale bytes of two steps are a request of their own, one row per lane; a lane of quarter q takes chunks 2q and 2q + 1 of a step, so that
+// their scales are two neighbouring bytes, which the instruction picks from one register.
+#include <type_traits>
+
+#include "mx_grids.h"
+#include "tile_requests.h"
+
+namespace ocs {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+struct MxGemm {
+    const uint8_t* Xq;
+    int64_t ldx;
+    const uint8_t* Xs;
+    int64_t ldxs;
+    const uint8_t* Wq;
+    int64_t ldw;
+    const uint8_t* Ws;
+    int64_t ldws;
+    int M, N, ksteps;                 // steps of 256 columns of K
+    const float* bias;
+    void* Y;
+    int64_t ldy;
+    int tiles_m, tiles_n;
+};
+
+// acc += a b over 128 columns; BYTE: which byte of either scale register is a lane's block's
+template <int BYTE>
+__device__ __forceinline__ f32x4 mx_multiply(i32x4 a, i32x4 b, f32x4 acc, int scale_a, int scale_b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const i32x8 wa = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), wb = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, acc, 4, 4, BYTE, scale_a, BYTE, scale_b);
+#else
+    (void)a;
+    (void)b;
+    (void)scale_a;
+    (void)scale_b;
+    return acc;
+#endif
+}
+
+// A BM x BN tile (tokens x outputs) per workgroup, a ring of NBUF steps in LDS.  WIDE: offsets inside a tile take 64 bits.
+template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool WIDE = false>
+__global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm p) {
+    constexpr int NW = WAVES_M * WAVES_N, ROWS = BM + BN;
+    constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW, LPS = XL + WL;
+    constexpr int SL = ROWS / 64 / NW > 0 ? ROWS / 64 / NW : 1;       // requests of scales per wave, every second step
+    constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;
+    constexpr int STEP = ROWS * 128, SCALES = (ROWS / 64 > NW ? ROWS : NW * 64) * 16, SBUF = NBUF / 2 + 1;
+    static_assert(XL >= 1 && WL >= 1 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole requests per wave");
+    static_assert((ROWS / 64) % NW == 0 || ROWS / 64 < NW, "whole requests of scales");
+    static_assert(NBUF * (LPS + SL) < 64 && NBUF >= 2, "requests under way");
+    __shared__ __align__(1024) int8_t lds[NBUF * STEP + SBUF * SCALES];
+    const int tid = (int)threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+    int bm, bn;
+    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, &bm, &bn);
+    const int row0 = bm * BM, col0 = bn * BN;
+
+    // request u of a step: rows 8 (u NW + wave) + lane / 8 of the step's image, chunk slot lane % 8; first the rows of X, then those of W
+    const int piece = (lane & 7) ^ (lane >> 3);
+    const int8_t* xbase = reinterpret_cast<const int8_t*>(p.Xq) + (int64_t)row0 * p.ldx;
+    const int8_t* wbase = reinterpret_cast<const int8_t*>(p.Wq) + (int64_t)col0 * p.ldw;
+    typename std::conditional<WIDE, int64_t, unsigned>::type from[LPS];
+#pragma unroll
+    for (int u = 0; u < XL; ++u) {
+        int r = (u * NW + wave) * 8 + (lane >> 3);
+        r = row0 + r < p.M ? r : p.M - 1 - row0;
+        from[u] = (decltype(from[0] + 0))(r * p.ldx + piece * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < WL; ++u) {
+        int r = column_of<OUT>((u * NW + wave) * 8 + (lane >> 3));
+        r = col0 + r < p.N ? r : p.N - 1 - col0;
+        from[XL + u] = (decltype(from[0] + 0))(r * p.ldw + piece * 16);
+    }
+    // scales: row 64 (u NW + wave) + lane of the image (beyond its rows: the last one again)
+    const int8_t* scales_from[SL];
+#pragma unroll
+    for (int u = 0; u < SL; ++u) {
+        int r = (u * NW + wave) * 64 + lane;
+        r = r < ROWS ? r : ROWS - 1;
+        if (r < BM) {
+            r = row0 + r < p.M ? row0 + r : p.M - 1;
+            scales_from[u] = reinterpret_cast<const int8_t*>(p.Xs) + r * p.ldxs;
+        } else {
+            r = col0 + column_of<OUT>(r - BM);
+            r = r < p.N ? r : p.N - 1;
+            scales_from[u] = reinterpret_cast<const int8_t*>(p.Ws) + r * p.ldws;
+        }
+    }
+    const unsigned lds0 = lds_address(lds) + (unsigned)wave * 1024;
+    const bool cut = p.ldx < (int64_t)p.ksteps * 128 || p.ldw < (int64_t)p.ksteps * 128;   // a pitch that ends inside the last step
+    auto request = [&](int u, int kt, int buf) {
+        const unsigned to = lds0 + (unsigned)(buf * STEP + u * NW * 1024);
+        const int8_t* base = (u < XL ? xbase : wbase) + (int64_t)kt * 128;
+        if (cut && kt == p.ksteps - 1)
+            request_1k((int64_t)kt * 128 + piece * 16 < (u < XL ? p.ldx : p.ldw) ? base + from[u] : rows_zero_chunk, to);
+        else if constexpr (WIDE)
+            request_1k(base + from[u], to);
+        else
+            request_1k(base, from[u], to);
+    };
+    auto request_scales = [&](int kt) {                               // of steps kt and kt + 1, kt even
+#pragma unroll
+        for (int u = 0; u < SL; ++u)
+            request_1k(scales_from[u] + (int64_t)kt * 8, lds0 + (unsigned)(NBUF * STEP + (kt >> 1) % SBUF * SCALES + u * NW * 1024));
+    };
+
+    f32x4 acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int fr = lane & 15, fq = lane >> 4;
+    i32x4 xf[2][TM], wf[2][TN];
+    int xs[TM], ws[TN];
+    // fragment f of a half step: the token tiles first, then the weight tiles
+    auto read = [&](int f, int buf, int ks) {
+        const int slot = ((2 * fq + ks) ^ (fr & 7)) * 16;
+        if (f < TM)
+            xf[ks][f] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + (wm * (BM / WAVES_M) + fr) * 128 + slot + f * 2048);
+        else
+            wf[ks][f - TM] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + BM * 128 + (wn * (BN / WAVES_N) + fr) * 128 + slot +
+                                                             (f - TM) * 2048);
+    };
+    // scales of both halves of step kt
+    int next_xs[TM], next_ws[TN];
+    auto read_scales = [&](int f, int kt) {
+        const int8_t* at = lds + NBUF * STEP + (kt >> 1) % SBUF * SCALES + (kt & 1) * 8 + 2 * fq;
+        if (f < TM) next_xs[f] = *reinterpret_cast<const unsigned short*>(at + (wm * (BM / WAVES_M) + f * 16 + fr) * 16);
+        else next_ws[f - TM] = *reinterpret_cast<const unsigned short*>(at + (BM + wn * (BN / WAVES_N) + (f - TM) * 16 + fr) * 16);
+    };
+    auto take_scales = [&]() {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) xs[j] = next_xs[j];
+#pragma unroll
+        for (int i = 0; i < TN; ++i) ws[i] = next_ws[i];
+    };
+    auto multiply = [&](int i, auto half) {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) acc[i][j] = mx_multiply<half.value>(wf[half.value][i], xf[half.value][j], acc[i][j], ws[i], xs[j]);
+    };
+
+    // Step kt: its first half and its scales are in registers when it begins; the second is read while the first is multiplied.  Then comes
+    // the one barrier of a step: every wave's part of step kt + 1 has landed and every wave has read all of step kt, so that the requests of
+    // step kt + NBUF go into its buffer, NBUF - 1 whole steps ahead of their use.
+    constexpr int FR = TM + TN, FPR = (FR + TN - 1) / TN, RPR = (LPS + TN - 1) / TN;
+    const int steps = p.ksteps;
+#pragma unroll
+    for (int u = 0; u < NBUF; ++u)
+        if (u < steps) {
+            if (u % 2 == 0) request_scales(u);
+#pragma unroll
+            for (int f = 0; f < LPS; ++f) request(f, u, u);
+        }
+    // (the requests of the last step that may stay under way are counted without its scales, which come first: a wait too many at most)
+    if (steps >= NBUF) wait_requests<(NBUF - 1) * LPS>();
+    else wait_requests<0>();
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < FR; ++f) {
+        read(f, 0, 0);
+        read_scales(f, 0);
+    }
+    auto step = [&](int buf, int kt) {
+        take_scales();
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+#pragma unroll
+            for (int f = i * FPR; f < (i + 1) * FPR && f < FR; ++f) read(f, buf, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(i, std::integral_constant<int, 0>{});
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (kt + NBUF <= steps) wait_requests<(NBUF - 2) * LPS>();
+        else wait_requests<0>();
+        __syncthreads();
+        const bool more = kt + NBUF < steps, next = kt + 1 < steps;
+        if (more && ((kt + NBUF) & 1) == 0) request_scales(kt + NBUF);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            if (next) {
+#pragma unroll
+                for (int f = i * FPR; f < (i + 1) * FPR && f < FR; ++f) {
+                    read(f, (buf + 1) % NBUF, 0);
+                    read_scales(f, kt + 1);
+                }
+            }
+            if (more) {
+#pragma unroll
+                for (int u = i * RPR; u < (i + 1) * RPR && u < LPS; ++u) request(u, kt + NBUF, buf);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(i, std::integral_constant<int, 1>{});
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (int kt = 0; kt < steps; kt += NBUF) {
+#pragma unroll
+        for (int u = 0; u < NBUF; ++u)
+            if (kt + u < steps) step(u, kt + u);
+    }
+
+    // NV accumulator tiles make 16 bytes of a token's outputs
+    constexpr int NV = OUT == Elem::f32 ? 1 : 2;
+    const int n0 = col0 + wn * (BN / WAVES_N) + fq * 4 * NV, m0 = row0 + wm * (BM / WAVES_M) + fr;
+    f32x4 bias[TN];
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+        bias[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (p.bias) bias[i] = four_of(p.bias, n0 + (i / NV) * 16 * NV + (i % NV) * 4, p.N);
+    }
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        const int m = m0 + j * 16;
+        if (m >= p.M) continue;
+        elem_t<OUT>* y = static_cast<elem_t<OUT>*>(p.Y) + (int64_t)m * p.ldy + n0;
+#pragma unroll
+        for (int i = 0; i < TN; i += NV) {
+            elem_t<OUT> v[4 * NV];
+#pragma unroll
+            for (int q = 0; q < NV; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * q + e] = float_to_elem<OUT>(acc[i + q][j][e] + bias[i + q][e]);
+            if (n0 + i * 16 + 4 * NV <= p.N) {
+                store_piece<OUT>(y + i * 16, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4 * NV; ++e)
+                    if (n0 + i * 16 + e < p.N) y[i * 16 + e] = v[e];
+            }
+        }
+    }
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool WIDE = false>
+static hipError_t run_mx_tile(MxGemm p, hipStream_t stream) {
+    p.tiles_m = (int)ceil_div(p.M, BM);
+    p.tiles_n = (int)ceil_div(p.N, BN);
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
+    if (total > 0x7FFFFFFF || p.ksteps < 1) return hipErrorInvalidValue;
+    return launch_kernel(kTimeGemm, mx_tile_kernel<BM, BN, WAVES_M, WAVES_N, NBUF, OUT, WIDE>, dim3((unsigned)total),
+                         dim3(WAVES_M * WAVES_N * 64), 0, stream, p);
+}
+
+// Few tokens: 16 XT tokens and 16 WT outputs per workgroup, the steps of K dealt over its NW waves, whose sums meet in LDS in the order of
+// the waves.  Each weight is used once, so codes and scales go from memory straight to the lanes that multiply them.
+// IN: the tokens' codes in memory (int), or rows of X of that type, which every workgroup puts on their grids itself, a block per
+// lane (a block's grid is its own affair: nothing waits for a row); the workgroups share the writing of codes and scales.
+struct Codes {};
+template <Elem T>
+struct RowsOf {
+    static constexpr Elem type = T;
+};
+
+template <int XT, int WT, int NW, Elem OUT, typename IN>
+__global__ __launch_bounds__(NW * 64) void mx_few_kernel(MxGemm p, MxRows rows) {
+    constexpr bool GIVEN = std::is_same<IN, Codes>::value;
+    __shared__ __align__(16) float sums[NW][XT * 16][WT * 16 + 4];
+    const int tid = (int)threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col0 = (int)(blockIdx.x % (unsigned)p.tiles_n) * (WT * 16), row0 = (int)(blockIdx.x / (unsigned)p.tiles_n) * (XT * 16);
+    f32x4 acc[WT][XT];
+#pragma unroll
+    for (int i = 0; i < WT; ++i)
+#pragma unroll
+        for (int j = 0; j < XT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint8_t* w[WT];
+    const uint8_t* ws[WT];
+#pragma unroll
+    for (int i = 0; i < WT; ++i) {
+        int n = col0 + i * 16 + fr;
+        n = n < p.N ? n : p.N - 1;
+        w[i] = p.Wq + n * p.ldw + 32 * fq;
+        ws[i] = p.Ws + n * p.ldws + 2 * fq;
+    }
+    const uint8_t* x[XT];
+    const uint8_t* xs[XT];
+    int m[XT];
+#pragma unroll
+    for (int j = 0; j < XT; ++j) {
+        m[j] = row0 + j * 16 + fr;
+        const int r = m[j] < p.M ? m[j] : p.M - 1;
+        x[j] = p.Xq + r * p.ldx + 32 * fq;
+        xs[j] = p.Xs + r * p.ldxs + 2 * fq;
+    }
+    for (int kt = wave; kt < p.ksteps; kt += NW) {
+        const int64_t k = (int64_t)kt * 128;
+        i32x4 wf[2][WT], xf[2][XT];
+        int wscale[WT], xscale[XT];
+        auto chunk = [&](const uint8_t* at, int half, int64_t ld) {
+            i32x4 r = {0, 0, 0, 0};
+            if (k + 32 * fq + 16 * half < ld) r = *reinterpret_cast<const i32x4*>(at + k + 16 * half);
+            return r;
+        };
+#pragma unroll
+        for (int i = 0; i < WT; ++i) {
+            wscale[i] = *reinterpret_cast<const unsigned short*>(ws[i] + kt * 8);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wf[h][i] = chunk(w[i], h, p.ldw);
+        }
+#pragma unroll
+        for (int j = 0; j < XT; ++j) {
+            if constexpr (GIVEN) {
+                xscale[j] = *reinterpret_cast<const unsigned short*>(xs[j] + kt * 8);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) xf[h][j] = chunk(x[j], h, p.ldx);
+            } else {
+                xscale[j] = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int block = kt * 8 + 2 * fq + h;
+                    const bool there = m[j] < p.M && (int64_t)block * kMxBlock < (int64_t)(rows.C + rows.s) * rows.g;
+                    i32x4 codes = {0, 0, 0, 0};
+                    unsigned byte = 0;
+                    if (there) {
+                        const elem_t<IN::type>* from = static_cast<const elem_t<IN::type>*>(rows.X) + m[j] * rows.ldx;
+                        float v[4][8];
+                        unsigned big = 0;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int k0 = block * kMxBlock + 8 * q;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[q][e] = 0.0f;
+                            if (k0 < (rows.C + rows.s) * rows.g) mx_expanded8<IN::type, false>(rows, from, k0, v[q]);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) big = mx_magnitude(v[q][e]) > big ? mx_magnitude(v[q][e]) : big;
+                        byte = mx_scale_byte(big);
+                        if (byte != 255u) {
+                            const float scale = mx_scale_value(byte);
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) codes[q] = (int)mx_codes8(v[q], scale);
+                        }
+                    }
+                    xf[h][j] = codes;
+                    xscale[j] |= (int)(byte << (8 * h));
+                    if (m[j] < p.M && (unsigned)(block + m[j]) % gridDim.x == blockIdx.x) {
+                        if ((int64_t)block * 16 < rows.ldq) *reinterpret_cast<i32x4*>(rows.q + m[j] * rows.ldq + (int64_t)block * 16) = codes;
+                        if (block < rows.lds) rows.scale[m[j] * rows.lds + block] = (uint8_t)byte;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < WT; ++i)
+#pragma unroll
+            for (int j = 0; j < XT; ++j) {
+                acc[i][j] = mx_multiply<0>(wf[0][i], xf[0][j], acc[i][j], wscale[i], xscale[j]);
+                acc[i][j] = mx_multiply<1>(wf[1][i], xf[1][j], acc[i][j], wscale[i], xscale[j]);
+            }
+    }
+    if constexpr (!GIVEN) {                                   // the padding behind the last step
+        for (int64_t o = blockIdx.x * (int64_t)(NW * 64) + tid, per = rows.ldq / 16 + rows.lds; o < p.M * per; o += gridDim.x * (int64_t)(NW * 64)) {
+            const int64_t r = o / per, at = o - r * per;
+            if (at < rows.ldq / 16) {
+                if (at >= p.ksteps * 8) *reinterpret_cast<i32x4*>(rows.q + r * rows.ldq + at * 16) = i32x4{0, 0, 0, 0};
+            } else if (at - rows.ldq / 16 >= p.ksteps * 8) {
+                rows.scale[r * rows.lds + at - rows.ldq / 16] = 0;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < WT; ++i)
+#pragma unroll
+        for (int j = 0; j < XT; ++j) *reinterpret_cast<f32x4*>(&sums[wave][j * 16 + fr][i * 16 + fq * 4]) = acc[i][j];
+    __syncthreads();
+    for (int o = tid; o < XT * 16 * WT * 16; o += NW * 64) {
+        const int t = o / (WT * 16), c = o % (WT * 16), mm = row0 + t, n = col0 + c;
+        if (mm >= p.M || n >= p.N) continue;
+        float v = sums[0][t][c];
+#pragma unroll
+        for (int q = 1; q < NW; ++q) v += sums[q][t][c];
+        if (p.bias) v += p.bias[n];
+        static_cast<elem_t<OUT>*>(p.Y)[(int64_t)mm * p.ldy + n] = float_to_elem<OUT>(v);
+    }
+}
+
+template <int XT, int WT, int NW, Elem OUT, typename IN>
+static hipError_t run_mx_few(MxGemm p, const MxRows& rows, hipStream_t stream) {
+    p.tiles_m = (int)ceil_div(p.M, XT * 16);
+    p.tiles_n = (int)ceil_div(p.N, WT * 16);
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
+    if (total > 0x7FFFFFFF || p.ksteps < 1) return hipErrorInvalidValue;
+    return launch_kernel(kTimeGemm, mx_few_kernel<XT, WT, NW, OUT, IN>, dim3((unsigned)total), dim3(NW * 64), 0, stream, p, rows);
+}
+
+template <Elem OUT>
+static hipError_t run_mx_gemm(const MxGemm& p, hipStream_t stream) {
+    if (p.ldx >= kWidePitch || p.ldw >= kWidePitch) return run_mx_tile<64, 64, 2, 2, 4, OUT, true>(p, stream);
+    const int64_t cus = compute_units();
+    if (p.M <= 16) return run_mx_few<1, 1, 8, OUT, Codes>(p, MxRows{}, stream);
+    if (p.M <= 32) return run_mx_few<2, 1, 8, OUT, Codes>(p, MxRows{}, stream);
+    if (ceil_div(p.M, 64) * ceil_div(p.N, 16) <= cus) return run_mx_few<4, 1, 8, OUT, Codes>(p, MxRows{}, stream);
+    if (ceil_div(p.M, 64) * ceil_div(p.N, 64) <= 2 * cus) return run_mx_tile<64, 64, 2, 2, 4, OUT>(p, stream);
+    if (ceil_div(p.M, 128) * ceil_div(p.N, 128) <= 2 * cus) return run_mx_tile<128, 128, 2, 4, 3, OUT>(p, stream);
+    return run_mx_tile<256, 256, 2, 4, 2, OUT>(p, stream);
+}
+
+// Outputs by the launch, as in the int8 product: as a rule all of them.
+template <Elem OUT>
+static hipError_t run_mx_ranges(const MxGemm& p, int64_t M, int64_t N, hipStream_t stream) {
+    constexpr int64_t kMostRows = (int64_t)1 << 28, kMostColumns = (int64_t)1 << 26, kMostOutputs = (int64_t)1 << 35;
+    for (int64_t n0 = 0; n0 < N; n0 += kMostColumns) {
+        const int64_t cols = N - n0 < kMostColumns ? N - n0 : kMostColumns;
+        const int64_t most = kMostOutputs / cols < kMostRows ? kMostOutputs / cols : kMostRows;
+        for (int64_t m0 = 0; m0 < M; m0 += most) {
+            MxGemm q = p;
+            q.M = (int)(M - m0 < most ? M - m0 : most);
+            q.N = (int)cols;
+            q.Xq += m0 * p.ldx;
+            q.Xs += m0 * p.ldxs;
+            q.Wq += n0 * p.ldw;
+            q.Ws += n0 * p.ldws;
+            if (p.bias) q.bias += n0;
+            q.Y = static_cast<elem_t<OUT>*>(p.Y) + m0 * p.ldy + n0;
+            const hipError_t e = run_mx_gemm<OUT>(q, stream);
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_qgemm_mx(const uint8_t* Xq, int64_t ldx, const uint8_t* Xs, int64_t ldxs, const uint8_t* Wq, int64_t ldw,
+                           const uint8_t* Ws, int64_t ldws, int64_t M, int64_t N, int64_t Kexp, const float* bias, void* Y, int out_type,
+                           int64_t ldy, hipStream_t stream) {
+    const MxGemm p{Xq, ldx, Xs, ldxs, Wq, ldw, Ws, ldws, 0, 0, (int)ceil_div(Kexp, 256), bias, Y, ldy, 0, 0};
+    switch (static_cast<Elem>(out_type)) {
+        case Elem::f32: return run_mx_ranges<Elem::f32>(p, M, N, stream);
+        case Elem::bf16: return run_mx_ranges<Elem::bf16>(p, M, N, stream);
+        case Elem::f16: return run_mx_ranges<Elem::f16>(p, M, N, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+template <Elem OUT, typename IN>
+static hipError_t run_forward_mx(const MxGemm& p, const MxRows& rows, hipStream_t stream) {
+    return run_mx_few<1, 1, 8, OUT, IN>(p, rows, stream);
+}
+
+template <Elem OUT>
+static hipError_t run_forward_mx_of(const MxGemm& p, const MxRows& rows, int type, hipStream_t stream) {
+    switch (static_cast<Elem>(type)) {
+        case Elem::f32: return run_forward_mx<OUT, RowsOf<Elem::f32>>(p, rows, stream);
+        case Elem::bf16: return run_forward_mx<OUT, RowsOf<Elem::bf16>>(p, rows, stream);
+        case Elem::f16: return run_forward_mx<OUT, RowsOf<Elem::f16>>(p, rows, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_forward_mx(const void* X, int type, int64_t ldx, int64_t M, int C, int g, int s, const int32_t* chan_src, uint8_t* Xq,
+                             int64_t ldq, uint8_t* Xs, int64_t ldxs, const uint8_t* Wq, int64_t ldw, const uint8_t* Ws, int64_t ldws,
+                             int64_t N, const float* bias, void* Y, int out_type, int64_t ldy, bool apart, hipStream_t stream) {
+    const int64_t Kexp = (int64_t)(C + s) * g;
+    if (apart && M <= 16 && N <= (int64_t)1 << 26) {              // (one launch reads X and W while outputs are being written)
+        const MxGemm p{Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, (int)M, (int)N, (int)ceil_div(Kexp, 256), bias, Y, ldy, 0, 0};
+        const MxRows rows{X, ldx, M, C, g, s, chan_src, nullptr, Xq, ldq, Xs, ldxs};
+        switch (static_cast<Elem>(out_type)) {
+            case Elem::f32: return run_forward_mx_of<Elem::f32>(p, rows, type, stream);
+            case Elem::bf16: return run_forward_mx_of<Elem::bf16>(p, rows, type, stream);
+            case Elem::f16: return run_forward_mx_of<Elem::f16>(p, rows, type, stream);
+        }
+    }
+    const hipError_t e = launch_mx_quantize(X, type, ldx, M, C, g, s, chan_src, nullptr, Xq, ldq, Xs, ldxs, stream);
+    if (e != hipSuccess) return e;
+    return launch_qgemm_mx(Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, M, N, Kexp, bias, Y, out_type, ldy, stream);
+}
+
+}  // namespace ocs

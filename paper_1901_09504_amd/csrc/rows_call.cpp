@@ -1,5 +1,5 @@
-// The Python side of the calls with a grid per row and of token scoring: marshalling only, as binding.py does for the other calls through
-// ctypes.  These four are made once or twice per generated token, on work of 2 to 6 us, and a ctypes call of 20 arguments costs the host
+// The Python side of the calls with a grid per row or per block, of the quantized cache and of token scoring: marshalling only, as binding.py
+// does for the other calls through ctypes.  These are made once or twice per layer and generated token, on work of 2 to 6 us, and a ctypes call of 20 arguments costs the host
 // 1.9 to 2.7 us beside the 3.2 of a launch; this takes the tensors as they are and costs 0.6 to 1.0.
 //
 // bind(float32, bfloat16, float16, current_device, current_raw_stream) comes first.  A tensor argument may be None (NULL), or False as
@@ -173,6 +173,160 @@ static PyObject* forward_rows(PyObject*, PyObject* const* args, Py_ssize_t given
     });
 }
 
+static PyObject* split_quantize_mx(PyObject*, PyObject* const* args, Py_ssize_t given) {
+    Args a(args, given, 13);
+    const int type = a.type();
+    const void* X = a.tensor();
+    const int64_t M = a.int64();
+    const int C = a.int32(), g = a.int32();
+    const int64_t ldx = a.int64();
+    const int32_t* src = a.tensor_of<int32_t>();
+    const int32_t* depth = a.tensor_of<int32_t>();
+    const int s = a.int32();
+    uint8_t* q = a.tensor_of<uint8_t>();
+    const int64_t ldq = a.int64();
+    uint8_t* scales = a.tensor_of<uint8_t>();
+    const int64_t lds = a.int64();
+    void* stream = a.stream();
+    return answer(a, [&] { return ocs_split_quantize_mx(X, type, M, C, g, ldx, src, depth, s, q, ldq, scales, lds, stream); });
+}
+
+static PyObject* dequantize_mx(PyObject*, PyObject* const* args, Py_ssize_t given) {
+    Args a(args, given, 9);
+    const uint8_t* q = a.tensor_of<uint8_t>();
+    const int64_t ldq = a.int64();
+    const uint8_t* scales = a.tensor_of<uint8_t>();
+    const int64_t lds = a.int64(), M = a.int64(), cols = a.int64();
+    const int type = a.type();
+    void* Y = a.tensor();
+    const int64_t ldy = a.int64();
+    void* stream = a.stream();
+    return answer(a, [&] { return ocs_dequantize_mx(q, ldq, scales, lds, M, cols, Y, type, ldy, stream); });
+}
+
+static PyObject* qgemm_mx(PyObject*, PyObject* const* args, Py_ssize_t given) {
+    Args a(args, given, 15);
+    const uint8_t* Xq = a.tensor_of<uint8_t>();
+    const int64_t ldx = a.int64();
+    const uint8_t* Xs = a.tensor_of<uint8_t>();
+    const int64_t ldxs = a.int64();
+    const uint8_t* Wq = a.tensor_of<uint8_t>();
+    const int64_t ldw = a.int64();
+    const uint8_t* Ws = a.tensor_of<uint8_t>();
+    const int64_t ldws = a.int64(), M = a.int64(), N = a.int64(), K = a.int64();
+    const float* bias = a.tensor_of<float>();
+    const int type = a.type();
+    void* Y = a.tensor();
+    const int64_t ldy = a.int64();
+    void* stream = a.stream();
+    return answer(a, [&] { return ocs_qgemm_mx(Xq, ldx, Xs, ldxs, Wq, ldw, Ws, ldws, M, N, K, bias, Y, type, ldy, stream); });
+}
+
+static PyObject* forward_mx(PyObject*, PyObject* const* args, Py_ssize_t given) {
+    Args a(args, given, 20);
+    const int type = a.type();
+    const void* X = a.tensor();
+    const int64_t M = a.int64();
+    const int C = a.int32(), g = a.int32();
+    const int64_t ldx = a.int64();
+    const int32_t* src = a.tensor_of<int32_t>();
+    const int s = a.int32();
+    uint8_t* Xq = a.tensor_of<uint8_t>();
+    const int64_t ldq = a.int64();
+    uint8_t* Xs = a.tensor_of<uint8_t>();
+    const int64_t ldxs = a.int64();
+    const uint8_t* Wq = a.tensor_of<uint8_t>();
+    const int64_t ldw = a.int64();
+    const uint8_t* Ws = a.tensor_of<uint8_t>();
+    const int64_t ldws = a.int64(), N = a.int64();
+    const float* bias = a.tensor_of<float>();
+    const int out = a.type();
+    void* Y = a.tensor();
+    const int64_t ldy = a.int64();
+    void* stream = a.stream();
+    return answer(a, [&] {
+        return ocs_forward_mx(X, type, M, C, g, ldx, src, s, Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, N, bias, Y, out, ldy, stream);
+    });
+}
+
+// the pool and its pages, as every call of the cache takes them
+struct Pool {
+    const int32_t* table;
+    int64_t cols, ldt;
+    int format;
+    void *keys, *kscales, *values, *vscales;
+    int64_t pages;
+    int P, H, D;
+    const int32_t *kdepth, *vdepth;
+    explicit Pool(Args& a) {
+        table = a.tensor_of<int32_t>();
+        cols = a.int64();
+        ldt = a.int64();
+        format = a.int32();
+        keys = a.tensor();
+        kscales = a.tensor();
+        values = a.tensor();
+        vscales = a.tensor();
+        pages = a.int64();
+        P = a.int32();
+        H = a.int32();
+        D = a.int32();
+        kdepth = a.tensor_of<int32_t>();
+        vdepth = a.tensor_of<int32_t>();
+    }
+};
+
+template <typename F>
+static PyObject* cache_rows(PyObject* const* args, Py_ssize_t given, F call) {
+    Args a(args, given, 25);
+    const int type = a.type();
+    void* K = a.tensor();
+    const int64_t ldk = a.int64(), hdk = a.int64();
+    const int same = a.type();
+    void* V = a.tensor();
+    const int64_t ldv = a.int64(), hdv = a.int64(), T = a.int64();
+    const int32_t* cu = a.tensor_of<int32_t>();
+    const int32_t* starts = a.tensor_of<int32_t>();
+    const int64_t B = a.int64();
+    const Pool c(a);
+    void* stream = a.stream();
+    return answer(a, [&] {
+        return call(K, ldk, hdk, V, ldv, hdv, same == type ? type : -1, T, cu, starts, B, c.table, c.cols, c.ldt, c.format, c.keys, c.kscales,
+                    c.values, c.vscales, c.pages, c.P, c.H, c.D, c.kdepth, c.vdepth, stream);
+    });
+}
+
+static PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t given) { return cache_rows(args, given, ocs_cache_write); }
+
+static PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t given) { return cache_rows(args, given, ocs_cache_read); }
+
+static PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t given) {
+    Args a(args, given, 31);
+    const int type = a.type();
+    const void* Q = a.tensor();
+    const int64_t ldq = a.int64(), hdq = a.int64();
+    const int Hq = a.int32();
+    const int64_t T = a.int64();
+    const int32_t* cu = a.tensor_of<int32_t>();
+    const int32_t* starts = a.tensor_of<int32_t>();
+    const int64_t B = a.int64(), most = a.int64();
+    const Pool c(a);
+    const float scale = a.number();
+    const int64_t window = a.int64();
+    const int same = a.type();
+    void* Y = a.tensor();
+    const int64_t ldy = a.int64(), hdy = a.int64();
+    float* lse = a.tensor_of<float>();
+    const size_t bytes = a.nbytes();
+    void* workspace = a.tensor();
+    void* stream = a.stream();
+    return answer(a, [&] {
+        return ocs_cache_attention(Q, same == type ? type : -1, ldq, hdq, Hq, T, cu, starts, B, most, c.table, c.cols, c.ldt, c.format, c.keys,
+                                   c.kscales, c.values, c.vscales, c.pages, c.P, c.H, c.D, c.kdepth, c.vdepth, scale, window, Y, ldy, hdy, lse,
+                                   workspace, bytes, stream);
+    });
+}
+
 static PyObject* token_logprobs(PyObject*, PyObject* const* args, Py_ssize_t given) {
     Args a(args, given, 12);
     const int type = a.type();
@@ -206,8 +360,10 @@ static PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t given) {
 }
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-static PyMethodDef methods[] = {METHOD(bind),         METHOD(split_quantize_rows), METHOD(qgemm_rows),
-                                METHOD(forward_rows), METHOD(token_logprobs),      {nullptr, nullptr, 0, nullptr}};
+static PyMethodDef methods[] = {METHOD(bind),         METHOD(split_quantize_rows), METHOD(qgemm_rows),  METHOD(forward_rows),
+                                METHOD(split_quantize_mx), METHOD(dequantize_mx),  METHOD(qgemm_mx),    METHOD(forward_mx),
+                                METHOD(cache_write),  METHOD(cache_read),          METHOD(cache_attention), METHOD(token_logprobs),
+                                {nullptr, nullptr, 0, nullptr}};
 static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rows_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 PyMODINIT_FUNC PyInit__rows_call(void) {
