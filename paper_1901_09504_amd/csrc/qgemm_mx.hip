@@ -30,12 +30,12 @@ struct MxGemm {
     int tiles_m, tiles_n;
 };
 
-// acc += a b over 128 columns; BYTE: which byte of either scale register is a lane's block's
-template <int BYTE>
+// acc += a b over 128 columns; which byte of either scale register is a lane's block's
+template <int BYTE_A, int BYTE_B>
 __device__ __forceinline__ f32x4 mx_multiply(i32x4 a, i32x4 b, f32x4 acc, int scale_a, int scale_b) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const i32x8 wa = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), wb = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, acc, 4, 4, BYTE, scale_a, BYTE, scale_b);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, acc, 4, 4, BYTE_A, scale_a, BYTE_B, scale_b);
 #else
     (void)a;
     (void)b;
@@ -45,16 +45,16 @@ __device__ __forceinline__ f32x4 mx_multiply(i32x4 a, i32x4 b, f32x4 acc, int sc
 #endif
 }
 
-// A BM x BN tile (tokens x outputs) per workgroup, a ring of NBUF steps in LDS.  WIDE: offsets inside a tile take 64 bits.
-template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool WIDE = false>
+// A BM x BN tile (tokens x outputs) per workgroup, a ring of NBUF steps in LDS.
+// ANY: pitches that are no multiples of 128, or so long that offsets inside a tile take 64 bits.
+template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool ANY = false>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm p) {
     constexpr int NW = WAVES_M * WAVES_N, ROWS = BM + BN;
     constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW, LPS = XL + WL;
-    constexpr int SL = ROWS / 64 / NW > 0 ? ROWS / 64 / NW : 1;       // requests of scales per wave, every second step
+    constexpr int SL = (ROWS + 64 * NW - 1) / (64 * NW);              // requests of scales per wave, every second step
     constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;
-    constexpr int STEP = ROWS * 128, SCALES = (ROWS / 64 > NW ? ROWS : NW * 64) * 16, SBUF = NBUF / 2 + 1;
+    constexpr int STEP = ROWS * 128, SCALES = SL * NW * 1024, SBUF = NBUF / 2 + 1;
     static_assert(XL >= 1 && WL >= 1 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole requests per wave");
-    static_assert((ROWS / 64) % NW == 0 || ROWS / 64 < NW, "whole requests of scales");
     static_assert(NBUF * (LPS + SL) < 64 && NBUF >= 2, "requests under way");
     __shared__ __align__(1024) int8_t lds[NBUF * STEP + SBUF * SCALES];
     const int tid = (int)threadIdx.x, lane = tid & 63;
@@ -65,10 +65,11 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm 
     const int row0 = bm * BM, col0 = bn * BN;
 
     // request u of a step: rows 8 (u NW + wave) + lane / 8 of the step's image, chunk slot lane % 8; first the rows of X, then those of W
-    const int piece = (lane & 7) ^ (lane >> 3);
+    // (slot 4 h + q of a row holds chunk 2 q + h: at any time the matrix cores' reads are of neighbouring slots, in different banks)
+    const int slot_of_row = (lane & 7) ^ (lane >> 3), piece = (slot_of_row & 3) * 2 + (slot_of_row >> 2);
     const int8_t* xbase = reinterpret_cast<const int8_t*>(p.Xq) + (int64_t)row0 * p.ldx;
     const int8_t* wbase = reinterpret_cast<const int8_t*>(p.Wq) + (int64_t)col0 * p.ldw;
-    typename std::conditional<WIDE, int64_t, unsigned>::type from[LPS];
+    typename std::conditional<ANY, int64_t, unsigned>::type from[LPS];
 #pragma unroll
     for (int u = 0; u < XL; ++u) {
         int r = (u * NW + wave) * 8 + (lane >> 3);
@@ -97,16 +98,19 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm 
         }
     }
     const unsigned lds0 = lds_address(lds) + (unsigned)wave * 1024;
-    const bool cut = p.ldx < (int64_t)p.ksteps * 128 || p.ldw < (int64_t)p.ksteps * 128;   // a pitch that ends inside the last step
     auto request = [&](int u, int kt, int buf) {
-        const unsigned to = lds0 + (unsigned)(buf * STEP + u * NW * 1024);
+        const int at = buf * STEP + u * NW * 1024;
         const int8_t* base = (u < XL ? xbase : wbase) + (int64_t)kt * 128;
-        if (cut && kt == p.ksteps - 1)
-            request_1k((int64_t)kt * 128 + piece * 16 < (u < XL ? p.ldx : p.ldw) ? base + from[u] : rows_zero_chunk, to);
-        else if constexpr (WIDE)
-            request_1k(base + from[u], to);
-        else
-            request_1k(base, from[u], to);
+        if constexpr (ANY) {
+            // A pitch that ends inside the last step: the lanes whose chunks are not there write zeros themselves.  (Every request has lanes
+            // whose chunks are, so that requests under way can be counted.)
+            if ((int64_t)kt * 128 + piece * 16 >= (u < XL ? p.ldx : p.ldw))
+                *reinterpret_cast<i32x4*>(lds + at + wave * 1024 + lane * 16) = i32x4{0, 0, 0, 0};
+            else
+                request_1k(base + from[u], lds0 + (unsigned)at);
+        } else {
+            request_1k(base, from[u], lds0 + (unsigned)at);
+        }
     };
     auto request_scales = [&](int kt) {                               // of steps kt and kt + 1, kt even
 #pragma unroll
@@ -120,39 +124,33 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm 
 #pragma unroll
         for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int fr = lane & 15, fq = lane >> 4;
-    i32x4 xf[2][TM], wf[2][TN];
-    int xs[TM], ws[TN];
-    // fragment f of a half step: the token tiles first, then the weight tiles
-    auto read = [&](int f, int buf, int ks) {
-        const int slot = ((2 * fq + ks) ^ (fr & 7)) * 16;
-        if (f < TM)
-            xf[ks][f] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + (wm * (BM / WAVES_M) + fr) * 128 + slot + f * 2048);
-        else
-            wf[ks][f - TM] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + BM * 128 + (wn * (BN / WAVES_N) + fr) * 128 + slot +
-                                                             (f - TM) * 2048);
+    i32x4 xf[2][TM], wf[TN];                                          // (the weights' of the next half take the place of those just multiplied)
+    int xs[TM], next_xs[TM], ws[TN];                                  // scales of both halves of a step
+    auto read_x = [&](int j, int buf, int ks) {
+        const int slot = ((4 * ks + fq) ^ (fr & 7)) * 16;
+        xf[ks][j] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + (wm * (BM / WAVES_M) + fr) * 128 + slot + j * 2048);
     };
-    // scales of both halves of step kt
-    int next_xs[TM], next_ws[TN];
-    auto read_scales = [&](int f, int kt) {
-        const int8_t* at = lds + NBUF * STEP + (kt >> 1) % SBUF * SCALES + (kt & 1) * 8 + 2 * fq;
-        if (f < TM) next_xs[f] = *reinterpret_cast<const unsigned short*>(at + (wm * (BM / WAVES_M) + f * 16 + fr) * 16);
-        else next_ws[f - TM] = *reinterpret_cast<const unsigned short*>(at + (BM + wn * (BN / WAVES_N) + (f - TM) * 16 + fr) * 16);
+    auto read_w = [&](int i, int buf, int ks) {
+        const int slot = ((4 * ks + fq) ^ (fr & 7)) * 16;
+        wf[i] = *reinterpret_cast<const i32x4*>(lds + buf * STEP + BM * 128 + (wn * (BN / WAVES_N) + fr) * 128 + slot + i * 2048);
     };
-    auto take_scales = [&]() {
-#pragma unroll
-        for (int j = 0; j < TM; ++j) xs[j] = next_xs[j];
-#pragma unroll
-        for (int i = 0; i < TN; ++i) ws[i] = next_ws[i];
-    };
+    const int8_t* xs_at = lds + NBUF * STEP + (wm * (BM / WAVES_M) + fr) * 16 + 2 * fq;
+    const int8_t* ws_at = lds + NBUF * STEP + (BM + wn * (BN / WAVES_N) + fr) * 16 + 2 * fq;
+    auto scales_of = [&](int kt) { return (kt >> 1) % SBUF * SCALES + (kt & 1) * 8; };
+    auto read_xs = [&](int j, int step_at) { next_xs[j] = *reinterpret_cast<const unsigned short*>(xs_at + step_at + j * 256); };
+    auto read_ws = [&](int i, int step_at) { ws[i] = *reinterpret_cast<const unsigned short*>(ws_at + step_at + i * 256); };
     auto multiply = [&](int i, auto half) {
 #pragma unroll
-        for (int j = 0; j < TM; ++j) acc[i][j] = mx_multiply<half.value>(wf[half.value][i], xf[half.value][j], acc[i][j], ws[i], xs[j]);
+        for (int j = 0; j < TM; ++j) acc[i][j] = mx_multiply<half.value, half.value>(wf[i], xf[half.value][j], acc[i][j], ws[i], xs[j]);
+        // here and not later: the compiler would deal these products over the whole step, and the operands into scratch memory
+#pragma unroll
+        for (int j = 0; j < TM; ++j) asm volatile("" : "+v"(acc[i][j]));
     };
 
     // Step kt: its first half and its scales are in registers when it begins; the second is read while the first is multiplied.  Then comes
     // the one barrier of a step: every wave's part of step kt + 1 has landed and every wave has read all of step kt, so that the requests of
     // step kt + NBUF go into its buffer, NBUF - 1 whole steps ahead of their use.
-    constexpr int FR = TM + TN, FPR = (FR + TN - 1) / TN, RPR = (LPS + TN - 1) / TN;
+    constexpr int XPR = (TM + TN - 1) / TN, RPR = (LPS + TN - 1) / TN;
     const int steps = p.ksteps;
 #pragma unroll
     for (int u = 0; u < NBUF; ++u)
@@ -166,32 +164,44 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm 
     else wait_requests<0>();
     __syncthreads();
 #pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        read(f, 0, 0);
-        read_scales(f, 0);
+    for (int j = 0; j < TM; ++j) {
+        read_x(j, 0, 0);
+        read_xs(j, 0);
     }
-    auto step = [&](int buf, int kt) {
-        take_scales();
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+        read_w(i, 0, 0);
+        read_ws(i, 0);
+    }
+    // MORE: there is a step kt + NBUF, and so kt + 1 (known in the loop over whole rings, looked up behind it)
+    auto step = [&](int buf, int kt, auto known) {
+        constexpr bool KNOWN = decltype(known)::value;
+        const bool more = KNOWN || kt + NBUF < steps, next = KNOWN || kt + 1 < steps;
+#pragma unroll
+        for (int j = 0; j < TM; ++j) xs[j] = next_xs[j];
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
 #pragma unroll
-            for (int f = i * FPR; f < (i + 1) * FPR && f < FR; ++f) read(f, buf, 1);
+            for (int j = i * XPR; j < (i + 1) * XPR && j < TM; ++j) read_x(j, buf, 1);
             __builtin_amdgcn_sched_barrier(0);
             multiply(i, std::integral_constant<int, 0>{});
             __builtin_amdgcn_sched_barrier(0);
+            read_w(i, buf, 1);
         }
-        if (kt + NBUF <= steps) wait_requests<(NBUF - 2) * LPS>();
+        // every read of this step's buffer has returned
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+        if (KNOWN || kt + NBUF <= steps) wait_requests<(NBUF - 2) * LPS>();
         else wait_requests<0>();
         __syncthreads();
-        const bool more = kt + NBUF < steps, next = kt + 1 < steps;
         if (more && ((kt + NBUF) & 1) == 0) request_scales(kt + NBUF);
+        const int next_at = scales_of(kt + 1);
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
             if (next) {
 #pragma unroll
-                for (int f = i * FPR; f < (i + 1) * FPR && f < FR; ++f) {
-                    read(f, (buf + 1) % NBUF, 0);
-                    read_scales(f, kt + 1);
+                for (int j = i * XPR; j < (i + 1) * XPR && j < TM; ++j) {
+                    read_x(j, (buf + 1) % NBUF, 0);
+                    read_xs(j, next_at);
                 }
             }
             if (more) {
@@ -201,12 +211,21 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm 
             __builtin_amdgcn_sched_barrier(0);
             multiply(i, std::integral_constant<int, 1>{});
             __builtin_amdgcn_sched_barrier(0);
+            if (next) {
+                read_w(i, (buf + 1) % NBUF, 0);
+                read_ws(i, next_at);
+            }
         }
     };
-    for (int kt = 0; kt < steps; kt += NBUF) {
+    int kt = 0;
+    for (; kt + 2 * NBUF <= steps; kt += NBUF) {
+#pragma unroll
+        for (int u = 0; u < NBUF; ++u) step(u, kt + u, std::true_type{});
+    }
+    for (; kt < steps; kt += NBUF) {
 #pragma unroll
         for (int u = 0; u < NBUF; ++u)
-            if (kt + u < steps) step(u, kt + u);
+            if (kt + u < steps) step(u, kt + u, std::false_type{});
     }
 
     // NV accumulator tiles make 16 bytes of a token's outputs
@@ -241,13 +260,13 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void mx_tile_kernel(MxGemm 
     }
 }
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool WIDE = false>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int NBUF, Elem OUT, bool ANY = false>
 static hipError_t run_mx_tile(MxGemm p, hipStream_t stream) {
     p.tiles_m = (int)ceil_div(p.M, BM);
     p.tiles_n = (int)ceil_div(p.N, BN);
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
     if (total > 0x7FFFFFFF || p.ksteps < 1) return hipErrorInvalidValue;
-    return launch_kernel(kTimeGemm, mx_tile_kernel<BM, BN, WAVES_M, WAVES_N, NBUF, OUT, WIDE>, dim3((unsigned)total),
+    return launch_kernel(kTimeGemm, mx_tile_kernel<BM, BN, WAVES_M, WAVES_N, NBUF, OUT, ANY>, dim3((unsigned)total),
                          dim3(WAVES_M * WAVES_N * 64), 0, stream, p);
 }
 
@@ -356,8 +375,8 @@ __global__ __launch_bounds__(NW * 64) void mx_few_kernel(MxGemm p, MxRows rows) 
         for (int i = 0; i < WT; ++i)
 #pragma unroll
             for (int j = 0; j < XT; ++j) {
-                acc[i][j] = mx_multiply<0>(wf[0][i], xf[0][j], acc[i][j], wscale[i], xscale[j]);
-                acc[i][j] = mx_multiply<1>(wf[1][i], xf[1][j], acc[i][j], wscale[i], xscale[j]);
+                acc[i][j] = mx_multiply<0, 0>(wf[0][i], xf[0][j], acc[i][j], wscale[i], xscale[j]);
+                acc[i][j] = mx_multiply<1, 1>(wf[1][i], xf[1][j], acc[i][j], wscale[i], xscale[j]);
             }
     }
     if constexpr (!GIVEN) {                                   // the padding behind the last step
@@ -395,16 +414,37 @@ static hipError_t run_mx_few(MxGemm p, const MxRows& rows, hipStream_t stream) {
     return launch_kernel(kTimeGemm, mx_few_kernel<XT, WT, NW, OUT, IN>, dim3((unsigned)total), dim3(NW * 64), 0, stream, p, rows);
 }
 
+// The kernel by shape.
+//
+// Up to 32 tokens, or while 64 x 16 tiles are no more than the compute units: K over a workgroup's waves, 16 outputs a workgroup, or 32
+// where 16 make more workgroups than compute units (us from a graph, 16 / 32: 1 x 4096 x 4096 4.3 / 5.9, 1 x 6000 x 3150 5.3 / 5.1,
+// 16 x 6000 x 3150 6.8 / 5.9, 20 x 6000 x 3150 7.7 / 6.8).
+// Then tiles: rounds of the chip times what a tile takes, a constant and a cost per step in 10 ns, fitted to these (us, bf16 outputs,
+// three sets of operands in turn, 256 x 256 / 128 x 128, 64 x 128 and 64 x 64 two to a unit):
+//   8192 x 4096 x 4178    78.7 /  95.7 / 124.3 / 183.8       700 x 6000 x 3150    24.5 / 17.9 / 22.1 / 27.6
+//   8192 x 8192 x 8192   259.4 / 339.2 / 467.7 / 634.8       333 x 2049 x 1052    23.7 /  9.1 /  6.7 /  6.9
+//   4096 x 4096 x 4096    40.2 /  46.8 /  57.7 /  90.7       700 x 33001 x 1575   48.6 / 47.8 / 49.4 / 78.7
 template <Elem OUT>
 static hipError_t run_mx_gemm(const MxGemm& p, hipStream_t stream) {
-    if (p.ldx >= kWidePitch || p.ldw >= kWidePitch) return run_mx_tile<64, 64, 2, 2, 4, OUT, true>(p, stream);
     const int64_t cus = compute_units();
-    if (p.M <= 16) return run_mx_few<1, 1, 8, OUT, Codes>(p, MxRows{}, stream);
-    if (p.M <= 32) return run_mx_few<2, 1, 8, OUT, Codes>(p, MxRows{}, stream);
+    const bool wide = ceil_div(p.N, 16) > cus;
+    if (p.M <= 16) return wide ? run_mx_few<1, 2, 8, OUT, Codes>(p, MxRows{}, stream) : run_mx_few<1, 1, 8, OUT, Codes>(p, MxRows{}, stream);
+    if (p.M <= 32) return wide ? run_mx_few<2, 2, 8, OUT, Codes>(p, MxRows{}, stream) : run_mx_few<2, 1, 8, OUT, Codes>(p, MxRows{}, stream);
     if (ceil_div(p.M, 64) * ceil_div(p.N, 16) <= cus) return run_mx_few<4, 1, 8, OUT, Codes>(p, MxRows{}, stream);
-    if (ceil_div(p.M, 64) * ceil_div(p.N, 64) <= 2 * cus) return run_mx_tile<64, 64, 2, 2, 4, OUT>(p, stream);
-    if (ceil_div(p.M, 128) * ceil_div(p.N, 128) <= 2 * cus) return run_mx_tile<128, 128, 2, 4, 3, OUT>(p, stream);
-    return run_mx_tile<256, 256, 2, 4, 2, OUT>(p, stream);
+    if (p.ldx >= kWidePitch || p.ldw >= kWidePitch || p.ldx % 128 != 0 || p.ldw % 128 != 0) return run_mx_tile<64, 64, 2, 2, 4, OUT, true>(p, stream);
+    const auto cost = [&](int64_t bm, int64_t bn, int64_t at_once, int64_t fixed, int64_t step) {
+        return ceil_div(ceil_div(p.M, bm) * ceil_div(p.N, bn), at_once * cus) * (fixed + step * p.ksteps);
+    };
+    const int64_t by_tile[4] = {cost(64, 64, 2, 250, 53), cost(64, 128, 2, 200, 92), cost(128, 128, 2, 450, 116), cost(256, 256, 1, 1350, 150)};
+    int best = 0;
+    for (int i = 1; i < 4; ++i)
+        if (by_tile[i] < by_tile[best]) best = i;
+    switch (best) {
+        case 0: return run_mx_tile<64, 64, 2, 2, 4, OUT>(p, stream);
+        case 1: return run_mx_tile<64, 128, 2, 4, 2, OUT>(p, stream);
+        case 2: return run_mx_tile<128, 128, 2, 4, 2, OUT>(p, stream);
+        default: return run_mx_tile<256, 256, 4, 2, 2, OUT>(p, stream);
+    }
 }
 
 // Outputs by the launch, as in the int8 product: as a rule all of them.
@@ -445,7 +485,7 @@ hipError_t launch_qgemm_mx(const uint8_t* Xq, int64_t ldx, const uint8_t* Xs, in
 
 template <Elem OUT, typename IN>
 static hipError_t run_forward_mx(const MxGemm& p, const MxRows& rows, hipStream_t stream) {
-    return run_mx_few<1, 1, 8, OUT, IN>(p, rows, stream);
+    return ceil_div(p.N, 16) > compute_units() ? run_mx_few<1, 2, 8, OUT, IN>(p, rows, stream) : run_mx_few<1, 1, 8, OUT, IN>(p, rows, stream);
 }
 
 template <Elem OUT>
