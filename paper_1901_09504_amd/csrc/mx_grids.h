@@ -63,6 +63,14 @@ __device__ __forceinline__ void mx_values8(unsigned codes, unsigned byte, float 
 
 __device__ __forceinline__ unsigned mx_magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
+// The largest over each four neighbouring lanes.
+__device__ __forceinline__ unsigned quad_max(unsigned v) {
+    unsigned o = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);     // lanes 1 0 3 2
+    v = o > v ? o : v;
+    o = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);              // lanes 2 3 0 1
+    return o > v ? o : v;
+}
+
 // 2^-d for a channel's halvings
 __device__ __forceinline__ float mx_halvings(int d) { return ldexpf(1.0f, -(d < 0 ? 0 : (d > 255 ? 255 : d))); }
 

@@ -8,13 +8,6 @@
 
 namespace ocs {
 
-__device__ __forceinline__ unsigned quad_max(unsigned v) {
-    unsigned o = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);     // lanes 1 0 3 2
-    v = o > v ? o : v;
-    o = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);              // lanes 2 3 0 1
-    return o > v ? o : v;
-}
-
 // One lane per 8 columns; `blocks` blocks a row, the padding of codes and scales among them.
 template <Elem T, bool SCALED>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(MxRows p, unsigned blocks) {

@@ -271,27 +271,27 @@ static hipError_t run_mx_tile(MxGemm p, hipStream_t stream) {
 }
 
 // Few tokens: 16 XT tokens and 16 WT outputs per workgroup, the steps of K dealt over its NW waves, whose sums meet in LDS in the order of
-// the waves.  Each weight is used once, so codes and scales go from memory straight to the lanes that multiply them.
-// IN: the tokens' codes in memory (int), or rows of X of that type, which every workgroup puts on their grids itself, a block per
-// lane (a block's grid is its own affair: nothing waits for a row); the workgroups share the writing of codes and scales.
+// the waves.  Each weight is used once, so codes and scales go from memory straight to the lanes that multiply them, a step ahead.
+// IN: the tokens' codes in memory, or rows of X of that type: every workgroup puts all of them on their grids itself while its first weights
+// are on their way, into LDS, and the workgroups share the writing of codes and scales to memory.
 struct Codes {};
 template <Elem T>
 struct RowsOf {
     static constexpr Elem type = T;
 };
 
+// Bytes of LDS that a token's codes and scales take.
+__host__ __device__ inline int mx_image_row(int ksteps) { return ksteps * 136 + 16; }
+
 template <int XT, int WT, int NW, Elem OUT, typename IN>
 __global__ __launch_bounds__(NW * 64) void mx_few_kernel(MxGemm p, MxRows rows) {
     constexpr bool GIVEN = std::is_same<IN, Codes>::value;
+    constexpr int NT = NW * 64;
     __shared__ __align__(16) float sums[NW][XT * 16][WT * 16 + 4];
+    extern __shared__ __align__(16) uint8_t image[];
     const int tid = (int)threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col0 = (int)(blockIdx.x % (unsigned)p.tiles_n) * (WT * 16), row0 = (int)(blockIdx.x / (unsigned)p.tiles_n) * (XT * 16);
-    f32x4 acc[WT][XT];
-#pragma unroll
-    for (int i = 0; i < WT; ++i)
-#pragma unroll
-        for (int j = 0; j < XT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const uint8_t* w[WT];
     const uint8_t* ws[WT];
 #pragma unroll
@@ -303,98 +303,99 @@ __global__ __launch_bounds__(NW * 64) void mx_few_kernel(MxGemm p, MxRows rows) 
     }
     const uint8_t* x[XT];
     const uint8_t* xs[XT];
-    int m[XT];
 #pragma unroll
     for (int j = 0; j < XT; ++j) {
-        m[j] = row0 + j * 16 + fr;
-        const int r = m[j] < p.M ? m[j] : p.M - 1;
-        x[j] = p.Xq + r * p.ldx + 32 * fq;
-        xs[j] = p.Xs + r * p.ldxs + 2 * fq;
+        const int m = row0 + j * 16 + fr, r = m < p.M ? m : p.M - 1;
+        x[j] = GIVEN ? p.Xq + r * p.ldx + 32 * fq : image + r * mx_image_row(p.ksteps) + 32 * fq;
+        xs[j] = GIVEN ? p.Xs + r * p.ldxs + 2 * fq : image + r * mx_image_row(p.ksteps) + p.ksteps * 128 + 2 * fq;
     }
-    for (int kt = wave; kt < p.ksteps; kt += NW) {
+    struct Operands {
+        i32x4 w[2][WT], x[2][XT];
+        int ws[WT], xs[XT];
+    };
+    auto chunk = [&](const uint8_t* at, int64_t k, int64_t ld) {     // behind the pitch: zeros
+        i32x4 r = {0, 0, 0, 0};
+        if (k + 32 * fq < ld) r = *reinterpret_cast<const i32x4*>(at + k);
+        return r;
+    };
+    auto load = [&](int kt, Operands& o) {
         const int64_t k = (int64_t)kt * 128;
-        i32x4 wf[2][WT], xf[2][XT];
-        int wscale[WT], xscale[XT];
-        auto chunk = [&](const uint8_t* at, int half, int64_t ld) {
-            i32x4 r = {0, 0, 0, 0};
-            if (k + 32 * fq + 16 * half < ld) r = *reinterpret_cast<const i32x4*>(at + k + 16 * half);
-            return r;
-        };
 #pragma unroll
         for (int i = 0; i < WT; ++i) {
-            wscale[i] = *reinterpret_cast<const unsigned short*>(ws[i] + kt * 8);
+            o.ws[i] = *reinterpret_cast<const unsigned short*>(ws[i] + kt * 8);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) wf[h][i] = chunk(w[i], h, p.ldw);
+            for (int h = 0; h < 2; ++h) o.w[h][i] = chunk(w[i], k + 16 * h, p.ldw);
         }
+        if constexpr (GIVEN) {
 #pragma unroll
-        for (int j = 0; j < XT; ++j) {
-            if constexpr (GIVEN) {
-                xscale[j] = *reinterpret_cast<const unsigned short*>(xs[j] + kt * 8);
+            for (int j = 0; j < XT; ++j) {
+                o.xs[j] = *reinterpret_cast<const unsigned short*>(xs[j] + kt * 8);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) xf[h][j] = chunk(x[j], h, p.ldx);
-            } else {
-                xscale[j] = 0;
+                for (int h = 0; h < 2; ++h) o.x[h][j] = chunk(x[j], k + 16 * h, p.ldx);
+            }
+        }
+    };
+    Operands next;
+    if (wave < p.ksteps) load(wave, next);
+    if constexpr (!GIVEN) {
+        // four lanes a block, 8 columns each, as the pass over rows does it
+        const int blocks = p.ksteps * 8, total = p.M * blocks, share = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+        const int mine = (int)blockIdx.x * share, pitch = mx_image_row(p.ksteps);
+        for (int o = tid; o < total * 4; o += NT) {
+            const int at = o >> 2, row = at / blocks, block = at - row * blocks, part = o & 3;
+            const int k0 = block * kMxBlock + part * 8;
+            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (k0 < (rows.C + rows.s) * rows.g) mx_expanded8<IN::type, false>(rows, static_cast<const elem_t<IN::type>*>(rows.X) + row * rows.ldx, k0, v);
+            unsigned big = 0;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int block = kt * 8 + 2 * fq + h;
-                    const bool there = m[j] < p.M && (int64_t)block * kMxBlock < (int64_t)(rows.C + rows.s) * rows.g;
-                    i32x4 codes = {0, 0, 0, 0};
-                    unsigned byte = 0;
-                    if (there) {
-                        const elem_t<IN::type>* from = static_cast<const elem_t<IN::type>*>(rows.X) + m[j] * rows.ldx;
-                        float v[4][8];
-                        unsigned big = 0;
+            for (int e = 0; e < 8; ++e) big = mx_magnitude(v[e]) > big ? mx_magnitude(v[e]) : big;
+            const unsigned byte = mx_scale_byte(quad_max(big));
+            const unsigned codes = byte == 255u ? 0u : mx_codes8(v, mx_scale_value(byte));
+            *reinterpret_cast<unsigned*>(image + row * pitch + block * 16 + part * 4) = codes;
+            if (part == 0) image[row * pitch + p.ksteps * 128 + block] = (uint8_t)byte;
+            if (at >= mine && at < mine + share) {
+                if ((int64_t)block * 16 < rows.ldq) *reinterpret_cast<unsigned*>(rows.q + row * rows.ldq + block * 16 + part * 4) = codes;
+                if (part == 0 && block < rows.lds) rows.scale[row * rows.lds + block] = (uint8_t)byte;
+            }
+        }
+        // the padding behind the last step
+        const int64_t code_pad = rows.ldq / 16 - blocks, scale_pad = rows.lds - blocks;
+        for (int r = (int)blockIdx.x; r < p.M; r += (int)gridDim.x) {
+            for (int64_t o = tid; o < code_pad; o += NT) *reinterpret_cast<i32x4*>(rows.q + r * rows.ldq + (blocks + o) * 16) = i32x4{0, 0, 0, 0};
+            for (int64_t o = tid; o < scale_pad; o += NT) rows.scale[r * rows.lds + blocks + o] = 0;
+        }
+        __syncthreads();
+    }
+    f32x4 acc[WT][XT];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int k0 = block * kMxBlock + 8 * q;
+    for (int i = 0; i < WT; ++i)
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[q][e] = 0.0f;
-                            if (k0 < (rows.C + rows.s) * rows.g) mx_expanded8<IN::type, false>(rows, from, k0, v[q]);
-                        }
+        for (int j = 0; j < XT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int kt = wave; kt < p.ksteps; kt += NW) {
+        Operands o = next;
+        if (kt + NW < p.ksteps) load(kt + NW, next);
+        if constexpr (!GIVEN) {                               // (rows of tokens that are not there repeat the last one's)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
+            for (int j = 0; j < XT; ++j) {
+                o.xs[j] = *reinterpret_cast<const unsigned short*>(xs[j] + kt * 8);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) big = mx_magnitude(v[q][e]) > big ? mx_magnitude(v[q][e]) : big;
-                        byte = mx_scale_byte(big);
-                        if (byte != 255u) {
-                            const float scale = mx_scale_value(byte);
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) codes[q] = (int)mx_codes8(v[q], scale);
-                        }
-                    }
-                    xf[h][j] = codes;
-                    xscale[j] |= (int)(byte << (8 * h));
-                    if (m[j] < p.M && (unsigned)(block + m[j]) % gridDim.x == blockIdx.x) {
-                        if ((int64_t)block * 16 < rows.ldq) *reinterpret_cast<i32x4*>(rows.q + m[j] * rows.ldq + (int64_t)block * 16) = codes;
-                        if (block < rows.lds) rows.scale[m[j] * rows.lds + block] = (uint8_t)byte;
-                    }
-                }
+                for (int h = 0; h < 2; ++h) o.x[h][j] = *reinterpret_cast<const i32x4*>(x[j] + kt * 128 + 16 * h);
             }
         }
 #pragma unroll
         for (int i = 0; i < WT; ++i)
 #pragma unroll
             for (int j = 0; j < XT; ++j) {
-                acc[i][j] = mx_multiply<0, 0>(wf[0][i], xf[0][j], acc[i][j], wscale[i], xscale[j]);
-                acc[i][j] = mx_multiply<1, 1>(wf[1][i], xf[1][j], acc[i][j], wscale[i], xscale[j]);
+                acc[i][j] = mx_multiply<0, 0>(o.w[0][i], o.x[0][j], acc[i][j], o.ws[i], o.xs[j]);
+                acc[i][j] = mx_multiply<1, 1>(o.w[1][i], o.x[1][j], acc[i][j], o.ws[i], o.xs[j]);
             }
-    }
-    if constexpr (!GIVEN) {                                   // the padding behind the last step
-        for (int64_t o = blockIdx.x * (int64_t)(NW * 64) + tid, per = rows.ldq / 16 + rows.lds; o < p.M * per; o += gridDim.x * (int64_t)(NW * 64)) {
-            const int64_t r = o / per, at = o - r * per;
-            if (at < rows.ldq / 16) {
-                if (at >= p.ksteps * 8) *reinterpret_cast<i32x4*>(rows.q + r * rows.ldq + at * 16) = i32x4{0, 0, 0, 0};
-            } else if (at - rows.ldq / 16 >= p.ksteps * 8) {
-                rows.scale[r * rows.lds + at - rows.ldq / 16] = 0;
-            }
-        }
     }
 #pragma unroll
     for (int i = 0; i < WT; ++i)
 #pragma unroll
         for (int j = 0; j < XT; ++j) *reinterpret_cast<f32x4*>(&sums[wave][j * 16 + fr][i * 16 + fq * 4]) = acc[i][j];
     __syncthreads();
-    for (int o = tid; o < XT * 16 * WT * 16; o += NW * 64) {
+    for (int o = tid; o < XT * 16 * WT * 16; o += NT) {
         const int t = o / (WT * 16), c = o % (WT * 16), mm = row0 + t, n = col0 + c;
         if (mm >= p.M || n >= p.N) continue;
         float v = sums[0][t][c];
@@ -411,7 +412,8 @@ static hipError_t run_mx_few(MxGemm p, const MxRows& rows, hipStream_t stream) {
     p.tiles_n = (int)ceil_div(p.N, WT * 16);
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
     if (total > 0x7FFFFFFF || p.ksteps < 1) return hipErrorInvalidValue;
-    return launch_kernel(kTimeGemm, mx_few_kernel<XT, WT, NW, OUT, IN>, dim3((unsigned)total), dim3(NW * 64), 0, stream, p, rows);
+    const unsigned lds = std::is_same<IN, Codes>::value ? 0u : (unsigned)(p.M * mx_image_row(p.ksteps));
+    return launch_kernel(kTimeGemm, mx_few_kernel<XT, WT, NW, OUT, IN>, dim3((unsigned)total), dim3(NW * 64), lds, stream, p, rows);
 }
 
 // The kernel by shape.
@@ -502,7 +504,11 @@ hipError_t launch_forward_mx(const void* X, int type, int64_t ldx, int64_t M, in
                              int64_t ldq, uint8_t* Xs, int64_t ldxs, const uint8_t* Wq, int64_t ldw, const uint8_t* Ws, int64_t ldws,
                              int64_t N, const float* bias, void* Y, int out_type, int64_t ldy, bool apart, hipStream_t stream) {
     const int64_t Kexp = (int64_t)(C + s) * g;
-    if (apart && M <= 16 && N <= (int64_t)1 << 26) {              // (one launch reads X and W while outputs are being written)
+    // One launch while every workgroup's pass over all rows takes its lanes two rounds at most; beyond, that costs more than a launch of its own
+    // (us, calls one after the other, one launch / two: 1 x 250 -> 4000 4.0 / 6.5, 1 x 3000 -> 6000 6.7 / 8.0, 2 x 3000 -> 6000 7.4 / 8.2, 1 x 4096 ->
+    // 12000 10.1 / 12.5; 4 x 3000 -> 6000 8.6 / 8.5, 8 x 1000 -> 4000 7.7 / 6.5, 16 x 3000 -> 6000 17.9 / 9.1).  It reads X and W while outputs
+    // are being written.
+    if (apart && M <= 16 && M * ceil_div(Kexp, 256) <= 32 && N <= (int64_t)1 << 26) {
         const MxGemm p{Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, (int)M, (int)N, (int)ceil_div(Kexp, 256), bias, Y, ldy, 0, 0};
         const MxRows rows{X, ldx, M, C, g, s, chan_src, nullptr, Xq, ldq, Xs, ldxs};
         switch (static_cast<Elem>(out_type)) {
