@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "cache.h"
+#include "tile_requests.h"
 
 namespace ocs {
 
@@ -23,12 +24,12 @@ struct Attention {
     int64_t ldq, hdq;
     int Hq, G;                              // query heads, and of them to a head of the cache
     float scale;                            // times log2(e): scores are exponents of 2 here
-    int64_t window, most;                   // 0: no window; no position at or beyond `most` is looked at
+    int window, held;                       // 0: no window; no position at or beyond `held` is looked at
+    unsigned page_magic;                    // 2^32 / P and one more
     void* Y;
     int64_t ldy, hdy;
     float* lse;
-    int parts;                              // of a sequence's positions, `chunk` each
-    int64_t chunk;
+    int tiles, parts, chunk;                // tiles of rows; parts of a sequence's positions, `chunk` each
     float* sums;                            // [parts][T * Hq][D] and maxima and sums [parts][T * Hq][2], where there are parts
     float* stats;
 };
@@ -83,13 +84,29 @@ __device__ __forceinline__ unsigned mx_pair(unsigned codes, float scale) {
 
 __device__ __forceinline__ float int8_value(unsigned word, int at) { return (float)(int8_t)(word >> (8 * at)); }
 
+// The largest and the sum over the four lanes that hold one query's scores (lanes l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ void exchange_quarters(float v, float* a, float* b, bool far) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const unsigned u = __float_as_uint(v);
+    const auto r = far ? __builtin_amdgcn_permlane32_swap(u, u, false, false) : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    *a = __uint_as_float(r[0]);
+    *b = __uint_as_float(r[1]);
+#else
+    *a = *b = v;
+    (void)far;
+#endif
+}
 __device__ __forceinline__ float over_quarters_max(float v) {
-    v = __builtin_fmaxf(v, __shfl_xor(v, 16));
-    return __builtin_fmaxf(v, __shfl_xor(v, 32));
+    float a, b;
+    exchange_quarters(v, &a, &b, false);
+    exchange_quarters(__builtin_fmaxf(a, b), &a, &b, true);
+    return __builtin_fmaxf(a, b);
 }
 __device__ __forceinline__ float over_quarters_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    float a, b;
+    exchange_quarters(v, &a, &b, false);
+    exchange_quarters(a + b, &a, &b, true);
+    return a + b;
 }
 
 // `BYTES` bytes at an address that is a multiple of its largest power of two
@@ -137,23 +154,80 @@ __device__ __forceinline__ int tile_sequence(const Attention& p, int tile, int* 
     return b;
 }
 
+// What a query sees: `count` positions from `from` on (the cache holds fewer than 2^31).
+struct Seen {
+    int from, count;
+};
+__device__ __forceinline__ Seen positions_seen(const Attention& p, int64_t position) {
+    const int64_t last = position < p.held ? position : p.held - 1, first = p.window > 0 && position >= p.window ? position - p.window + 1 : 0;
+    Seen s{0, 0};
+    if (first <= last) s = Seen{(int)first, (int)(last - first + 1)};
+    return s;
+}
+
+// The row of the pool (of head 0, counted in [pages, H, P]) where 16 positions from j on begin, or -1.  The page's number comes first: what
+// it costs is the look-up in the table, which callers make one block of positions ahead.
+struct PageAt {
+    int page, at;
+};
+__device__ __forceinline__ PageAt page_of(const Attention& p, const int32_t* table, int j, int end) {
+    int col = (int)__umulhi((unsigned)j, p.page_magic), at = j - col * p.c.P;          // col is j / P or one more
+    if (at < 0) {
+        col -= 1;
+        at += p.c.P;
+    }
+    return PageAt{j < end ? table[col] : -1, at};
+}
+
+// How far above the softmax's reference a score may be before the sums are put on a new one (in powers of two): the reference then hardly
+// ever changes after the first positions, and weights stay far inside fp32's and bf16's range.
+constexpr float kSlack = 8.0f;
+
 constexpr int kAttendWaves = 4;
 
+// The columns of a key that a lane of quarter `fq` multiplies in step s of the product: 8 from here on.  Steps go in groups, for which a
+// lane loads up to 16 bytes, 64 of a row between the four quarters; queries take the same order.
+template <bool MX, int D>
+struct KeyColumns {
+    static constexpr int STEPS = D / 32, MOST = MX ? 4 : 2;
+    static constexpr int start(int s) { return s / MOST * MOST; }
+    static constexpr int steps(int s) { return STEPS - start(s) < MOST ? STEPS - start(s) : MOST; }
+    static __device__ __forceinline__ int column(int s, int fq) { return 32 * start(s) + 8 * (steps(s) * fq + s - start(s)); }
+};
+
+// A lane's part of a key, a group of steps after the other.
+template <bool MX, int D, int S>
+__device__ __forceinline__ void load_key(const uint8_t* key, int fq, unsigned* w) {
+    if constexpr (S < D / 32) {
+        constexpr int BYTES = (MX ? 4 : 8) * KeyColumns<MX, D>::steps(S);
+        unsigned part[BYTES / 4];
+        load_bytes<BYTES>(key + (MX ? 16 : 32) * S + BYTES * fq, part);
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i) w[(MX ? 1 : 2) * S + i] = part[i];
+        load_key<MX, D, S + KeyColumns<MX, D>::steps(S)>(key, fq, w);
+    }
+}
+
+// Workgroups are dealt to the 8 XCDs in turn: heads come first among them, so that every XCD gets its share of each sequence (64 sequences
+// of 128 to 8192 positions, 8 heads, tiles first 163 us, heads first 147).
+//
 // 16 rows of a sequence and head per workgroup; its waves take 32 positions at a time in turn and meet at the end.  Keys and values go
-// from memory to the lanes that multiply them: of a key a lane has D / 4 columns, a quarter; of a value D / 16, and the accumulator's tile t
+// from memory to the lanes that multiply them: of a key a lane has D / 4 columns, of a value D / 16, and the accumulator's tile t
 // holds column (D / 16) m + t in its row m.
 template <Elem T, CacheFormat F, int D>
-__global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attention p) {
+__global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Attention p) {
     constexpr int N = kPieces<T>, KS = D / 32, DT = D / 16, ROWS = 16, NW = kAttendWaves;
     constexpr bool MX = F == CacheFormat::mx4;
     constexpr int KB = MX ? D / 8 : D / 4, VB = MX ? D / 32 : D / 16;       // bytes of a lane's part of a key and of a value
+    using Columns = KeyColumns<MX, D>;
     constexpr int ROWB = MX ? D / 2 : D;
     __shared__ float top_of[NW][ROWS], total_of[NW][ROWS];
     __shared__ __align__(16) float out_of[NW / 2][ROWS][D + 4];
     const int lane = (int)threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = (int)(blockIdx.x % (unsigned)p.c.H), part = (int)(blockIdx.x / (unsigned)p.c.H / (unsigned)p.tiles);
     int row0 = 0, t0 = 0, n = 0;
-    const int b = __builtin_amdgcn_readfirstlane(tile_sequence<ROWS>(p, (int)blockIdx.x, &row0, &t0, &n));
+    const int b = __builtin_amdgcn_readfirstlane(tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles), &row0, &t0, &n));
     if (b < 0) return;
     row0 = __builtin_amdgcn_readfirstlane(row0);
     t0 = __builtin_amdgcn_readfirstlane(t0);
@@ -161,33 +235,35 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
     const int rows = n * p.G - row0 < ROWS ? n * p.G - row0 : ROWS;
     const int64_t start = p.s.starts[b];
 
-    // this lane's query, and the positions that any of the tile sees
+    // this lane's query, and the positions that any of the tile sees and that all of it see
     const int row = row0 + (fr < rows ? fr : rows - 1), token = row / p.G, head = h * p.G + row % p.G;
-    const int64_t seen = start + token, from = p.window > 0 ? seen - p.window + 1 : 0;
-    const int64_t held = p.most < p.c.cols * p.c.P ? p.most : p.c.cols * p.c.P;
-    int64_t end = start + (row0 + rows - 1) / p.G + 1, begin = p.window > 0 ? start + row0 / p.G - p.window + 1 : 0;
-    end = end < held ? end : held;
-    begin = begin > 0 ? begin & ~(int64_t)31 : 0;
+    const int first_token = row0 / p.G, last_token = (row0 + rows - 1) / p.G;
+    const Seen mine = positions_seen(p, start + token), first = positions_seen(p, start + first_token), last = positions_seen(p, start + last_token);
+    const int64_t first_seen = start + first_token - p.window + 1, past = start + last_token + 1;
+    int begin = p.window > 0 && first_seen > 0 ? (int)(first_seen < p.held ? first_seen & ~(int64_t)31 : p.held) : 0;
+    int end = past < 0 ? 0 : past < p.held ? (int)past : p.held;
+    const int all_from = last.count > 0 ? last.from : 0x7FFFFFFF, all_end = first.from + first.count;
     if (p.parts > 1) {
-        begin += blockIdx.z * p.chunk;
-        end = begin + p.chunk < end ? begin + p.chunk : end;
+        const int64_t at = begin + part * (int64_t)p.chunk;
+        begin = at < end ? (int)at : end;
+        end = at + p.chunk < end ? (int)(at + p.chunk) : end;
     }
 
     u32x4 q[KS][N];
     {
-        const elem_t<T>* x = static_cast<const elem_t<T>*>(p.Q) + (int64_t)(t0 + token) * p.ldq + head * p.hdq + fq * (D / 4);
+        const elem_t<T>* x = static_cast<const elem_t<T>*>(p.Q) + (int64_t)(t0 + token) * p.ldq + head * p.hdq;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             float v[8];
 #pragma unroll
             for (int g = 0; g < 8 / kVec<T>; ++g) {
-                const u32x4 piece = load_piece<T>(x + 8 * s + g * kVec<T>);
+                const u32x4 piece = load_piece<T>(x + Columns::column(s, fq) + g * kVec<T>);
 #pragma unroll
                 for (int e = 0; e < kVec<T>; ++e) v[g * kVec<T> + e] = piece_elem<T>(piece, e);
             }
             if (p.c.kdepth) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= cache_doublings(p.c.kdepth[h * D + fq * (D / 4) + 8 * s + e]);
+                for (int e = 0; e < 8; ++e) v[e] *= cache_doublings(p.c.kdepth[h * D + Columns::column(s, fq) + e]);
             }
             bf16_sums<N>(v, q[s]);
         }
@@ -197,29 +273,32 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
         unsigned k[2][(KB + 3) / 4], v[8][(VB + 3) / 4];
         float kstep[2][4], vstep[2][4];                     // 8 bits: of this lane's keys and values
         unsigned kscale[2][KS], vscale[8][2];               // 4 bits: the bytes of its blocks
-        bool there[2];
     };
-    auto load = [&](int64_t j0, Block& x) {
+    struct Where {                                          // its pages
+        PageAt at[2];
+    };
+    const int32_t* table = p.c.table + b * p.c.ldt;
+    auto look_up = [&](int j0, Where& w) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) w.at[g] = page_of(p, table, j0 + 16 * g, end);
+    };
+    auto there = [&](const PageAt& at) { return at.page >= 0 && at.page < p.c.pages; };
+    auto load = [&](const Where& w, Block& x) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const int64_t j = j0 + 16 * g;
-            int64_t col = j / p.c.P;
-            const int at = (int)(j - col * p.c.P);
-            int64_t page = -1;
-            if (j < held) page = p.c.table[b * p.c.ldt + col];
-            x.there[g] = page >= 0 && page < p.c.pages;
-            if (!x.there[g]) page = 0;
-            const int64_t r = (page * p.c.H + h) * p.c.P + (x.there[g] ? at : 0);       // of the group's first position
-            load_bytes<KB>(static_cast<const uint8_t*>(p.c.keys) + (r + fr) * ROWB + fq * KB, x.k[g]);
+            const bool ok = there(w.at[g]);
+            const int64_t r = ((int64_t)(ok ? w.at[g].page : 0) * p.c.H + h) * p.c.P + (ok ? w.at[g].at : 0);       // of the group's first position
+            const uint8_t* keys = static_cast<const uint8_t*>(p.c.keys) + r * ROWB;
+            const uint8_t* values = static_cast<const uint8_t*>(p.c.values) + r * ROWB;
+            load_key<MX, D, 0>(keys + fr * ROWB, fq, x.k[g]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                load_bytes<VB>(static_cast<const uint8_t*>(p.c.values) + (r + 4 * fq + i) * ROWB + fr * VB, x.v[4 * g + i]);
+            for (int i = 0; i < 4; ++i) load_bytes<VB>(values + (4 * fq + i) * ROWB + fr * VB, x.v[4 * g + i]);
             if constexpr (MX) {
-                const uint8_t* ks = static_cast<const uint8_t*>(p.c.kscales) + (r + fr) * (D / 32);
-                const uint8_t* vs = static_cast<const uint8_t*>(p.c.vscales) + (r + 4 * fq) * (D / 32);
+                const uint8_t* ks = static_cast<const uint8_t*>(p.c.kscales) + r * (D / 32) + fr * (D / 32);
+                const uint8_t* vs = static_cast<const uint8_t*>(p.c.vscales) + r * (D / 32) + 4 * fq * (D / 32);
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
-                    if (s == 0 || (D / 4) % 32 != 0 || s % 4 == 0) x.kscale[g][s] = ks[(fq * (D / 4) + 8 * s) / 32];
+                    if (Columns::steps(s) != 4 || s % 4 == 0) x.kscale[g][s] = ks[Columns::column(s, fq) / 32];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     x.vscale[4 * g + i][0] = vs[i * (D / 32) + fr * DT / 32];
@@ -240,11 +319,11 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
     f32x4 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float top = -__builtin_inff(), total = 0.0f;            // total: of this lane's positions
-    auto use = [&](int64_t j0, const Block& x) {
+    float top = -__builtin_inff(), total = 0.0f;            // the softmax's reference; the sum over this lane's positions
+    auto use = [&](int j0, const Where& where, const Block& x) {
         float s[8];
-        bool sees[8];
-        float most = -__builtin_inff();
+        // whether every row of the tile sees all 32
+        const bool whole = j0 >= all_from && j0 + 32 <= all_end && j0 + 32 <= end && there(where.at[0]) && there(where.at[1]);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -253,7 +332,7 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
                 u32x4 k;
                 if constexpr (MX) {
                     const unsigned w = x.k[g][st];
-                    const float scale = mx_scale_value(x.kscale[g][(D / 4) % 32 != 0 ? st : st / 4 * 4]);
+                    const float scale = mx_scale_value(x.kscale[g][Columns::steps(st) != 4 ? st : st / 4 * 4]);
                     k = u32x4{mx_pair<0>(w, scale), mx_pair<1>(w, scale), mx_pair<2>(w, scale), mx_pair<3>(w, scale)};
                 } else {
 #pragma unroll
@@ -266,36 +345,62 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
                 for (int m = N - 1; m >= 0; --m) a = multiply_bf16(k, q[st][m], a);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t j = j0 + 16 * g + 4 * fq + i;
-                sees[4 * g + i] = x.there[g] && j <= seen && j >= from && j < end;
-                float v = a[i] * p.scale;
-                if constexpr (!MX) v = a[i] * (x.kstep[g][i] * p.scale);
-                s[4 * g + i] = sees[4 * g + i] ? v : -__builtin_inff();
-                most = s[4 * g + i] > most || s[4 * g + i] != s[4 * g + i] ? s[4 * g + i] : most;
+            for (int i = 0; i < 4; ++i) s[4 * g + i] = MX ? a[i] * p.scale : a[i] * (x.kstep[g][i] * p.scale);
+        }
+        unsigned sees = 0xFFu;                              // a bit per position of this lane
+        if (!whole) {
+            sees = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int j = j0 + 16 * (i / 4) + 4 * fq + i % 4;
+                if (there(where.at[i / 4]) && j < end && (unsigned)(j - mine.from) < (unsigned)mine.count) sees |= 1u << i;
+                else s[i] = -__builtin_inff();
             }
         }
-        // (a score that is NaN makes the row NaN by its weight; as a maximum it may be lost)
-        const float next = __builtin_fmaxf(top, over_quarters_max(most)), base = next == -__builtin_inff() ? 0.0f : next;
-        const float shrink = __builtin_amdgcn_exp2f(top - base);
-        top = next;
-        total *= shrink;
+        float most = s[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) most = __builtin_fmaxf(most, s[i]);
+        if (__any(most > top + kSlack)) {                   // (the lanes of a query take the same reference: they all come here)
+            const float next = __builtin_fmaxf(top, over_quarters_max(most));
+            const float shrink = next == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - next);
+            top = next;
+            total *= shrink;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[t][i] *= shrink;
+        }
+        const float base = top == -__builtin_inff() ? 0.0f : top;
         float w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             w[i] = __builtin_amdgcn_exp2f(s[i] - base);
             total += w[i];
         }
-        bool nan_value[8];
+        unsigned vscale[8][2];
+        if constexpr (MX) {
+            unsigned highest = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (MX) {
-                // 255: a NaN for those who see it, nothing for the others
-                nan_value[i] = x.vscale[i][0] == 255u || (32 % DT != 0 && x.vscale[i][1] == 255u);
-                if (nan_value[i] && sees[i]) w[i] = __uint_as_float(0x7FC00000u);
-            } else {
-                w[i] = sees[i] ? w[i] * x.vstep[i / 4][i % 4] : 0.0f;
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < (32 % DT != 0 ? 2 : 1); ++e) {
+                    vscale[i][e] = x.vscale[i][e];
+                    highest = vscale[i][e] > highest ? vscale[i][e] : highest;
+                }
+            if (__any(highest == 255u)) {                   // 255: a NaN for those who see it, nothing for the others
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (vscale[i][0] != 255u && (32 % DT == 0 || vscale[i][1] != 255u)) continue;
+                    if (sees >> i & 1) w[i] = __uint_as_float(0x7FC00000u);
+                    vscale[i][0] = vscale[i][1] = 127u;
+                }
             }
+        } else if (whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] *= x.vstep[i / 4][i % 4];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = sees >> i & 1 ? w[i] * x.vstep[i / 4][i % 4] : 0.0f;
         }
         u32x4 pw[N];
         bf16_sums<N>(w, pw);
@@ -310,10 +415,10 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int i = 2 * d + e;
-                        unsigned byte = x.vscale[i][0];
+                        unsigned byte = vscale[i][0];
                         if constexpr (32 % DT != 0)
-                            if ((fr * DT + t) / 32 != fr * DT / 32) byte = x.vscale[i][1];
-                        const float scale = mx_scale_value(nan_value[i] ? 0u : byte);
+                            if ((fr * DT + t) / 32 != fr * DT / 32) byte = vscale[i][1];
+                        const float scale = mx_scale_value(byte);
                         const unsigned word = x.v[i][t / 8];
                         pair[e] = t % 8 == 0 ? mx_pair<0>(word, scale) : t % 8 == 2 ? mx_pair<1>(word, scale) : t % 8 == 4 ? mx_pair<2>(word, scale) : mx_pair<3>(word, scale);
                     }
@@ -328,22 +433,33 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
                 v[1][d] = c;
             }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t + e][i] *= shrink;
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int m = N - 1; m >= 0; --m) acc[t + e] = multiply_bf16(v[e], pw[m], acc[t + e]);
-            }
         }
     };
     {
-        int64_t j = begin + 32 * wave;
-        Block now, next;
-        if (j < end) load(j, now);
-        for (; j < end; j += 32 * NW) {
-            if (j + 32 * NW < end) load(j + 32 * NW, next);
-            use(j, now);
-            now = next;
+        // pages are looked up two blocks ahead, rows loaded one ahead; two blocks by turns, so that none is copied
+        constexpr int STRIDE = 32 * NW;
+        int j = begin + 32 * wave;
+        Block even, odd;
+        Where at_even{}, at_odd{};
+        if (j < end) {
+            look_up(j, at_even);
+            if (j + STRIDE < end) look_up(j + STRIDE, at_odd);
+            load(at_even, even);
+        }
+        auto turn = [&](Where& at, Block& x, const Where& next_at, Block& next) {
+            if (j + STRIDE < end) load(next_at, next);
+            const Where now = at;
+            if (j + 2 * STRIDE < end) look_up(j + 2 * STRIDE, at);
+            use(j, now, x);
+            j += STRIDE;
+        };
+        while (j < end) {
+            turn(at_even, even, at_odd, odd);
+            if (j >= end) break;
+            turn(at_odd, odd, at_even, even);
         }
     }
     total = over_quarters_sum(total);
@@ -384,7 +500,7 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
     if (wave != 0 || fr >= rows) return;
     const int64_t out_row = (int64_t)(t0 + token) * p.Hq + head;
     if (p.parts > 1) {
-        const int64_t at = blockIdx.z * ((int64_t)p.s.T * p.Hq) + out_row;
+        const int64_t at = part * ((int64_t)p.s.T * p.Hq) + out_row;
         if (fq == 0) {
             p.stats[2 * at] = all;
             p.stats[2 * at + 1] = sum;
@@ -397,51 +513,427 @@ __global__ __launch_bounds__(kAttendWaves * 64) void attend_rows_kernel(Attentio
     }
     if (p.lse && fq == 0) p.lse[out_row] = sum > 0.0f ? (all + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : (sum == 0.0f ? -__builtin_inff() : sum);
     elem_t<T>* y = static_cast<elem_t<T>*>(p.Y) + (int64_t)(t0 + token) * p.ldy + head * p.hdy;
-    const float part = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float share = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
             const int d = (4 * fq + i) * DT + t;
-            float v = sum == 0.0f ? 0.0f : acc[t][i] * part;
+            float v = sum == 0.0f ? 0.0f : acc[t][i] * share;
             if (p.c.vdepth) v *= cache_doublings(p.c.vdepth[h * D + d]);
             y[d] = float_to_elem<T>(v);
         }
 }
 
-// The parts of a row put together, one workgroup of D lanes per row.
+// Of 4 rows of 16 two-byte numbers in LDS, to which 16 lanes give the addresses of 8 bytes each, lane i gets column i.
+__device__ __forceinline__ u32x2 read_transposed(const uint8_t* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)lds));
+#else
+    (void)lds;
+    return u32x2{0u, 0u};
+#endif
+}
+
+// Many rows: 64 NT rows of a sequence and head per workgroup, 16 NT to each of its four waves.  The workgroup turns KT positions at a time into
+// bf16 numbers in LDS, once for all its rows, while the next positions' codes are on their way, and the waves multiply from there: keys a
+// row at a time, values transposed as they are read (ds_read_b64_tr_b16).  Rows of LDS are 4 and 8 banks apart beyond a multiple of 64, so
+// that what the matrix cores read at a time lies in different banks.
+template <Elem T, int D>
+struct AttendTile {
+    static constexpr int N = kPieces<T>;
+    static constexpr int NT = D <= 128 ? 2 : 1, ROWS = 64 * NT, KT = D <= 128 && N == 1 ? 64 : 32;
+    static constexpr int KPITCH = 2 * D + 16, VPITCH = 2 * D + 32;
+    static constexpr int LDS = 2 * KT * (KPITCH + VPITCH);
+};
+
+template <Elem T, CacheFormat F, int D>
+__global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
+    using Tile = AttendTile<T, D>;
+    constexpr int N = Tile::N, NT = Tile::NT, ROWS = Tile::ROWS, KT = Tile::KT, KPITCH = Tile::KPITCH, VPITCH = Tile::VPITCH;
+    constexpr int KS = D / 32, DT = D / 16, MT = KT / 16;
+    constexpr bool MX = F == CacheFormat::mx4;
+    constexpr int ROWB = MX ? D / 2 : D, PIECE = MX ? 8 : 16;              // bytes of a row, and of 16 of its codes
+    constexpr int ITEMS = KT * (D / 16), LOADS = (ITEMS + 255) / 256;
+    extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ __align__(16) float ksteps[2][KT], vsteps[2][KT];
+    __shared__ int there_of[2][MT];
+    const int tid = (int)threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = (int)(blockIdx.x % (unsigned)p.c.H), part = (int)(blockIdx.x / (unsigned)p.c.H / (unsigned)p.tiles);
+    int row0 = 0, t0 = 0, n = 0;
+    const int b = __builtin_amdgcn_readfirstlane(tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles), &row0, &t0, &n));
+    if (b < 0) return;
+    row0 = __builtin_amdgcn_readfirstlane(row0);
+    t0 = __builtin_amdgcn_readfirstlane(t0);
+    n = __builtin_amdgcn_readfirstlane(n);
+    const int rows = n * p.G - row0 < ROWS ? n * p.G - row0 : ROWS;
+    const int64_t start = p.s.starts[b];
+    const int first_token = row0 / p.G, last_token = (row0 + rows - 1) / p.G;
+    const Seen first = positions_seen(p, start + first_token), last = positions_seen(p, start + last_token);
+    const int64_t first_seen = start + first_token - p.window + 1, past = start + last_token + 1;
+    int begin = p.window > 0 && first_seen > 0 ? (int)(first_seen < p.held ? first_seen & ~(int64_t)31 : p.held) : 0;
+    int end = past < 0 ? 0 : past < p.held ? (int)past : p.held;
+    const int all_from = last.count > 0 ? last.from : 0x7FFFFFFF, all_end = first.from + first.count;
+    if (p.parts > 1) {
+        const int64_t at = begin + part * (int64_t)p.chunk;
+        begin = at < end ? (int)at : end;
+        end = at + p.chunk < end ? (int)(at + p.chunk) : end;
+    }
+
+    // this lane's queries, and the positions that the wave sees
+    const int wave_row = wave * 16 * NT;
+    int token[NT], head[NT];
+    Seen mine[NT];
+    u32x4 q[NT][KS][N];
+    int wave_from = 0x7FFFFFFF, wave_end = 0;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const int r = wave_row + 16 * u + fr, row = row0 + (r < rows ? r : rows - 1);
+        token[u] = row / p.G;
+        head[u] = h * p.G + row - token[u] * p.G;
+        mine[u] = positions_seen(p, start + token[u]);
+        if (r >= rows) mine[u].count = 0;
+        const elem_t<T>* x = static_cast<const elem_t<T>*>(p.Q) + (int64_t)(t0 + token[u]) * p.ldq + head[u] * p.hdq + 8 * fq;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            float v[8];
+#pragma unroll
+            for (int g = 0; g < 8 / kVec<T>; ++g) {
+                const u32x4 piece = load_piece<T>(x + 32 * s + g * kVec<T>);
+#pragma unroll
+                for (int e = 0; e < kVec<T>; ++e) v[g * kVec<T> + e] = piece_elem<T>(piece, e);
+            }
+            if (p.c.kdepth) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= cache_doublings(p.c.kdepth[h * D + 32 * s + 8 * fq + e]);
+            }
+            bf16_sums<N>(v, q[u][s]);
+        }
+    }
+    if (wave_row < rows) {
+        const int last_row = wave_row + 16 * NT < rows ? wave_row + 16 * NT - 1 : rows - 1;
+        const Seen a = positions_seen(p, start + (row0 + wave_row) / p.G), z = positions_seen(p, start + (row0 + last_row) / p.G);
+        wave_from = a.count > 0 ? a.from : z.from;
+        wave_end = z.count > 0 ? z.from + z.count : a.from + a.count;
+    }
+
+    // codes of KT positions on their way: 16 of a key and of a value to a lane
+    struct Codes {
+        unsigned k[PIECE / 4], v[PIECE / 4];
+        float kstep, vstep;                                 // 4 bits: the scale bytes' numbers
+    };
+    Codes codes[LOADS];
+    PageAt at[LOADS];
+    const int32_t* table = p.c.table + b * p.c.ldt;
+    auto key_of = [&](int u) { return (tid + 256 * u) / (D / 16); };
+    auto part_of = [&](int u) { return (tid + 256 * u) % (D / 16); };
+    auto there = [&](const PageAt& w) { return w.page >= 0 && w.page < p.c.pages; };
+    auto look_up = [&](int j0) {
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u)
+            if (tid + 256 * u < ITEMS) {
+                at[u] = page_of(p, table, j0 + (key_of(u) & ~15), end);
+                at[u].at += key_of(u) & 15;
+            }
+    };
+    auto load = [&]() {
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u)
+            if (tid + 256 * u < ITEMS) {
+                const int64_t r = there(at[u]) ? ((int64_t)at[u].page * p.c.H + h) * p.c.P + at[u].at : (int64_t)h * p.c.P;
+                load_bytes<PIECE>(static_cast<const uint8_t*>(p.c.keys) + r * ROWB + part_of(u) * PIECE, codes[u].k);
+                load_bytes<PIECE>(static_cast<const uint8_t*>(p.c.values) + r * ROWB + part_of(u) * PIECE, codes[u].v);
+                if constexpr (MX) {
+                    codes[u].kstep = mx_scale_value(static_cast<const uint8_t*>(p.c.kscales)[r * (D / 32) + part_of(u) / 2]);
+                    codes[u].vstep = mx_scale_value(static_cast<const uint8_t*>(p.c.vscales)[r * (D / 32) + part_of(u) / 2]);
+                } else {
+                    codes[u].kstep = static_cast<const float*>(p.c.kscales)[r];
+                    codes[u].vstep = static_cast<const float*>(p.c.vscales)[r];
+                }
+            }
+    };
+    auto numbers = [&](const unsigned (&w)[PIECE / 4], float step, u32x4 (&out)[2]) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if constexpr (MX) {
+                out[e] = u32x4{mx_pair<0>(w[e], step), mx_pair<1>(w[e], step), mx_pair<2>(w[e], step), mx_pair<3>(w[e], step)};
+            } else {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const unsigned c = w[2 * e + d / 2];
+                    out[e][d] = bf16_pair(int8_value(c, 2 * (d & 1)), int8_value(c, 2 * (d & 1) + 1));
+                }
+            }
+    };
+    auto store = [&](int j0, int buf) {                      // (of the positions whose pages are still in `at`)
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u)
+            if (tid + 256 * u < ITEMS) {
+                const int key = key_of(u), col = part_of(u), j = j0 + key;
+                u32x4 x[2];
+                numbers(codes[u].k, codes[u].kstep, x);
+                uint8_t* k = lds + (buf * KT + key) * KPITCH + col * 32;
+                *reinterpret_cast<u32x4*>(k) = x[0];
+                *reinterpret_cast<u32x4*>(k + 16) = x[1];
+                float vstep = codes[u].vstep, weight = 1.0f;
+                if constexpr (MX) {
+                    // a value that is no number, where not all rows see it: 0 here, and NaN as the weight's factor for those who do
+                    const bool all = there(at[u]) && j >= all_from && j < all_end && j < end;
+                    if (!all && __float_as_uint(vstep) == 0x7F800000u) {
+                        vstep = 1.0f;
+                        weight = __uint_as_float(0x7FC00000u);
+                    }
+                } else {
+                    weight = vstep;
+                }
+                numbers(codes[u].v, vstep, x);
+                uint8_t* v = lds + 2 * KT * KPITCH + (buf * KT + key) * VPITCH + col * 32;
+                *reinterpret_cast<u32x4*>(v) = x[0];
+                *reinterpret_cast<u32x4*>(v + 16) = x[1];
+                if (col == 0) {
+                    if constexpr (!MX) ksteps[buf][key] = codes[u].kstep * p.scale;
+                    vsteps[buf][key] = weight;
+                    if ((key & 15) == 0) there_of[buf][key >> 4] = there(at[u]);
+                }
+            }
+    };
+
+    f32x4 acc[DT][NT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) acc[t][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float top[NT], total[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        top[u] = -__builtin_inff();
+        total[u] = 0.0f;
+    }
+    auto use = [&](int j0, int buf) {
+        bool whole = j0 >= all_from && j0 + KT <= all_end && j0 + KT <= end;
+        unsigned pages = 0;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) pages |= (there_of[buf][m] ? 1u : 0u) << m;
+        whole = whole && pages == (1u << MT) - 1;
+        f32x4 s[MT][NT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int u = 0; u < NT; ++u) s[m][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                const u32x4 k = *reinterpret_cast<const u32x4*>(lds + (buf * KT + 16 * m + fr) * KPITCH + (32 * st + 8 * fq) * 2);
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int e = N - 1; e >= 0; --e) s[m][u] = multiply_bf16(k, q[u][st][e], s[m][u]);
+            }
+            f32x4 factor = {p.scale, p.scale, p.scale, p.scale};
+            if constexpr (!MX) factor = *reinterpret_cast<const f32x4*>(&ksteps[buf][16 * m + 4 * fq]);
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[m][u][i] *= factor[i];
+        }
+        if (!whole) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = j0 + 16 * m + 4 * fq + i;
+                        if (!(pages >> m & 1) || j >= end || (unsigned)(j - mine[u].from) >= (unsigned)mine[u].count) s[m][u][i] = -__builtin_inff();
+                    }
+        }
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            float most = s[0][u][0];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = __builtin_fmaxf(most, s[m][u][i]);
+            if (__any(most > top[u] + kSlack)) {
+                const float next = __builtin_fmaxf(top[u], over_quarters_max(most));
+                const float shrink = next == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top[u] - next);
+                top[u] = next;
+                total[u] *= shrink;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[t][u][i] *= shrink;
+            }
+        }
+#pragma unroll
+        for (int kk = 0; kk < MT / 2; ++kk) {
+            u32x4 w[NT][N];
+#pragma unroll
+            for (int u = 0; u < NT; ++u) {
+                const float base = top[u] == -__builtin_inff() ? 0.0f : top[u];
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int m = 2 * kk + i / 4;
+                    x[i] = __builtin_amdgcn_exp2f(s[m][u][i % 4] - base);
+                    total[u] += x[i];
+                }
+                if (!MX || !whole) {
+                    const f32x4 a = *reinterpret_cast<const f32x4*>(&vsteps[buf][32 * kk + 4 * fq]), c = *reinterpret_cast<const f32x4*>(&vsteps[buf][32 * kk + 16 + 4 * fq]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float f = i < 4 ? a[i % 4] : c[i % 4];
+                                x[i] = whole || x[i] != 0.0f ? x[i] * f : 0.0f;
+                    }
+                }
+                bf16_sums<N>(x, w[u]);
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                const uint8_t* v = lds + 2 * KT * KPITCH + (buf * KT + 32 * kk + 4 * fq + (fr >> 2)) * VPITCH + (16 * t + (fr & 3) * 4) * 2;
+                const u32x2 lo = read_transposed(v), hi = read_transposed(v + 16 * VPITCH);
+                const u32x4 vt = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int e = N - 1; e >= 0; --e) acc[t][u] = multiply_bf16(vt, w[u][e], acc[t][u]);
+            }
+        }
+    };
+
+    // One barrier for KT positions: the next ones' numbers go into the other buffer while these are used.
+    if (begin < end) {
+        look_up(begin);
+        load();
+        store(begin, 0);
+        if (begin + KT < end) look_up(begin + KT);
+        __syncthreads();
+        int buf = 0;
+        for (int j = begin; j < end; j += KT, buf ^= 1) {
+            const bool more = j + KT < end;
+            if (more) load();
+            if (j < wave_end && j + KT > wave_from) use(j, buf);
+            if (more) {
+                store(j + KT, buf ^ 1);
+                if (j + 2 * KT < end) look_up(j + 2 * KT);
+            }
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const float sum = over_quarters_sum(total[u]);
+        if (wave_row + 16 * u + fr >= rows) continue;
+        const int64_t out_row = (int64_t)(t0 + token[u]) * p.Hq + head[u];
+        if (p.parts > 1) {
+            const int64_t to = part * ((int64_t)p.s.T * p.Hq) + out_row;
+            if (fq == 0) {
+                p.stats[2 * to] = top[u];
+                p.stats[2 * to + 1] = sum;
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(p.sums + to * D + 16 * t + 4 * fq) = acc[t][u];
+            continue;
+        }
+        if (p.lse && fq == 0)
+            p.lse[out_row] = sum > 0.0f ? (top[u] + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : (sum == 0.0f ? -__builtin_inff() : sum);
+        elem_t<T>* y = static_cast<elem_t<T>*>(p.Y) + (int64_t)(t0 + token[u]) * p.ldy + head[u] * p.hdy + 4 * fq;
+        const float share = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v = sum == 0.0f ? 0.0f : acc[t][u][i] * share;
+                if (p.c.vdepth) v *= cache_doublings(p.c.vdepth[h * D + 16 * t + 4 * fq + i]);
+                y[16 * t + i] = float_to_elem<T>(v);
+            }
+    }
+}
+
+// The parts of a row put together, one workgroup per row: its parts' maxima and sums, one to a lane, then their columns, four to a lane, as
+// many parts at once as there are lanes for.
 template <Elem T>
 __global__ __launch_bounds__(256) void attend_join_kernel(Attention p) {
+    __shared__ float weight[256], red[2][4];
+    __shared__ f32x4 partial[256];
     const int64_t rows = (int64_t)p.s.T * p.Hq, row = blockIdx.x;
-    const int t = (int)(row / p.Hq), head = (int)(row % p.Hq), d = (int)threadIdx.x, D = p.c.D;
-    if (sequence_of(p.s, t) < 0 || d >= D) return;
-    float all = -__builtin_inff();
-    for (int i = 0; i < p.parts; ++i) all = __builtin_fmaxf(all, p.stats[2 * (i * rows + row)]);
-    const float base = all == -__builtin_inff() ? 0.0f : all;
-    float sum = 0.0f, v = 0.0f;
-    for (int i = 0; i < p.parts; ++i) {
-        const float part = p.stats[2 * (i * rows + row) + 1], f = __builtin_amdgcn_exp2f(p.stats[2 * (i * rows + row)] - base);
-        sum += part * f;
-        v += p.sums[(i * rows + row) * D + d] * f;
+    const int t = (int)(row / p.Hq), head = (int)(row % p.Hq), tid = (int)threadIdx.x, D = p.c.D;
+    if (sequence_of(p.s, t) < 0) return;
+    const int lanes = D / 4, groups = 256 / lanes, group = tid / lanes, d = tid % lanes * 4;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    float all = -__builtin_inff(), sum = 0.0f;
+    for (int i0 = 0; i0 < p.parts; i0 += 256) {             // (256 parts hold any cache but the longest)
+        const int i = i0 + tid, n = p.parts - i0 < 256 ? p.parts - i0 : 256;
+        float top = -__builtin_inff(), total = 0.0f;
+        if (i < p.parts) {
+            top = p.stats[2 * (i * rows + row)];
+            total = p.stats[2 * (i * rows + row) + 1];
+        }
+        float most = top;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, m));
+        if ((tid & 63) == 0) red[0][tid >> 6] = most;
+        __syncthreads();
+        most = __builtin_fmaxf(__builtin_fmaxf(red[0][0], red[0][1]), __builtin_fmaxf(red[0][2], red[0][3]));
+        const float next = __builtin_fmaxf(all, most), base = next == -__builtin_inff() ? 0.0f : next;
+        const float f = __builtin_amdgcn_exp2f(top - base), shrink = __builtin_amdgcn_exp2f(all - base);
+        all = next;
+        weight[tid] = total == 0.0f ? 0.0f : f;             // (a part without a position has written no columns)
+        float part = total * f;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) part += __shfl_xor(part, m);
+        if ((tid & 63) == 0) red[1][tid >> 6] = part;
+        __syncthreads();
+        sum = sum * shrink + ((red[1][0] + red[1][1]) + (red[1][2] + red[1][3]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= shrink;
+        if (group < groups) {
+#pragma unroll 4
+            for (int k = group; k < n; k += groups) {
+                const float w = weight[k];
+                if (w != 0.0f) {                            // (NaN is not 0)
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(p.sums + ((i0 + k) * rows + row) * D + d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += x[e] * w;
+                }
+            }
+        }
+        __syncthreads();
     }
-    v = sum == 0.0f ? 0.0f : v / sum;
-    if (p.c.vdepth) v *= cache_doublings(p.c.vdepth[head / p.G * D + d]);
-    static_cast<elem_t<T>*>(p.Y)[t * p.ldy + head * p.hdy + d] = float_to_elem<T>(v);
-    if (p.lse && d == 0) p.lse[row] = sum > 0.0f ? (all + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : (sum == 0.0f ? -__builtin_inff() : sum);
+    partial[tid] = v;
+    __syncthreads();
+    if (tid >= lanes) return;
+    for (int g = 1; g < groups; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += partial[g * lanes + tid][e];
+    elem_t<T>* y = static_cast<elem_t<T>*>(p.Y) + t * p.ldy + head * p.hdy + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float o = sum == 0.0f ? 0.0f : v[e] / sum;
+        if (p.c.vdepth) o *= cache_doublings(p.c.vdepth[head / p.G * D + d + e]);
+        y[e] = float_to_elem<T>(o);
+    }
+    if (p.lse && tid == 0) p.lse[row] = sum > 0.0f ? (all + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : (sum == 0.0f ? -__builtin_inff() : sum);
 }
 
 struct AttentionPlan {
+    bool many;                              // rows: the kernel with tiles of them
     int64_t tiles;
     int parts;
     int64_t chunk;
 };
 
-// Parts of the positions where the tiles alone leave compute units idle.
-static AttentionPlan plan_attention(int64_t T, int64_t B, int64_t H, int64_t Hq, int64_t most, int64_t window) {
-    const int64_t G = Hq / H, tiles = T * G / 16 + B, range = window > 0 && window + T < most ? window + T : most;
-    AttentionPlan a{tiles, 1, 0};
-    const int64_t want = ceil_div(8 * (int64_t)compute_units(), tiles * H), can = ceil_div(range, 32 * kAttendWaves * 2);
+// Which kernel, and parts of the positions where the tiles alone leave compute units idle.
+static AttentionPlan plan_attention(int64_t T, int64_t B, int64_t H, int64_t Hq, int64_t D, int64_t most, int64_t window) {
+    const int64_t G = Hq / H, cus = compute_units(), range = window > 0 && window + T < most ? window + T : most;
+    const bool many = T * G >= 48 * B;
+    const int64_t rows = !many ? 16 : D <= 128 ? 128 : 64, tiles = T * G / rows + B, per_cu = B < 4 ? 2 * B : 8;
+    AttentionPlan a{many, tiles, 1, 0};
+    const int64_t want = ceil_div(per_cu * cus, tiles * H), can = ceil_div(range, 32 * kAttendWaves * 2), fit = ((int64_t)48 << 20) / (T * Hq * (D + 2) * 4);
     int64_t parts = want < can ? want : can;
+    parts = parts < fit ? parts : fit;
     if (parts > 1) {
         a.chunk = round_up(ceil_div(range + 31, parts), 32 * kAttendWaves);
         parts = ceil_div(range + 31, a.chunk);
@@ -451,14 +943,25 @@ static AttentionPlan plan_attention(int64_t T, int64_t B, int64_t H, int64_t Hq,
 }
 
 size_t cache_attention_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hq, int64_t D, int64_t most, int64_t window) {
-    const AttentionPlan a = plan_attention(T, B, H, Hq, most, window);
+    const AttentionPlan a = plan_attention(T, B, H, Hq, D, most, window);
     return a.parts > 1 ? (size_t)a.parts * (size_t)(T * Hq) * (size_t)(D + 2) * 4 : 0;
 }
 
 template <Elem T, CacheFormat F, int D>
 static hipError_t run_attention(const Attention& p, const AttentionPlan& a, hipStream_t stream) {
-    const hipError_t e = launch_kernel(kTimeGemm, attend_rows_kernel<T, F, D>, dim3((unsigned)a.tiles, (unsigned)p.c.H, (unsigned)p.parts),
-                                       dim3(kAttendWaves * 64), 0, stream, p);
+    const dim3 grid((unsigned)(a.tiles * p.c.H * p.parts));
+    hipError_t e;
+    if (a.many) {
+        constexpr int LDS = AttendTile<T, D>::LDS;
+        if constexpr (LDS > 65536) {
+            static std::atomic<bool> allowed[kMaxDevices];
+            e = allow_lds(reinterpret_cast<const void*>(&attend_tile_kernel<T, F, D>), LDS, allowed);
+            if (e != hipSuccess) return e;
+        }
+        e = launch_kernel(kTimeGemm, attend_tile_kernel<T, F, D>, grid, dim3(256), (unsigned)LDS, stream, p);
+    } else {
+        e = launch_kernel(kTimeGemm, attend_rows_kernel<T, F, D>, grid, dim3(kAttendWaves * 64), 0, stream, p);
+    }
     if (e != hipSuccess || p.parts == 1) return e;
     return launch_kernel(0, attend_join_kernel<T>, dim3((unsigned)((int64_t)p.s.T * p.Hq)), dim3(256), 0, stream, p);
 }
@@ -481,9 +984,11 @@ static hipError_t run_attention_of(const Attention& p, const AttentionPlan& a, h
 hipError_t launch_cache_attention(const void* Q, int type, int64_t ldq, int64_t hdq, int Hq, const Sequences& s, int64_t most, int format,
                                   const Cache& c, float scale, int64_t window, void* Y, int64_t ldy, int64_t hdy, float* lse,
                                   void* workspace, hipStream_t stream) {
-    const AttentionPlan a = plan_attention(s.T, s.B, c.H, Hq, most, window);
+    const AttentionPlan a = plan_attention(s.T, s.B, c.H, Hq, c.D, most, window);
     float* sums = static_cast<float*>(workspace);
-    Attention p{c, s, Q, ldq, hdq, Hq, Hq / c.H, scale * 1.44269504088896341f, window, most, Y, ldy, hdy, lse, a.parts, a.chunk, sums, nullptr};
+    const int64_t held = most < c.cols * c.P ? most : c.cols * c.P;
+    Attention p{c, s, Q, ldq, hdq, Hq, Hq / c.H, scale * 1.44269504088896341f, (int)(window < 0x7FFFFFFF ? window : 0), (int)held,
+                (unsigned)(((uint64_t)1 << 32) / c.P) + 1, Y, ldy, hdy, lse, (int)a.tiles, a.parts, (int)a.chunk, sums, nullptr};
     if (a.parts > 1) p.stats = sums + (int64_t)a.parts * s.T * Hq * c.D;
     const bool mx = format == (int)CacheFormat::mx4;
     switch (static_cast<Elem>(type)) {

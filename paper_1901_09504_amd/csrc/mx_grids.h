@@ -27,7 +27,8 @@ __device__ __forceinline__ unsigned mx_scale_byte(unsigned magnitude) {
     return e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
 }
 
-__device__ __forceinline__ float mx_scale_value(unsigned byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+// The power of two of a scale byte as the conversions take it: they look at the exponent field alone, 0 for 2^-127 and 255 for NaN.
+__device__ __forceinline__ float mx_scale_value(unsigned byte) { return __uint_as_float(byte << 23); }
 
 // Codes of eight values, first in the low bits: the hardware's conversion, nearest, halves to the even code, at most 6.
 __device__ __forceinline__ unsigned mx_codes8(const float (&v)[8], float scale) {
@@ -53,7 +54,7 @@ __device__ __forceinline__ void mx_values8(unsigned codes, unsigned byte, float 
                 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
     const float all[8] = {a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = byte == 255u ? __uint_as_float(0x7FC00000u) : all[e];
+    for (int e = 0; e < 8; ++e) v[e] = all[e];
 #else
     (void)codes;
     (void)byte;

@@ -1178,10 +1178,10 @@ int ocs_cache_read(void* K, int64_t ldk, int64_t hdk, void* V, int64_t ldv, int6
     return cache_rows(false, K, ldk, hdk, V, ldv, hdv, type, T, cu, starts, B, format, c, stream);
 }
 
-// What bounds the tiles of a launch: 256 lanes for every 16 rows of a head.
+// What bounds a launch: 256 lanes for every 16 rows of a head.
 static bool attention_fits(int64_t T, int64_t B, int64_t heads, int64_t query_heads) {
     return heads >= 1 && query_heads >= heads && query_heads % heads == 0 && query_heads <= 1 << 20 &&
-           (double)T * (query_heads / heads) / 16 + B < 1 << 23;
+           (double)T * query_heads / 16 + (double)B * heads < 16e6;
 }
 
 size_t ocs_cache_attention_workspace_bytes(int64_t T, int64_t B, int heads, int query_heads, int D, int64_t most, int64_t window) {
