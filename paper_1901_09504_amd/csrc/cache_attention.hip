@@ -42,8 +42,7 @@ __device__ __forceinline__ unsigned bf16_pair(float lo, float hi) {         // o
 }
 
 __device__ __forceinline__ unsigned bf16_rounded(float lo, float hi) {
-    const bf16x2 r = {(__bf16)lo, (__bf16)hi};
-    return __builtin_bit_cast(unsigned, r);
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
 }
 
 // v[0 .. 7] as N sets of bf16 numbers that add up to them
@@ -177,6 +176,43 @@ __device__ __forceinline__ PageAt page_of(const Attention& p, const int32_t* tab
         at += p.c.P;
     }
     return PageAt{j < end ? table[col] : -1, at};
+}
+
+// The same for tiles of many rows, those that see most first: what a workgroup takes goes with the positions that its rows see, and one that
+// begins last should not be the longest.  A sequence's tiles go backwards; up to 64 sequences go by length.  (Prompts of 512 to 1501 tokens in
+// sequences of 1501 to 6001, 8 heads: in the order given 428 us, so 345.)
+template <int ROWS>
+__device__ __forceinline__ int long_tile_sequence(const Attention& p, int tile, int* row0, int* first, int* tokens) {
+    const int lane = (int)threadIdx.x & 63;
+    int b, left;                                            // tiles of b behind this one
+    if (p.s.B <= 64) {
+        int t0 = 0, n = 0, tiles = 0, before = 0;
+        int64_t length = 0;
+        if (lane < p.s.B) {
+            t0 = clamp_int(p.s.cu[lane], 0, p.s.T);
+            n = clamp_int(p.s.cu[lane + 1], t0, p.s.T) - t0;
+            tiles = (n * p.G + ROWS - 1) / ROWS;
+            length = (int64_t)p.s.starts[lane] + n;
+        }
+        const int size = (int)(length < 0 ? 0 : length < 0x7FFFFFFF ? length : 0x7FFFFFFF);
+        for (int j = 0; j < p.s.B; ++j) {
+            const int other = __builtin_amdgcn_readlane(size, j), more = __builtin_amdgcn_readlane(tiles, j);
+            if (other > size || (other == size && j < lane)) before += more;
+        }
+        const uint64_t which = __ballot(tile >= before && tile < before + tiles);
+        if (which == 0) return -1;
+        b = __builtin_ctzll(which);
+        *first = __builtin_amdgcn_readlane(t0, b);
+        *tokens = __builtin_amdgcn_readlane(n, b);
+        left = __builtin_amdgcn_readlane(before + tiles, b) - 1 - tile;
+    } else {
+        int r = 0;
+        b = tile_sequence<ROWS>(p, tile, &r, first, tokens);
+        if (b < 0) return -1;
+        left = (*tokens * p.G + ROWS - 1) / ROWS - 1 - r / ROWS;
+    }
+    *row0 = left * ROWS;
+    return b;
 }
 
 // How far above the softmax's reference a score may be before the sums are put on a new one (in powers of two): the reference then hardly
@@ -564,7 +600,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = (int)(blockIdx.x % (unsigned)p.c.H), part = (int)(blockIdx.x / (unsigned)p.c.H / (unsigned)p.tiles);
     int row0 = 0, t0 = 0, n = 0;
-    const int b = __builtin_amdgcn_readfirstlane(tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles), &row0, &t0, &n));
+    const int b = __builtin_amdgcn_readfirstlane(long_tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles), &row0, &t0, &n));
     if (b < 0) return;
     row0 = __builtin_amdgcn_readfirstlane(row0);
     t0 = __builtin_amdgcn_readfirstlane(t0);
@@ -626,32 +662,41 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
         float kstep, vstep;                                 // 4 bits: the scale bytes' numbers
     };
     Codes codes[LOADS];
-    PageAt at[LOADS];
+    int page[LOADS], row_of[LOADS];
+    bool there[LOADS];
     const int32_t* table = p.c.table + b * p.c.ldt;
+    const unsigned pages = (unsigned)p.c.pages, page_rows = (unsigned)p.c.H * (unsigned)p.c.P;
+    const uint8_t* const keys = static_cast<const uint8_t*>(p.c.keys) + (int64_t)h * p.c.P * ROWB;
+    const uint8_t* const values = static_cast<const uint8_t*>(p.c.values) + (int64_t)h * p.c.P * ROWB;
+    const uint8_t* const kscales = static_cast<const uint8_t*>(p.c.kscales) + (int64_t)h * p.c.P * (MX ? D / 32 : 4);
+    const uint8_t* const vscales = static_cast<const uint8_t*>(p.c.vscales) + (int64_t)h * p.c.P * (MX ? D / 32 : 4);
     auto key_of = [&](int u) { return (tid + 256 * u) / (D / 16); };
     auto part_of = [&](int u) { return (tid + 256 * u) % (D / 16); };
-    auto there = [&](const PageAt& w) { return w.page >= 0 && w.page < p.c.pages; };
-    auto look_up = [&](int j0) {
+    auto look_up = [&](int j0) {                             // (positions behind the last repeat it)
 #pragma unroll
         for (int u = 0; u < LOADS; ++u)
-            if (tid + 256 * u < ITEMS) {
-                at[u] = page_of(p, table, j0 + (key_of(u) & ~15), end);
-                at[u].at += key_of(u) & 15;
+            if (ITEMS % 256 == 0 || tid + 256 * u < ITEMS) {
+                const int j = j0 + key_of(u) < end ? j0 + key_of(u) : end - 1;
+                int col = (int)__umulhi((unsigned)j, p.page_magic), at = j - col * p.c.P;
+                col -= at < 0;
+                row_of[u] = at < 0 ? at + p.c.P : at;
+                page[u] = table[col];
             }
     };
     auto load = [&]() {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u)
-            if (tid + 256 * u < ITEMS) {
-                const int64_t r = there(at[u]) ? ((int64_t)at[u].page * p.c.H + h) * p.c.P + at[u].at : (int64_t)h * p.c.P;
-                load_bytes<PIECE>(static_cast<const uint8_t*>(p.c.keys) + r * ROWB + part_of(u) * PIECE, codes[u].k);
-                load_bytes<PIECE>(static_cast<const uint8_t*>(p.c.values) + r * ROWB + part_of(u) * PIECE, codes[u].v);
+            if (ITEMS % 256 == 0 || tid + 256 * u < ITEMS) {
+                there[u] = (unsigned)page[u] < pages;
+                const uint64_t r = (uint64_t)(there[u] ? (unsigned)page[u] : 0u) * page_rows + (unsigned)row_of[u];
+                load_bytes<PIECE>(keys + r * ROWB + part_of(u) * PIECE, codes[u].k);
+                load_bytes<PIECE>(values + r * ROWB + part_of(u) * PIECE, codes[u].v);
                 if constexpr (MX) {
-                    codes[u].kstep = mx_scale_value(static_cast<const uint8_t*>(p.c.kscales)[r * (D / 32) + part_of(u) / 2]);
-                    codes[u].vstep = mx_scale_value(static_cast<const uint8_t*>(p.c.vscales)[r * (D / 32) + part_of(u) / 2]);
+                    codes[u].kstep = mx_scale_value(kscales[r * (D / 32) + part_of(u) / 2]);
+                    codes[u].vstep = mx_scale_value(vscales[r * (D / 32) + part_of(u) / 2]);
                 } else {
-                    codes[u].kstep = static_cast<const float*>(p.c.kscales)[r];
-                    codes[u].vstep = static_cast<const float*>(p.c.vscales)[r];
+                    codes[u].kstep = *reinterpret_cast<const float*>(kscales + r * 4);
+                    codes[u].vstep = *reinterpret_cast<const float*>(vscales + r * 4);
                 }
             }
     };
@@ -668,35 +713,33 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
                 }
             }
     };
-    auto store = [&](int j0, int buf) {                      // (of the positions whose pages are still in `at`)
+    // Scores get a key's factor, weights a value's.  A value that is no number is 0 here, so that it is nothing to rows that do not see it, and
+    // its key's factor is NaN: scores of rows that do are NaN, and so is what they come to.
+    auto store = [&](int buf) {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u)
-            if (tid + 256 * u < ITEMS) {
-                const int key = key_of(u), col = part_of(u), j = j0 + key;
+            if (ITEMS % 256 == 0 || tid + 256 * u < ITEMS) {
+                const int key = key_of(u), col = part_of(u);
                 u32x4 x[2];
                 numbers(codes[u].k, codes[u].kstep, x);
                 uint8_t* k = lds + (buf * KT + key) * KPITCH + col * 32;
                 *reinterpret_cast<u32x4*>(k) = x[0];
                 *reinterpret_cast<u32x4*>(k + 16) = x[1];
-                float vstep = codes[u].vstep, weight = 1.0f;
+                const bool number = (__float_as_uint(codes[u].vstep) & 0x7F800000u) != 0x7F800000u;
                 if constexpr (MX) {
-                    // a value that is no number, where not all rows see it: 0 here, and NaN as the weight's factor for those who do
-                    const bool all = there(at[u]) && j >= all_from && j < all_end && j < end;
-                    if (!all && __float_as_uint(vstep) == 0x7F800000u) {
-                        vstep = 1.0f;
-                        weight = __uint_as_float(0x7FC00000u);
-                    }
+#pragma unroll
+                    for (int e = 0; e < PIECE / 4; ++e) codes[u].v[e] = number ? codes[u].v[e] : 0u;
+                    numbers(codes[u].v, number ? codes[u].vstep : 1.0f, x);
                 } else {
-                    weight = vstep;
+                    numbers(codes[u].v, 1.0f, x);
                 }
-                numbers(codes[u].v, vstep, x);
                 uint8_t* v = lds + 2 * KT * KPITCH + (buf * KT + key) * VPITCH + col * 32;
                 *reinterpret_cast<u32x4*>(v) = x[0];
                 *reinterpret_cast<u32x4*>(v + 16) = x[1];
                 if (col == 0) {
-                    if constexpr (!MX) ksteps[buf][key] = codes[u].kstep * p.scale;
-                    vsteps[buf][key] = weight;
-                    if ((key & 15) == 0) there_of[buf][key >> 4] = there(at[u]);
+                    ksteps[buf][key] = number ? (MX ? p.scale : codes[u].kstep * p.scale) : __uint_as_float(0x7FC00000u);
+                    if constexpr (!MX) vsteps[buf][key] = number ? codes[u].vstep : 1.0f;
+                    if ((key & 15) == 0) there_of[buf][key >> 4] = there[u];
                 }
             }
     };
@@ -713,11 +756,11 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
         total[u] = 0.0f;
     }
     auto use = [&](int j0, int buf) {
-        bool whole = j0 >= all_from && j0 + KT <= all_end && j0 + KT <= end;
-        unsigned pages = 0;
+        unsigned groups = 0;                                // of 16 positions whose pages are there
 #pragma unroll
-        for (int m = 0; m < MT; ++m) pages |= (there_of[buf][m] ? 1u : 0u) << m;
-        whole = whole && pages == (1u << MT) - 1;
+        for (int m = 0; m < MT; ++m) groups |= (unsigned)there_of[buf][m] << m;
+        groups = __builtin_amdgcn_readfirstlane(groups);
+        const bool whole = j0 >= all_from && j0 + KT <= all_end && j0 + KT <= end && groups == (1u << MT) - 1;
         f32x4 s[MT][NT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
@@ -731,8 +774,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
 #pragma unroll
                     for (int e = N - 1; e >= 0; --e) s[m][u] = multiply_bf16(k, q[u][st][e], s[m][u]);
             }
-            f32x4 factor = {p.scale, p.scale, p.scale, p.scale};
-            if constexpr (!MX) factor = *reinterpret_cast<const f32x4*>(&ksteps[buf][16 * m + 4 * fq]);
+            const f32x4 factor = *reinterpret_cast<const f32x4*>(&ksteps[buf][16 * m + 4 * fq]);
 #pragma unroll
             for (int u = 0; u < NT; ++u)
 #pragma unroll
@@ -746,7 +788,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int j = j0 + 16 * m + 4 * fq + i;
-                        if (!(pages >> m & 1) || j >= end || (unsigned)(j - mine[u].from) >= (unsigned)mine[u].count) s[m][u][i] = -__builtin_inff();
+                        if (!(groups >> m & 1) || j >= end || (unsigned)(j - mine[u].from) >= (unsigned)mine[u].count) s[m][u][i] = -__builtin_inff();
                     }
         }
 #pragma unroll
@@ -780,13 +822,11 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
                     x[i] = __builtin_amdgcn_exp2f(s[m][u][i % 4] - base);
                     total[u] += x[i];
                 }
-                if (!MX || !whole) {
-                    const f32x4 a = *reinterpret_cast<const f32x4*>(&vsteps[buf][32 * kk + 4 * fq]), c = *reinterpret_cast<const f32x4*>(&vsteps[buf][32 * kk + 16 + 4 * fq]);
+                if constexpr (!MX) {
+                    const f32x4 f[2] = {*reinterpret_cast<const f32x4*>(&vsteps[buf][32 * kk + 4 * fq]),
+                                        *reinterpret_cast<const f32x4*>(&vsteps[buf][32 * kk + 16 + 4 * fq])};
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float f = i < 4 ? a[i % 4] : c[i % 4];
-                                x[i] = whole || x[i] != 0.0f ? x[i] * f : 0.0f;
-                    }
+                    for (int i = 0; i < 8; ++i) x[i] *= f[i / 4][i % 4];
                 }
                 bf16_sums<N>(x, w[u]);
             }
@@ -807,18 +847,18 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
     if (begin < end) {
         look_up(begin);
         load();
-        store(begin, 0);
-        if (begin + KT < end) look_up(begin + KT);
+        store(0);
+        look_up(begin + KT);
         __syncthreads();
         int buf = 0;
         for (int j = begin; j < end; j += KT, buf ^= 1) {
             const bool more = j + KT < end;
-            if (more) load();
-            if (j < wave_end && j + KT > wave_from) use(j, buf);
             if (more) {
-                store(j + KT, buf ^ 1);
-                if (j + 2 * KT < end) look_up(j + 2 * KT);
+                load();
+                look_up(j + 2 * KT);                        // (a table's entry has as long as the codes to come)
             }
+            if (j < wave_end && j + KT > wave_from) use(j, buf);
+            if (more) store(buf ^ 1);
             __syncthreads();
         }
     }

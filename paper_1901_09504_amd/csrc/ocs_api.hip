@@ -1128,9 +1128,9 @@ static int check_cache(int64_t T, const int32_t* cu, const int32_t* starts, int6
     if (T != 0 && B != 0 && (!cu || !starts || !c.table || !c.keys || !c.kscales || !c.values || !c.vscales)) return OCS_E_NULL;
     if (format != OCS_CACHE_INT8 && format != OCS_CACHE_MX4) return OCS_E_MODE;
     if (c.cols < 1 || c.ldt < c.cols || c.cols > (int64_t)1 << 31 || c.ldt > (int64_t)1 << 31) return OCS_E_SHAPE;
-    if (c.pages < 1 || c.pages > (int64_t)1 << 31 || c.P < 16 || c.P % 16 != 0 || c.P > 1 << 24 || c.H < 1 || c.H > 65535) return OCS_E_SHAPE;
+    if (c.pages < 1 || c.pages > 0x7FFFFFFF || c.P < 16 || c.P % 16 != 0 || c.P > 1 << 24 || c.H < 1 || c.H > 65535) return OCS_E_SHAPE;
     if (c.D < 32 || c.D > 256 || c.D % 32 != 0) return OCS_E_SHAPE;
-    if ((double)c.pages * c.H * c.P > 1e15) return OCS_E_SHAPE;
+    if ((double)c.pages * c.H * c.P > 1e15 || (int64_t)c.H * c.P > 0x7FFFFFFF) return OCS_E_SHAPE;
     if (!aligned(cu, 4) || !aligned(starts, 4) || !aligned(c.table, 4) || !aligned(c.kdepth, 4) || !aligned(c.vdepth, 4) ||
         !aligned(c.keys, 16) || !aligned(c.kscales, 16) || !aligned(c.values, 16) || !aligned(c.vscales, 16))
         return OCS_E_ALIGN;
