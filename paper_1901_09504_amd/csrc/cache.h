@@ -51,12 +51,28 @@ __device__ __forceinline__ int wave_count(int n, F at_most) {
     return lo;
 }
 
-// The sequence of token t (the same in the whole wave), or -1 behind the last.
-__device__ __forceinline__ int sequence_of(const Sequences& q, int t) {
-    int b;
-    if (q.T == q.B && q.cu[t] == t && q.cu[t + 1] == t + 1) b = t;              // a token each
-    else b = wave_count(q.B, [&](int i) { return q.cu[i + 1] <= t; });
-    return b < q.B && q.cu[b] <= t ? b : -1;
+// The sequence of token t (the same in the whole wave), or -1 behind the last, and the token's position in it.  Up to 64 sequences are looked
+// at once.
+__device__ __forceinline__ int sequence_of(const Sequences& q, int t, int64_t* position) {
+    int b, first, start;
+    if (q.B <= 64) {
+        const int lane = (int)threadIdx.x & 63, i = lane < q.B ? lane : q.B - 1;
+        const int from = q.cu[i], to = q.cu[i + 1], at = q.starts[i];
+        const uint64_t which = __ballot(lane < q.B && from <= t && t < to);
+        if (which == 0) return -1;
+        b = __builtin_ctzll(which);
+        first = __builtin_amdgcn_readlane(from, b);
+        start = __builtin_amdgcn_readlane(at, b);
+    } else {
+        if (q.T == q.B && q.cu[t] == t && q.cu[t + 1] == t + 1) b = t;          // a token each
+        else b = wave_count(q.B, [&](int i) { return q.cu[i + 1] <= t; });
+        if (b >= q.B) return -1;
+        first = q.cu[b];
+        start = q.starts[b];
+        if (first > t) return -1;
+    }
+    *position = (int64_t)start + ((int64_t)t - first);
+    return b;
 }
 
 // The row of position `pos` of sequence b in the pool, counted in [pages, H, P] for head 0, or -1 where there is none.

@@ -900,7 +900,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attention p) {
     __shared__ f32x4 partial[256];
     const int64_t rows = (int64_t)p.s.T * p.Hq, row = blockIdx.x;
     const int t = (int)(row / p.Hq), head = (int)(row % p.Hq), tid = (int)threadIdx.x, D = p.c.D;
-    if (sequence_of(p.s, t) < 0) return;
+    int64_t position;
+    if (sequence_of(p.s, t, &position) < 0) return;
     const int lanes = D / 4, groups = 256 / lanes, group = tid / lanes, d = tid % lanes * 4;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     float all = -__builtin_inff(), sum = 0.0f;

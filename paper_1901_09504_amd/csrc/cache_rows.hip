@@ -38,87 +38,130 @@ __device__ __forceinline__ void store8(elem_t<T>* y, const float (&v)[8]) {
     }
 }
 
-// LANES lanes a row, 64 / LANES rows a wave: rows 0 .. H - 1 of a token are its keys', H .. 2H - 1 its values'.
-template <Elem T, CacheFormat F, int LANES, bool WRITE>
+// LANES lanes a row, 64 / LANES rows a wave at a time, TIMES times: rows 0 .. H - 1 of a token are its keys', H .. 2H - 1 its values'.
+template <Elem T, CacheFormat F, int LANES, int TIMES, bool WRITE>
 __global__ __launch_bounds__(256) void cache_rows_kernel(CacheRows p, unsigned waves_per_token) {
+    constexpr int ROWS = 64 / LANES;
     const int lane = (int)threadIdx.x & 63, c = lane % LANES * 8, H = p.c.H, D = p.c.D;
     const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     const unsigned nth = wave / waves_per_token, t = p.t0 + nth;
     if (t >= (unsigned)p.s.T) return;
-    const int r = (int)(wave - nth * waves_per_token) * (64 / LANES) + lane / LANES;
-    const int b = sequence_of(p.s, (int)t);
+    const int first = (int)(wave - nth * waves_per_token) * (ROWS * TIMES) + lane / LANES;
+    int64_t position;
+    const int b = sequence_of(p.s, (int)t, &position);
     if (b < 0) return;
-    int64_t row = cache_row(p.c, b, (int64_t)p.s.starts[b] + ((int64_t)t - p.s.cu[b]));
+    const int64_t row = cache_row(p.c, b, position);
     if (WRITE && row < 0) return;
-    const bool live = r < 2 * H && c < D, values = r >= H;
-    const int h = values ? r - H : r;
-    const int64_t at = (row + (int64_t)h * p.c.P);
-    const int32_t* depth = values ? p.c.vdepth : p.c.kdepth;
-    void* codes = values ? p.c.values : p.c.keys;
-    void* scales = values ? p.c.vscales : p.c.kscales;
-    elem_t<T>* x = values ? static_cast<elem_t<T>*>(p.V) + t * p.ldv + h * p.hdv + c : static_cast<elem_t<T>*>(p.K) + t * p.ldk + h * p.hdk + c;
-    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+
+    struct Row {
+        bool live, values;
+        int h;
+        int64_t at;
+    };
+    auto row_of = [&](int i) {
+        const int r = first + i * ROWS;
+        Row w;
+        w.live = r < 2 * H && c < D;
+        w.values = r >= H;
+        w.h = w.values ? r - H : r;
+        w.at = row + (int64_t)w.h * p.c.P;
+        return w;
+    };
+    auto elements = [&](const Row& w) {
+        return w.values ? static_cast<elem_t<T>*>(p.V) + t * p.ldv + w.h * p.hdv + c : static_cast<elem_t<T>*>(p.K) + t * p.ldk + w.h * p.hdk + c;
+    };
+    auto scaled = [&](const Row& w, float (&v)[8], auto factor) {
+        const int32_t* depth = w.values ? p.c.vdepth : p.c.kdepth;
+        if (depth == nullptr) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= factor(depth[w.h * D + c + e]);
+    };
+    float v[TIMES][8];
     if constexpr (WRITE) {
-        unsigned big = 0;
-        if (live) {
-            load8<T>(x, v);
-            if (depth != nullptr) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= cache_halvings(depth[h * D + c + e]);
+        for (int i = 0; i < TIMES; ++i) {
+            const Row w = row_of(i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+            if (w.live) load8<T>(elements(w), v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < TIMES; ++i) {
+            const Row w = row_of(i);
+            if (w.live) scaled(w, v[i], cache_halvings);
+            unsigned big = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) big = mx_magnitude(v[i][e]) > big ? mx_magnitude(v[i][e]) : big;
+            unsigned whole = big;                                 // of the row; 4 bits: `big` of the block of 4 lanes
+#pragma unroll
+            for (int m = 1; m < LANES; m *= 2) {
+                const unsigned o = (unsigned)__shfl_xor((int)whole, m);
+                whole = o > whole ? o : whole;
+                if (m == 2) big = whole;
             }
-        }
+            if (!w.live) continue;
+            void* codes = w.values ? p.c.values : p.c.keys;
+            void* scales = w.values ? p.c.vscales : p.c.kscales;
+            if constexpr (F == CacheFormat::int8) {
+                const float thr = __uint_as_float(whole), inv = inv_step_of(thr, 127.0f);
+                unsigned q[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) big = mx_magnitude(v[e]) > big ? mx_magnitude(v[e]) : big;
-        unsigned whole = big;                                     // of the row; 4 bits: `big` of the block of 4 lanes
-#pragma unroll
-        for (int m = 1; m < LANES; m *= 2) {
-            const unsigned o = (unsigned)__shfl_xor((int)whole, m);
-            whole = o > whole ? o : whole;
-            if (m == 2) big = whole;
-        }
-        if (!live) return;
-        if constexpr (F == CacheFormat::int8) {
-            const float thr = __uint_as_float(whole), inv = inv_step_of(thr, 127.0f);
-            unsigned q[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q[e] = code_bits(v[e], inv, 127.0f);
-            *reinterpret_cast<u32x2*>(static_cast<int8_t*>(codes) + at * D + c) = u32x2{pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7])};
-            if (c == 0) static_cast<float*>(scales)[at] = __fdiv_rn(thr, 127.0f);
-        } else {
-            const bool finite = whole < 0x7F800000u;              // a row with NaN or an infinity: every scale 255
-            const unsigned byte = finite ? mx_scale_byte(big) : 255u;
-            *reinterpret_cast<unsigned*>(static_cast<uint8_t*>(codes) + at * (D / 2) + c / 2) = finite ? mx_codes8(v, mx_scale_value(byte)) : 0u;
-            if (c % kMxBlock == 0) static_cast<uint8_t*>(scales)[at * (D / kMxBlock) + c / kMxBlock] = (uint8_t)byte;
+                for (int e = 0; e < 8; ++e) q[e] = code_bits(v[i][e], inv, 127.0f);
+                *reinterpret_cast<u32x2*>(static_cast<int8_t*>(codes) + w.at * D + c) = u32x2{pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7])};
+                if (c == 0) static_cast<float*>(scales)[w.at] = __fdiv_rn(thr, 127.0f);
+            } else {
+                const bool finite = whole < 0x7F800000u;          // a row with NaN or an infinity: every scale 255
+                const unsigned byte = finite ? mx_scale_byte(big) : 255u;
+                *reinterpret_cast<unsigned*>(static_cast<uint8_t*>(codes) + w.at * (D / 2) + c / 2) = finite ? mx_codes8(v[i], mx_scale_value(byte)) : 0u;
+                if (c % kMxBlock == 0) static_cast<uint8_t*>(scales)[w.at * (D / kMxBlock) + c / kMxBlock] = (uint8_t)byte;
+            }
         }
     } else {
-        if (!live) return;
-        if (row >= 0) {
+        u32x2 q[TIMES];
+        float step[TIMES];
+#pragma unroll
+        for (int i = 0; i < TIMES; ++i) {
+            const Row w = row_of(i);
+            q[i] = u32x2{0u, 0u};
+            step[i] = 0.0f;
+            if (!w.live || row < 0) continue;                     // a position without a page: zeros
+            const void* codes = w.values ? p.c.values : p.c.keys;
+            const void* scales = w.values ? p.c.vscales : p.c.kscales;
             if constexpr (F == CacheFormat::int8) {
-                const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(codes) + at * D + c);
-                const float step = static_cast<const float*>(scales)[at];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)(q[e / 4] >> (8 * (e % 4))) * step;
+                q[i] = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(codes) + w.at * D + c);
+                step[i] = static_cast<const float*>(scales)[w.at];
             } else {
-                mx_values8(*reinterpret_cast<const unsigned*>(static_cast<const uint8_t*>(codes) + at * (D / 2) + c / 2),
-                           static_cast<const uint8_t*>(scales)[at * (D / kMxBlock) + c / kMxBlock], v);
-            }
-            if (depth != nullptr) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= cache_doublings(depth[h * D + c + e]);
+                q[i][0] = *reinterpret_cast<const unsigned*>(static_cast<const uint8_t*>(codes) + w.at * (D / 2) + c / 2);
+                q[i][1] = static_cast<const uint8_t*>(scales)[w.at * (D / kMxBlock) + c / kMxBlock];
             }
         }
-        store8<T>(x, v);
+#pragma unroll
+        for (int i = 0; i < TIMES; ++i) {
+            const Row w = row_of(i);
+            if (!w.live) continue;
+            if constexpr (F == CacheFormat::int8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = (float)(int8_t)(q[i][e / 4] >> (8 * (e % 4))) * step[i];
+            } else {
+                mx_values8(q[i][0], q[i][1], v[i]);
+            }
+            scaled(w, v[i], cache_doublings);
+            store8<T>(elements(w), v[i]);
+        }
     }
 }
 
 template <Elem T, CacheFormat F, bool WRITE>
 static hipError_t run_cache_rows(CacheRows p, hipStream_t stream) {
     const int lanes = p.c.D <= 32 ? 4 : p.c.D <= 64 ? 8 : p.c.D <= 128 ? 16 : 32;
-    const int64_t per_token = ceil_div(2 * (int64_t)p.c.H, 64 / lanes), most = (kMostLanes / 64 - 3) / per_token;   // tokens a launch
-    auto kernel = cache_rows_kernel<T, F, 32, WRITE>;
-    if (lanes == 4) kernel = cache_rows_kernel<T, F, 4, WRITE>;
-    if (lanes == 8) kernel = cache_rows_kernel<T, F, 8, WRITE>;
-    if (lanes == 16) kernel = cache_rows_kernel<T, F, 16, WRITE>;
+    // A token's rows by one wave, which looks its sequence and page up once for up to four times as many rows as it holds at a time; one time
+    // each while that leaves compute units without a wave (us, writing and reading FIGURES).
+    const int64_t at_once = ceil_div(2 * (int64_t)p.c.H, 64 / lanes), times = at_once * p.s.T >= 16 * compute_units() ? 4 : 1;
+    const int64_t per_token = ceil_div(at_once, times), most = (kMostLanes / 64 - 3) / per_token;   // tokens a launch
+    auto kernel = times == 1 ? cache_rows_kernel<T, F, 32, 1, WRITE> : cache_rows_kernel<T, F, 32, 4, WRITE>;
+    if (lanes == 4) kernel = times == 1 ? cache_rows_kernel<T, F, 4, 1, WRITE> : cache_rows_kernel<T, F, 4, 4, WRITE>;
+    if (lanes == 8) kernel = times == 1 ? cache_rows_kernel<T, F, 8, 1, WRITE> : cache_rows_kernel<T, F, 8, 4, WRITE>;
+    if (lanes == 16) kernel = times == 1 ? cache_rows_kernel<T, F, 16, 1, WRITE> : cache_rows_kernel<T, F, 16, 4, WRITE>;
     for (int64_t t0 = 0; t0 < p.s.T; t0 += most) {
         const int64_t n = p.s.T - t0 < most ? p.s.T - t0 : most;
         p.t0 = (int)t0;

@@ -75,54 +75,67 @@ __device__ __forceinline__ unsigned quad_max(unsigned v) {
 // 2^-d for a channel's halvings
 __device__ __forceinline__ float mx_halvings(int d) { return ldexpf(1.0f, -(d < 0 ? 0 : (d > 255 ? 255 : d))); }
 
-// Column that expanded column k copies, and its channel.
-__device__ __forceinline__ int mx_source(const MxRows& p, int k, int* channel) {
-    const int j = p.g == 1 ? k : k / p.g;
-    *channel = j;
-    if (p.chan_src == nullptr) return k;
-    int src = p.chan_src[j];
-    src = src < 0 ? 0 : (src >= p.C ? p.C - 1 : src);
-    return p.g == 1 ? src : src * p.g + (k - j * p.g);
-}
-
-// Columns k0 .. k0 + 7 of an expanded row, with their halvings; past its end zeros.  The first C * g columns are the row's own: whole
-// pieces of it are loaded as they are.
-template <Elem T, bool SCALED>
-__device__ __forceinline__ void mx_expanded8(const MxRows& p, const elem_t<T>* x, int k0, float (&v)[8]) {
+// The channels that expanded columns k0 .. k0 + 7 copy (g = 1) or the columns themselves: what is looked up ahead of the values.
+struct MxSources {
+    int at[8];
+};
+typedef int i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ MxSources mx_sources(const MxRows& p, int k0) {
     const int K = p.C * p.g, Ke = (p.C + p.s) * p.g;
-    if (k0 + 8 <= K) {
+    MxSources s;
+    if (p.g == 1 && k0 + 8 <= Ke) {
+        const i32x4_a4 a = *reinterpret_cast<const i32x4_a4*>(p.chan_src + k0), b = *reinterpret_cast<const i32x4_a4*>(p.chan_src + k0 + 4);
 #pragma unroll
-        for (int h = 0; h < 8 / kVec<T>; ++h) {
-            const u32x4 piece = load_piece<T>(x + k0 + h * kVec<T>);
-#pragma unroll
-            for (int e = 0; e < kVec<T>; ++e) v[h * kVec<T> + e] = piece_elem<T>(piece, e);
-        }
-        if constexpr (SCALED) {
-            if (p.g == 1) {
-                typedef int i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
-                const i32x4_a4 a = *reinterpret_cast<const i32x4_a4*>(p.chan_depth + k0), b = *reinterpret_cast<const i32x4_a4*>(p.chan_depth + k0 + 4);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= mx_halvings(e < 4 ? a[e & 3] : b[e & 3]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= mx_halvings(p.chan_depth[(k0 + e) / p.g]);
-            }
-        }
+        for (int e = 0; e < 8; ++e) s.at[e] = e < 4 ? a[e & 3] : b[e & 3];
     } else {
-        int src[8], channel[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int k = k0 + e < Ke ? k0 + e : Ke - 1;
-            src[e] = mx_source(p, k, &channel[e]);
-            if (k < K) src[e] = k;
+            s.at[e] = k < K ? (p.g == 1 ? k : k / p.g) : p.chan_src[p.g == 1 ? k : k / p.g];
         }
+    }
+    return s;
+}
+
+// Columns k0 .. k0 + 7 of an expanded row, with their halvings; past its end zeros.  The first C * g columns are the row's own: whole
+// pieces of it are loaded as they are.  Lanes behind them ask for their sources first, so that those come while the others' pieces do.
+template <Elem T, bool SCALED>
+__device__ __forceinline__ void mx_expanded8(const MxRows& p, const elem_t<T>* x, int k0, bool there, float (&v)[8]) {
+    const int K = p.C * p.g, Ke = (p.C + p.s) * p.g;
+    const bool own = there && k0 + 8 <= K, looked = there && !own && k0 < Ke;
+    MxSources s;
+    u32x4 pieces[8 / kVec<T>];
+    if (looked) s = mx_sources(p, k0);
+#pragma unroll
+    for (int h = 0; h < 8 / kVec<T>; ++h) {
+        pieces[h] = u32x4{0u, 0u, 0u, 0u};
+        if (own) pieces[h] = load_piece<T>(x + k0 + h * kVec<T>);
+    }
+    elem_t<T> copies[8];
+    if (looked) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[e] = 0.0f;
-            if (k0 + e < Ke) {
-                v[e] = elem_to_float<T>(x[src[e]]);
-                if constexpr (SCALED) v[e] *= mx_halvings(p.chan_depth[channel[e]]);
-            }
+            const int k = k0 + e < Ke ? k0 + e : Ke - 1;
+            int src = s.at[e];
+            src = src < 0 ? 0 : (src >= p.C ? p.C - 1 : src);
+            copies[e] = x[k < K ? k : (p.g == 1 ? src : src * p.g + k % p.g)];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = piece_elem<T>(pieces[e / kVec<T>], e % kVec<T>);
+    if (looked) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k0 + e < Ke ? elem_to_float<T>(copies[e]) : 0.0f;
+    }
+    if constexpr (SCALED) {
+        if (there && p.g == 1 && k0 + 8 <= Ke) {
+            const i32x4_a4 a = *reinterpret_cast<const i32x4_a4*>(p.chan_depth + k0), b = *reinterpret_cast<const i32x4_a4*>(p.chan_depth + k0 + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= mx_halvings(e < 4 ? a[e & 3] : b[e & 3]);
+        } else if (there) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (k0 + e < Ke) v[e] *= mx_halvings(p.chan_depth[p.g == 1 ? k0 + e : (k0 + e) / p.g]);
         }
     }
 }

@@ -8,16 +8,21 @@
 
 namespace ocs {
 
-// One lane per 8 columns; `blocks` blocks a row, the padding of codes and scales among them.
+// `blocks` blocks a row, the padding of codes and scales among them.
 template <Elem T, bool SCALED>
-__global__ __launch_bounds__(256) void mx_quantize_kernel(MxRows p, unsigned blocks) {
-    const unsigned at = blockIdx.x * 256 + threadIdx.x;     // (kMostLanes fits 32 bits)
-    const int64_t row = (at >> 2) / blocks;
-    if (row >= p.M) return;                      // whole groups of four
-    const int block = (int)((at >> 2) - (unsigned)row * blocks), part = (int)(at & 3);
-    const int64_t k0 = (int64_t)block * kMxBlock + part * 8;
-    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (k0 < (int64_t)(p.C + p.s) * p.g) mx_expanded8<T, SCALED>(p, static_cast<const elem_t<T>*>(p.X) + row * p.ldx, (int)k0, v);
+__global__ __launch_bounds__(256) void mx_quantize_kernel(MxRows p, unsigned blocks, unsigned magic) {
+    const unsigned at = (blockIdx.x * 256 + threadIdx.x) >> 2;      // (kMostLanes fits 32 bits)
+    const int part = (int)(threadIdx.x & 3);
+    unsigned r = __umulhi(at, magic);                               // at / blocks or one more: magic is 2^32 / blocks and one more, at below 2^30
+    int block = (int)(at - r * blocks);
+    if (block < 0) {
+        r -= 1;
+        block += (int)blocks;
+    }
+    const int64_t row = r, k0 = (int64_t)block * kMxBlock + part * 8;
+    if (row >= p.M) return;                                         // whole groups of four
+    float v[8];
+    mx_expanded8<T, SCALED>(p, static_cast<const elem_t<T>*>(p.X) + row * p.ldx, (int)k0, k0 < (int64_t)(p.C + p.s) * p.g, v);
     unsigned big = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) big = mx_magnitude(v[e]) > big ? mx_magnitude(v[e]) : big;
@@ -31,11 +36,12 @@ template <Elem T>
 static hipError_t run_mx_quantize(MxRows p, hipStream_t stream) {
     const int64_t codes = p.ldq / 16, blocks = codes > p.lds ? codes : p.lds, most = (kMostLanes - 255) / 4 / blocks;   // rows a launch
     if (most < 1) return hipErrorInvalidValue;
+    const unsigned magic = (unsigned)(((uint64_t)1 << 32) / blocks) + 1;       // (of one block: 2^32 and one more would not fit, but there are 16)
     for (int64_t left = p.M; left > 0;) {
         p.M = left < most ? left : most;
         const dim3 grid((unsigned)ceil_div(p.M * blocks * 4, 256));
-        const hipError_t e = p.chan_depth ? launch_kernel(kTimeSplitQuantize, mx_quantize_kernel<T, true>, grid, dim3(256), 0, stream, p, (unsigned)blocks)
-                                          : launch_kernel(kTimeSplitQuantize, mx_quantize_kernel<T, false>, grid, dim3(256), 0, stream, p, (unsigned)blocks);
+        const hipError_t e = launch_kernel(kTimeSplitQuantize, p.chan_depth ? mx_quantize_kernel<T, true> : mx_quantize_kernel<T, false>, grid,
+                                           dim3(256), 0, stream, p, (unsigned)blocks, magic);
         if (e != hipSuccess) return e;
         left -= p.M;
         p.X = static_cast<const elem_t<T>*>(p.X) + p.M * p.ldx;

@@ -344,8 +344,8 @@ __global__ __launch_bounds__(NW * 64) void mx_few_kernel(MxGemm p, MxRows rows) 
         for (int o = tid; o < total * 4; o += NT) {
             const int at = o >> 2, row = at / blocks, block = at - row * blocks, part = o & 3;
             const int k0 = block * kMxBlock + part * 8;
-            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-            if (k0 < (rows.C + rows.s) * rows.g) mx_expanded8<IN::type, false>(rows, static_cast<const elem_t<IN::type>*>(rows.X) + row * rows.ldx, k0, v);
+            float v[8];
+            mx_expanded8<IN::type, false>(rows, static_cast<const elem_t<IN::type>*>(rows.X) + row * rows.ldx, k0, k0 < (rows.C + rows.s) * rows.g, v);
             unsigned big = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) big = mx_magnitude(v[e]) > big ? mx_magnitude(v[e]) : big;
