@@ -485,9 +485,14 @@ hipError_t launch_qgemm_mx(const uint8_t* Xq, int64_t ldx, const uint8_t* Xs, in
     return hipErrorInvalidValue;
 }
 
+// 16 waves share the pass over the rows and K while every workgroup has a compute unit to itself, 8 where there are more (us, 8 waves / 16:
+// 1 x 3000 -> 6000 6.7 / 6.1, 1 x 4096 -> 4096 6.8 / 6.0, 16 x 250 -> 4000 6.1 / 5.1, 1 x 4096 -> 12000 9.6 / 12.1).
 template <Elem OUT, typename IN>
 static hipError_t run_forward_mx(const MxGemm& p, const MxRows& rows, hipStream_t stream) {
-    return ceil_div(p.N, 16) > compute_units() ? run_mx_few<1, 2, 8, OUT, IN>(p, rows, stream) : run_mx_few<1, 1, 8, OUT, IN>(p, rows, stream);
+    const int64_t cus = compute_units();
+    if (ceil_div(p.N, 16) <= cus) return run_mx_few<1, 1, 16, OUT, IN>(p, rows, stream);
+    if (ceil_div(p.N, 32) <= cus) return run_mx_few<1, 2, 16, OUT, IN>(p, rows, stream);
+    return run_mx_few<1, 2, 8, OUT, IN>(p, rows, stream);
 }
 
 template <Elem OUT>
@@ -506,9 +511,9 @@ hipError_t launch_forward_mx(const void* X, int type, int64_t ldx, int64_t M, in
     const int64_t Kexp = (int64_t)(C + s) * g;
     // One launch while every workgroup's pass over all rows takes its lanes two rounds at most; beyond, that costs more than a launch of its own
     // (us, calls one after the other, one launch / two: 1 x 250 -> 4000 4.0 / 6.5, 1 x 3000 -> 6000 6.7 / 8.0, 2 x 3000 -> 6000 7.4 / 8.2, 1 x 4096 ->
-    // 12000 10.1 / 12.5; 4 x 3000 -> 6000 8.6 / 8.5, 8 x 1000 -> 4000 7.7 / 6.5, 16 x 3000 -> 6000 17.9 / 9.1).  It reads X and W while outputs
-    // are being written.
-    if (apart && M <= 16 && M * ceil_div(Kexp, 256) <= 32 && N <= (int64_t)1 << 26) {
+    // 12000 10.1 / 12.5; 4 x 3000 -> 6000 8.6 / 8.5, 8 x 1000 -> 4000 7.7 / 6.5, 16 x 3000 -> 6000 17.9 / 9.1), nor with more than two workgroups
+    // a compute unit, which repeat it one after the other (1 x 1500 -> 33001 14.6 / 12.7).  It reads X and W while outputs are being written.
+    if (apart && M <= 16 && M * ceil_div(Kexp, 256) <= 32 && ceil_div(N, 32) <= 2 * (int64_t)compute_units()) {
         const MxGemm p{Xq, ldq, Xs, ldxs, Wq, ldw, Ws, ldws, (int)M, (int)N, (int)ceil_div(Kexp, 256), bias, Y, ldy, 0, 0};
         const MxRows rows{X, ldx, M, C, g, s, chan_src, nullptr, Xq, ldq, Xs, ldxs};
         switch (static_cast<Elem>(out_type)) {
