@@ -586,13 +586,14 @@ int ocs_forward_mx(const void *X, int type, int64_t M, int C, int g, int64_t ldx
  *
  * ocs_cache_write: keys and values [T, heads, D] of element type `type`, ld elements between tokens and hd between heads -> their rows
  *   of the pool; positions without a page are left out.  Two tokens of a call must not be the same row of the pool.
- *   A row with NaN or an infinity: 8 bits: a step that is not finite, 4 bits: scales 255.
+ *   A row with NaN or an infinity: 8 bits: a step that is not finite, 4 bits: scales 255 (scales 253 and 254 are never written).
  * ocs_cache_read: the rows as numbers, rounded once to `type`; positions without a page read as 0.
  * ocs_cache_attention: queries Q [T, query_heads, D] of the tokens, whose own rows the pool holds already; query head i reads
  *   head i / (query_heads / heads).  Over the positions j that a token at position p sees, j <= p, j > p - window (window 0: all),
  *   j < most, with a page that is there:
  *        s_j = scale * q . k_j,   Y[t, i] = sum exp(s_j) v_j / sum exp(s_j),   lse[t, i] = log sum exp(s_j)   (dense fp32, may be NULL).
- *   A token that sees none: Y 0, lse -inf.  What other positions' rows hold does not matter.  `most` is at least the longest sequence's
+ *   A token that sees none: Y 0, lse -inf.  One that sees a row with NaN (a value with scales from 253 on): NaN.  What positions' rows hold
+ *   that it does not see does not matter.  `most` is at least the longest sequence's
  *   positions, this call's among them.  Scores and sums in fp32; bf16 queries meet weights rounded to bf16, others finer ones.
  *   workspace: at least ocs_cache_attention_workspace_bytes() bytes, 256-byte aligned; it may be NULL where that is 0.  Needs no
  *   initialisation.

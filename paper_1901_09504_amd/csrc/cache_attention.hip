@@ -219,6 +219,10 @@ __device__ __forceinline__ int long_tile_sequence(const Attention& p, int tile, 
 // ever changes after the first positions, and weights stay far inside fp32's and bf16's range.
 constexpr float kSlack = 8.0f;
 
+// Scale bytes of values from here on are no numbers: 255 by definition, the two below it because 6 times their power of two is beyond
+// bf16 (no row that was written has them, but rubbish where nothing is seen may, and infinity times a weight of 0 is NaN).
+constexpr unsigned kNoNumber = 253;
+
 constexpr int kAttendWaves = 4;
 
 // The columns of a key that a lane of quarter `fq` multiplies in step s of the product: 8 from here on.  Steps go in groups, for which a
@@ -423,10 +427,10 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
                     vscale[i][e] = x.vscale[i][e];
                     highest = vscale[i][e] > highest ? vscale[i][e] : highest;
                 }
-            if (__any(highest == 255u)) {                   // 255: a NaN for those who see it, nothing for the others
+            if (__any(highest >= kNoNumber)) {              // a NaN for those who see it, nothing for the others
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (vscale[i][0] != 255u && (32 % DT == 0 || vscale[i][1] != 255u)) continue;
+                    if (vscale[i][0] < kNoNumber && (32 % DT == 0 || vscale[i][1] < kNoNumber)) continue;
                     if (sees >> i & 1) w[i] = __uint_as_float(0x7FC00000u);
                     vscale[i][0] = vscale[i][1] = 127u;
                 }
@@ -725,7 +729,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
                 uint8_t* k = lds + (buf * KT + key) * KPITCH + col * 32;
                 *reinterpret_cast<u32x4*>(k) = x[0];
                 *reinterpret_cast<u32x4*>(k + 16) = x[1];
-                const bool number = (__float_as_uint(codes[u].vstep) & 0x7F800000u) != 0x7F800000u;
+                const bool number = (__float_as_uint(codes[u].vstep) >> 23 & 0xFFu) < (MX ? kNoNumber : 0xFFu);
                 if constexpr (MX) {
 #pragma unroll
                     for (int e = 0; e < PIECE / 4; ++e) codes[u].v[e] = number ? codes[u].v[e] : 0u;

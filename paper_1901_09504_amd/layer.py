@@ -10,8 +10,9 @@ arithmetic happens here.
       forward(X[, threshold])      per batch: duplicate channels + quantize, GEMM (X1/X2, G1, G2)
   activation OCS (Eq. 4) with the channels chosen on the batch itself (Sec. 5.3):
       forward_act_ocs(W, X)        select on X, duplicate weights, halve + quantize X, GEMM
-  weight OCS with a grid per token and per output channel (TokenLayer), and what a language model's logits come
-      to (token_logprobs): log probabilities of given tokens, entropy, the most likely alternatives
+  weight OCS with a grid per token and per output channel (TokenLayer) or per block of 32 columns, in 4 bits (MxLayer), and what a
+      language model's logits come to (token_logprobs): log probabilities of given tokens, entropy, the most likely alternatives
+  keys and values of a language model's tokens on 8- or 4-bit grids, in pages, and attention over them (TokenCache)
 """
 import torch
 
@@ -317,7 +318,6 @@ class TokenLayer:
         self.K = self.C * self.g
         self.s = B.ocs_num_splits(self.C, r)
         self.Ke = (self.C + self.s) * self.g
-        self.ldq = B.ocs_padded_cols(self.Ke)
         self.bits_w, self.bits_x = int(bits_w), int(bits_x)
         self.clip_ratio_w, self.clip_ratio_x = float(clip_ratio_w), float(clip_ratio_x)
         self.out_dtype, self.device = out_dtype, device
@@ -326,8 +326,7 @@ class TokenLayer:
         self.split_src = torch.empty(max(self.s, 1), **i32)
         self.chan_src = torch.empty(E, **i32)
         self.chan_depth = torch.empty(E, **i32)
-        self.Wq = torch.empty((self.N, self.ldq), dtype=torch.int8, device=device)
-        self.step_w = torch.empty(self.N, dtype=torch.float32, device=device)
+        self._new_weights()
         self.bias = None
         if self.s == 0:                                     # what a selection of none would write
             torch.arange(E, out=self.chan_src)
@@ -341,14 +340,25 @@ class TokenLayer:
         if max_rows:
             self._ensure_rows(max_rows)
 
+    def _new_weights(self):
+        self.ldq = B.ocs_padded_cols(self.Ke)
+        self.Wq = torch.empty((self.N, self.ldq), dtype=torch.int8, device=self.device)
+        self.step_w = torch.empty(self.N, dtype=torch.float32, device=self.device)
+
+    def _new_rows(self, M):
+        self.Xq = torch.empty((M, self.ldq), dtype=torch.int8, device=self.device)
+        self.step_x = torch.empty(M, dtype=torch.float32, device=self.device)
+
     def _ensure_rows(self, M):
         if M > self._rows:
-            self.Xq = torch.empty((M, self.ldq), dtype=torch.int8, device=self.device)
-            self.step_x = torch.empty(M, dtype=torch.float32, device=self.device)
+            self._new_rows(M)
             self.Y = torch.empty((M, self.N), dtype=self.out_dtype, device=self.device)
             self._rows = M
             self._rows_from = torch.cuda.current_stream()
             self._streams.clear()
+
+    def _tensors(self):
+        return (self.split_src, self.chan_src, self.chan_depth, self.Wq, self.step_w, self.bias, self.Xq, self.step_x, self.Y)
 
     def _use_on_current_stream(self):
         """Before work on the current stream: the buffers may be memory that another stream's earlier work is not done with, and may be
@@ -357,7 +367,7 @@ class TokenLayer:
         if not torch.cuda.is_current_stream_capturing():    # (a capture begins with the device idle)
             for other in {self._weights_from, self._rows_from} - {stream}:
                 stream.wait_stream(other)
-        for t in (self.split_src, self.chan_src, self.chan_depth, self.Wq, self.step_w, self.bias, self.Xq, self.step_x, self.Y):
+        for t in self._tensors():
             if t is not None:
                 t.record_stream(stream)
         self._streams.add(stream.cuda_stream)
@@ -381,8 +391,15 @@ class TokenLayer:
         if self.s:
             ws = B.alloc_workspace(self.N, self.K, self.device)
             B.ocs_select_channels(W, self.N, self.C, self.g, ldw, self.s, self.split_src, self.chan_src, self.chan_depth, None, ws)
+        self._put_weights(W, ldw)
+
+    def _put_weights(self, W, ldw):
         B.ocs_split_quantize_rows(W, self.N, self.C, self.g, ldw, self.chan_src, self.chan_depth if self.s else None, self.s,
                                   self.bits_w, self.clip_ratio_w, self.Wq, self.ldq, self.step_w)
+
+    def _put_batch(self, X, M, ldx):
+        B.ocs_forward_rows(X, M, self.C, self.g, ldx, self.chan_src, self.s, self.bits_x, self.clip_ratio_x, self.Xq, self.ldq, self.step_x,
+                           self.Wq, self.ldq, self.N, self.bits_w, self.step_w, self.bias, self.Y, self.N)
 
     def forward(self, X, stream=None):
         """X [M, C*g] in fp32, bf16 or fp16 -> Y [M, N] in out_dtype (M = 0 included), the layer's own buffer: the next call
@@ -402,10 +419,168 @@ class TokenLayer:
             self._use_on_current_stream()
         if raw and torch._C._cuda_isCurrentStreamCapturing():   # (the null stream is never captured)
             self._hold_for_graph()
-        B.ocs_forward_rows(X, M, self.C, self.g, X.stride(0) if M > 1 else self.K, self.chan_src, self.s, self.bits_x,
-                           self.clip_ratio_x, self.Xq, self.ldq, self.step_x, self.Wq, self.ldq, self.N, self.bits_w, self.step_w,
-                           self.bias, self.Y, self.N)
+        self._put_batch(X, M, X.stride(0) if M > 1 else self.K)
         return self.Y[:M]
+
+
+class MxLayer(TokenLayer):
+    """The layer of Eq. 3 on microscaled 4-bit grids, one per 32 columns of a token's row and of an output channel's: weights and
+    activations of 17 bits for 4 values.  step_w and step_x are scale bytes, a row each.  Streams, graphs and the buffers' life as TokenLayer's."""
+
+    def __init__(self, N, C, r, g=1, out_dtype=torch.float32, max_rows=None, device="cuda"):
+        super().__init__(N, C, r, g, bits_w=4, bits_x=4, out_dtype=out_dtype, max_rows=max_rows, device=device)
+
+    def _new_weights(self):
+        self.ldq, self.lds = B.ocs_mx_code_pitch(self.Ke), B.ocs_mx_scale_pitch(self.Ke)
+        self.Wq = torch.empty((self.N, self.ldq), dtype=torch.uint8, device=self.device)
+        self.step_w = torch.empty((self.N, self.lds), dtype=torch.uint8, device=self.device)
+
+    def _new_rows(self, M):
+        self.Xq = torch.empty((M, self.ldq), dtype=torch.uint8, device=self.device)
+        self.step_x = torch.empty((M, self.lds), dtype=torch.uint8, device=self.device)
+
+    def _put_weights(self, W, ldw):
+        B.ocs_split_quantize_mx(W, self.N, self.C, self.g, ldw, self.chan_src, self.chan_depth if self.s else None, self.s, self.Wq, self.ldq,
+                                self.step_w, self.lds)
+
+    def _put_batch(self, X, M, ldx):
+        B.ocs_forward_mx(X, M, self.C, self.g, ldx, self.chan_src, self.s, self.Xq, self.ldq, self.step_x, self.lds, self.Wq, self.ldq,
+                         self.step_w, self.lds, self.N, self.bias, self.Y, self.N)
+
+
+class TokenCache:
+    """Keys and values of sequences of tokens, quantized as they come into pages of a pool, and attention over them.
+
+    A sequence is a number 0 .. sequences - 1; it takes pages as it grows and gives them back when it is freed.  Which pages, and how many
+    positions each sequence has, is kept on the host, and every call sends what it needs of that to the device; a program that captures
+    its steps into graphs keeps the table and the positions on the device itself and makes the calls of `binding`.
+    key_depth, value_depth: int32 [heads, D], how often a channel is halved before its row's grid (outlier_depths gives them).
+    Calls run on the current stream; one on another stream than the last waits for that one's work.  Not to be captured: what a call sends
+    comes from the host."""
+
+    def __init__(self, sequences, pages, heads, D, page_rows=64, bits=8, key_depth=None, value_depth=None, device="cuda"):
+        assert bits in (8, 4)
+        self.sequences, self.pages, self.heads, self.D, self.page_rows = int(sequences), int(pages), int(heads), int(D), int(page_rows)
+        self.format = B.CACHE_INT8 if bits == 8 else B.CACHE_MX4
+        self.device = device
+        for depth in (key_depth, value_depth):
+            assert depth is None or (depth.is_cuda and depth.dtype == torch.int32 and depth.shape == (self.heads, self.D) and depth.is_contiguous())
+        self.key_depth, self.value_depth = key_depth, value_depth
+        shape = (self.pages, self.heads, self.page_rows)
+        codes = dict(dtype=torch.int8 if bits == 8 else torch.uint8, device=device)
+        width, scales = (self.D, dict(dtype=torch.float32, device=device)) if bits == 8 else (self.D // 2, dict(dtype=torch.uint8, device=device))
+        per_row = () if bits == 8 else (self.D // B.MX_BLOCK,)
+        self.keys, self.values = torch.empty(shape + (width,), **codes), torch.empty(shape + (width,), **codes)
+        self.key_scales, self.value_scales = torch.empty(shape + per_row, **scales), torch.empty(shape + per_row, **scales)
+        self.lengths = [0] * self.sequences
+        self.tables = [[] for _ in range(self.sequences)]
+        self.spare = list(range(self.pages - 1, -1, -1))
+        self._stream = torch.cuda.current_stream()          # the last call's
+
+    def _use_on_current_stream(self):
+        stream = torch.cuda.current_stream()
+        if stream != self._stream:
+            stream.wait_stream(self._stream)
+            for t in (self.keys, self.key_scales, self.values, self.value_scales, self.key_depth, self.value_depth):
+                if t is not None:
+                    t.record_stream(stream)
+            self._stream = stream
+
+    def _sequences(self, which, counts):
+        which = list(range(self.sequences)) if which is None else list(which)
+        assert all(0 <= b < self.sequences for b in which) and (counts is None or len(counts) == len(which))
+        return which
+
+    def free(self, sequence):
+        """Gives the sequence's pages back: it has no positions."""
+        self.spare += reversed(self.tables[sequence])
+        self.tables[sequence], self.lengths[sequence] = [], 0
+
+    def _on_device(self, which, counts, starts):
+        """Offsets, first positions and tables of a call's sequences, in one copy to the device."""
+        self._use_on_current_stream()
+        cols = max(1, max((len(self.tables[b]) for b in which), default=1))
+        n = len(which)
+        host = torch.full((2 * n + 1 + n * cols,), -1, dtype=torch.int32)
+        host[:n + 1] = torch.tensor([0] + list(counts)).cumsum(0)
+        host[n + 1:2 * n + 1] = torch.tensor(starts)
+        for i, b in enumerate(which):
+            at = 2 * n + 1 + i * cols
+            host[at:at + len(self.tables[b])] = torch.tensor(self.tables[b], dtype=torch.int32)
+        sent = host.to(self.device)
+        return sent[:n + 1], sent[n + 1:2 * n + 1], sent[2 * n + 1:].view(n, cols)
+
+    def _pool(self, table):
+        return (table, table.shape[1], table.stride(0), self.format, self.keys, self.key_scales, self.values, self.value_scales, self.pages,
+                self.page_rows, self.heads, self.D, self.key_depth, self.value_depth)
+
+    def _check_rows(self, x, counts, heads):
+        assert x.is_cuda and x.dim() == 3 and x.shape[1:] == (heads, self.D) and (x.stride(2) == 1 or x.numel() == 0) and x.shape[0] == sum(counts)
+
+    def append(self, K, V, counts, which=None):
+        """K, V [T, heads, D] in fp32, bf16 or fp16: the next counts[i] tokens of sequence which[i] (all of them in order if None), one
+        sequence after the other.  MemoryError where the pool has too few pages left; nothing is changed then."""
+        which = self._sequences(which, counts)
+        assert len(which) == len(set(which)) and all(n >= 0 for n in counts) and V.dtype == K.dtype
+        self._check_rows(K, counts, self.heads)
+        self._check_rows(V, counts, self.heads)
+        need = [-(-(self.lengths[b] + n) // self.page_rows) - len(self.tables[b]) for b, n in zip(which, counts)]
+        if sum(need) > len(self.spare):
+            raise MemoryError(f"{sum(need)} pages wanted, {len(self.spare)} left")
+        for b, n in zip(which, need):
+            self.tables[b] += [self.spare.pop() for _ in range(n)]
+        cu, starts, table = self._on_device(which, counts, [self.lengths[b] for b in which])
+        B.ocs_cache_write(K, K.stride(0), K.stride(1), V, V.stride(0), V.stride(1), K.shape[0], cu, starts, len(which), *self._pool(table))
+        for b, n in zip(which, counts):
+            self.lengths[b] += n
+
+    def read(self, which=None, dtype=torch.float32):
+        """(keys, values) [positions, heads, D] of the sequences, one after the other, as numbers."""
+        which = self._sequences(which, None)
+        counts = [self.lengths[b] for b in which]
+        K = torch.empty((sum(counts), self.heads, self.D), dtype=dtype, device=self.device)
+        V = torch.empty_like(K)
+        if which:
+            cu, starts, table = self._on_device(which, counts, [0] * len(which))
+            B.ocs_cache_read(K, K.stride(0), K.stride(1), V, V.stride(0), V.stride(1), K.shape[0], cu, starts, len(which), *self._pool(table))
+        return K, V
+
+    def attend(self, Q, counts, which=None, scale=None, window=0, with_lse=False):
+        """Q [T, query_heads, D]: queries of the last counts[i] tokens of sequence which[i], which the cache holds already.  -> Y like Q, and
+        with with_lse the logarithm of the sums of exponentials, fp32 [T, query_heads].  scale: 1 / sqrt(D) if None; window: how many
+        positions, its own among them, a token sees (0: all)."""
+        which = self._sequences(which, counts)
+        assert all(0 <= n <= self.lengths[b] for n, b in zip(counts, which)) and Q.dim() == 3
+        query_heads = Q.shape[1]
+        self._check_rows(Q, counts, query_heads)
+        Y = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device) if with_lse else None
+        if which and Q.shape[0]:
+            most = max(self.lengths[b] for b in which)
+            cu, starts, table = self._on_device(which, counts, [self.lengths[b] - n for n, b in zip(counts, which)])
+            need = B.ocs_cache_attention_workspace_bytes(Q.shape[0], len(which), self.heads, query_heads, self.D, most, window)
+            ws = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
+            B.ocs_cache_attention(Q, Q.stride(0), Q.stride(1), query_heads, Q.shape[0], cu, starts, len(which), most, *self._pool(table),
+                                  self.D ** -0.5 if scale is None else scale, window, Y, Y.stride(0), Y.stride(1), lse, ws)
+        return (Y, lse) if with_lse else Y
+
+
+def outlier_depths(rows, r):
+    """How often each channel of each head is halved, int32 [heads, D], for rows [T, heads, D] such as a cache is to hold: the selection of
+    Sec. 3.4 on every head, ceil(r * D) splits; a channel that it splits is halved as often as its deepest copy."""
+    T, heads, D = rows.shape
+    s = B.ocs_num_splits(D, r)
+    depths = torch.zeros((heads, D), dtype=torch.int32, device=rows.device)
+    if s == 0:
+        return depths
+    i32 = dict(dtype=torch.int32, device=rows.device)
+    split_src, chan_src, chan_depth = torch.empty(s, **i32), torch.empty(D + s, **i32), torch.empty(D + s, **i32)
+    ws = B.alloc_workspace(T, D, rows.device)
+    for h in range(heads):
+        x = rows[:, h].float().contiguous()
+        B.ocs_select_channels(x, T, D, 1, D, s, split_src, chan_src, chan_depth, None, ws)
+        depths[h].scatter_reduce_(0, chan_src.long(), chan_depth, "amax")
+    return depths
 
 
 def token_logprobs(logits, tokens=None, top_k=0, stream=None):

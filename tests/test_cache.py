@@ -28,7 +28,7 @@ def _gpu():
 class Pool:
     """Pages full of rubbish that is no number, a table with every sequence's pages scattered over them, and where it is on the host."""
 
-    def __init__(self, fmt, held, H, D, P, seed=0, halved=False, spare=3, rubbish=True):
+    def __init__(self, fmt, held, H, D, P, seed=0, halved=False, spare=3):
         rng = np.random.default_rng(seed)
         need = [-(-L // P) for L in held]
         self.fmt, self.H, self.D, self.P, self.pages, self.held = fmt, H, D, P, sum(need) + spare, held
@@ -44,9 +44,11 @@ class Pool:
         self.codes = [torch.randint(-128 if fmt == INT8 else 0, 128 if fmt == INT8 else 256, shape + (width,), dtype=dtype,
                                     generator=torch.Generator().manual_seed(seed + i)).cuda() for i in (1, 2)]
         if fmt == INT8:
-            self.scales = [torch.full(shape, torch.nan, device="cuda") for _ in range(2)]
+            rubbish = torch.tensor([torch.nan, torch.inf, -torch.inf, 3e38])
+            self.scales = [rubbish[torch.randint(0, 4, shape, generator=torch.Generator().manual_seed(seed + i))].cuda() for i in (3, 4)]
         else:
-            self.scales = [torch.full(shape + per, 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+            self.scales = [torch.randint(253, 256, shape + per, dtype=torch.uint8, generator=torch.Generator().manual_seed(seed + i)).cuda()
+                           for i in (3, 4)]
         self.depth = [torch.from_numpy(rng.integers(0, 4, (H, D)).astype(np.int32)).cuda() if halved else None for _ in range(2)]
 
     def args(self, table=None):
@@ -462,3 +464,86 @@ def test_a_run_of_generation_with_its_layers_in_a_graph(fmt):
         step(eager, torch.tensor([n + i for n in n0], dtype=torch.int32, device="cuda"), want, eager_args)
         assert torch.equal(got, want), i
     assert starts.tolist() == [n + steps for n in n0]
+
+
+# ---- the cache that keeps its pages ----------------------------------------------------------
+
+def _pool_of(cache):
+    """The tests' view of a TokenCache's sequences."""
+    pool = Pool.__new__(Pool)
+    pool.fmt, pool.H, pool.D, pool.P, pool.pages = cache.format, cache.heads, cache.D, cache.page_rows, cache.pages
+    pool.held = list(cache.lengths)
+    pool.table = np.full((cache.sequences, max(1, max(len(t) for t in cache.tables))), -1, dtype=np.int32)
+    for b, t in enumerate(cache.tables):
+        pool.table[b, :len(t)] = t
+    pool.codes, pool.scales, pool.depth = [cache.keys, cache.values], [cache.key_scales, cache.value_scales], [cache.key_depth, cache.value_depth]
+    return pool
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_sequences_come_grow_and_go(bits):
+    from paper_1901_09504_amd.layer import TokenCache, outlier_depths
+
+    H, Hq, D = 2, 6, 64
+    sample = random_rows(100, H, D, F32, 5)
+    depths = outlier_depths(sample, 0.1)
+    assert depths.shape == (H, D) and int(depths.max()) >= 1 and bool((depths[:, 11::11] >= 0).all())
+    cache = TokenCache(3, 12, H, D, page_rows=16, bits=bits, key_depth=depths)
+    seed = 0
+    for which, counts, freed in (([0, 2], [20, 5], None), (None, [1, 0, 1], None), ([1], [40], None), ([0, 1, 2], [1, 1, 1], 1), ([1, 0], [17, 30], None)):
+        seq = [0, 1, 2] if which is None else which
+        k, v, q = (random_rows(sum(counts), h, D, BF16, seed + i) for i, h in enumerate((H, H, Hq)))
+        seed += 3
+        cache.append(k, v, counts, which)
+        y, lse = cache.attend(q, counts, which, with_lse=True)
+        pool = _pool_of(cache)
+        new = [0, 0, 0]
+        for b, n in zip(seq, counts):
+            new[b] = n
+        order = [sum(counts[:seq.index(b)]) + i for b in range(3) for i in range(new[b])]     # the tests' tokens are in the sequences' order
+        want, want_lse = check_attention(pool, new, Hq, BF16, q=q[order].contiguous())
+        # the call's parts may be others than the checked one's, whose table is wider: both are within the tolerance of the 64-bit values
+        assert bool(((y[order].float() - want.float()).abs() <= 2.0 ** -6 * want.float().abs() + 2.0 ** -6 * v.float().abs().max()).all())
+        assert bool(((lse[order] - want_lse).abs() <= 1e-4 * (1 + want_lse.abs())).all())
+        back = cache.read()
+        assert back[0].shape == (sum(cache.lengths), H, D)
+        if freed is not None:
+            cache.free(freed)
+            assert cache.lengths[freed] == 0
+    assert sorted(cache.spare + sum(cache.tables, [])) == list(range(12))
+    before = [list(t) for t in cache.tables], list(cache.lengths), list(cache.spare)
+    with pytest.raises(MemoryError):
+        cache.append(random_rows(200, H, D, BF16, 1), random_rows(200, H, D, BF16, 2), [200], [0])
+    assert before == ([list(t) for t in cache.tables], list(cache.lengths), list(cache.spare))
+    side = torch.cuda.Stream()
+    plain = cache.read()
+    with torch.cuda.stream(side):
+        again = cache.read()
+    side.synchronize()
+    assert torch.equal(plain[0], again[0]) and torch.equal(plain[1], again[1])
+
+
+def test_a_cache_refuses_what_does_not_fit():
+    from paper_1901_09504_amd.layer import TokenCache
+
+    cache = TokenCache(2, 4, 2, 32, page_rows=16)
+    k = random_rows(3, 2, 32, F32, 1)
+    for K, V, counts, which in ((k, k, [3], None), (k, k, [1, 1], None), (k, k, [1, 2], [0, 0]), (k, k.to(BF16), [1, 2], None), (k, k, [3], [2]),
+                                (k.cpu(), k, [1, 2], None), (k[:, :1], k, [1, 2], None), (k, k, [4, -1], None)):
+        with pytest.raises(AssertionError):
+            cache.append(K, V, counts, which)
+    cache.append(k, k, [1, 2])
+    with pytest.raises(AssertionError):
+        cache.attend(k, [2, 1])                                              # more queries than positions
+    with pytest.raises(AssertionError):
+        TokenCache(2, 4, 2, 32, bits=5)
+    with pytest.raises(B.OcsError):
+        TokenCache(2, 4, 2, 48).append(random_rows(2, 2, 48, F32, 1), random_rows(2, 2, 48, F32, 1), [1, 1])
+
+
+def test_scores_behind_a_quantized_cache():
+    from paper_1901_09504_amd import score
+
+    rows = score.run_cache(sequences=2, length=40, vocab=500)
+    assert [(b, r) for b, r, _, _ in rows] == [(32, 0.0), (8, 0.0), (8, 0.1), (4, 0.0), (4, 0.1)]
+    assert all(math.isfinite(p) and p >= 1 and 0 <= same <= 1 for _, _, p, same in rows)

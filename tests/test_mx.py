@@ -1,5 +1,7 @@
 """Microscaled 4-bit grids on the GPU: codes and scale bytes bit for bit against 64-bit definitions, products exactly where sums are whole
 numbers of 24 bits and within the roundings of a 32-bit sum elsewhere; edges, strides, alignments, NaN, streams and graphs."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -314,3 +316,73 @@ def test_streams_and_graphs(M):
         got = y.clone()
         torch.cuda.synchronize()
         assert torch.equal(got, forward(x, C, 1, None, 0, wq, ws, N, None, F32)[2])
+
+
+# ---- the layer that keeps its buffers --------------------------------------------------------
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("N,C,r,g", [(50, 64, 0.05, 1), (300, 500, 0.1, 1), (33, 40, 0.0, 9), (700, 1001, 0.02, 1), (1, 1, 0.0, 1)])
+def test_layers_from_their_weights(out, N, C, r, g):
+    """prepare_weights: channels chosen on the tensor, halved, put on their grids; forward: codes of the batch, product and bias."""
+    from oracle import ref
+    from paper_1901_09504_amd.layer import MxLayer
+
+    rng = np.random.default_rng(N + C)
+    W = rng.standard_normal((N, C * g)).astype(np.float32)
+    W[:, :g] *= 7
+    bias = torch.from_numpy(rng.standard_normal(N).astype(np.float32)).cuda()
+    layer = MxLayer(N, C, r, g, out_dtype=out)
+    layer.prepare_weights(torch.from_numpy(W).cuda(), bias)
+    s, K = layer.s, layer.Ke
+    if s:
+        sel = ref.split_weights(W, C, g, s)
+        src, depth = sel["chan_src"], sel["chan_depth"]
+        assert np.array_equal(G.host(layer.chan_src), src) and np.array_equal(G.host(layer.chan_depth), depth)
+    else:
+        src, depth = np.arange(C, dtype=np.int32), None
+    codes, scales = on_grids(expanded(torch.from_numpy(W), C, g, src, depth))
+    assert np.array_equal(G.host(layer.Wq), packed(codes, layer.ldq)) and np.array_equal(G.host(layer.step_w)[:, :scales.shape[1]], scales)
+    w = torch.from_numpy(numbers(codes, scales)).cuda()
+    for M in (1, 5, 40, 3, 0):
+        x = torch.from_numpy(rng.standard_normal((M, C * g)).astype(np.float32)).cuda()
+        y = layer.forward(x)
+        assert y.shape == (M, N) and y.dtype == out
+        if M:
+            codes, scales = on_grids(expanded(x, C, g, src, None))
+            v = torch.from_numpy(numbers(codes, scales)).cuda()
+            want, size = v @ w.t() + bias.double(), v.abs() @ w.abs().t() + bias.double().abs()
+            assert bool(((y.double() - want).abs() <= (K + 1) * 2.0 ** -23 * size + HALF_STEP[out] * want.abs()).all())
+
+
+def test_a_layer_on_streams_and_in_a_graph():
+    from paper_1901_09504_amd.layer import MxLayer
+
+    W = torch.randn((200, 300), device="cuda")
+    layer = MxLayer(200, 300, 0.05, max_rows=4)
+    layer.prepare_weights(W)
+    x = torch.randn((4, 300), device="cuda")
+    want = layer.forward(x).clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y = layer.forward(x, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = layer.forward(x)
+    big = torch.randn((50, 300), device="cuda")
+    for seed in range(3):
+        x.copy_(torch.randn((4, 300), generator=torch.Generator().manual_seed(seed)))
+        graph.replay()
+        got = y.clone()
+        layer.forward(big)                                                   # outgrows the buffers that the graph was captured with
+        torch.cuda.synchronize()
+        assert torch.equal(got, layer.forward(x))
+
+
+def test_scores_of_microscaled_layers():
+    from paper_1901_09504_amd import score
+
+    rows = score.run_mx(tokens=200, hidden=256, vocab=1000)
+    assert [(b, r) for b, r, _, _ in rows] == [(4, 0.0), (4, 0.05)]
+    assert all(math.isfinite(p) and p >= 1 and 0 <= same <= 1 for _, _, p, same in rows)
