@@ -137,20 +137,41 @@ __device__ __forceinline__ void load_bytes(const uint8_t* p, unsigned (&w)[(BYTE
     }
 }
 
-// Tiles of ROWS rows (token by token, a token's G heads together): sequence b's begin at cu[b] G / ROWS + b, which leaves each as many as
-// it needs.  Answers the tile's sequence, or -1, the tile's first row, the sequence's first token and how many it has.
+// A tile of rows (token by token, a token's G heads together): its sequence, or -1, its first row, and the sequence's first token, tokens and
+// first position.
+struct TileOf {
+    int b, row0, first, tokens;
+    int start;
+};
+
+// Tiles of ROWS rows: sequence b's begin at cu[b] G / ROWS + b, which leaves each as many as it needs.  (T G is below 2^28.)
 template <int ROWS>
-__device__ __forceinline__ int tile_sequence(const Attention& p, int tile, int* row0, int* first, int* tokens) {
-    auto begin = [&](int b) { return (int64_t)clamp_int(p.s.cu[b], 0, p.s.T) * p.G / ROWS + b; };
-    const int after = wave_count(p.s.B, [&](int i) { return begin(i) <= tile; });
-    if (after == 0) return -1;
-    const int b = after - 1, t0 = clamp_int(p.s.cu[b], 0, p.s.T);
-    *first = t0;
-    *tokens = clamp_int(p.s.cu[b + 1], t0, p.s.T) - t0;
-    const int64_t r = (tile - begin(b)) * ROWS;
-    if (r >= (int64_t)*tokens * p.G) return -1;
-    *row0 = (int)r;
-    return b;
+__device__ __forceinline__ TileOf tile_sequence(const Attention& p, int tile) {
+    TileOf t{-1, 0, 0, 0, 0};
+    int begin;
+    if (p.s.B <= 64) {                                      // all of them at one look
+        const int lane = (int)threadIdx.x & 63, i = lane < p.s.B ? lane : p.s.B - 1;
+        const int from = p.s.cu[i], to = p.s.cu[i + 1], at = p.s.starts[i];
+        const int t0 = clamp_int(from, 0, p.s.T), n = clamp_int(to, t0, p.s.T) - t0, mine = t0 * p.G / ROWS + i;
+        const int after = __popcll(__ballot(lane < p.s.B && mine <= tile));
+        if (after == 0) return t;
+        t.b = after - 1;
+        t.first = __builtin_amdgcn_readlane(t0, after - 1);
+        t.tokens = __builtin_amdgcn_readlane(n, after - 1);
+        t.start = __builtin_amdgcn_readlane(at, after - 1);
+        begin = __builtin_amdgcn_readlane(mine, after - 1);
+    } else {
+        const int after = wave_count(p.s.B, [&](int i) { return clamp_int(p.s.cu[i], 0, p.s.T) * p.G / ROWS + i <= tile; });
+        if (after == 0) return t;
+        t.b = after - 1;
+        t.first = clamp_int(p.s.cu[t.b], 0, p.s.T);
+        t.tokens = clamp_int(p.s.cu[t.b + 1], t.first, p.s.T) - t.first;
+        t.start = p.s.starts[t.b];
+        begin = t.first * p.G / ROWS + t.b;
+    }
+    t.row0 = (tile - begin) * ROWS;
+    if (t.row0 >= t.tokens * p.G) t.b = -1;
+    return t;
 }
 
 // What a query sees: `count` positions from `from` on (the cache holds fewer than 2^31).
@@ -182,37 +203,35 @@ __device__ __forceinline__ PageAt page_of(const Attention& p, const int32_t* tab
 // begins last should not be the longest.  A sequence's tiles go backwards; up to 64 sequences go by length.  (Prompts of 512 to 1501 tokens in
 // sequences of 1501 to 6001, 8 heads: in the order given 428 us, so 345.)
 template <int ROWS>
-__device__ __forceinline__ int long_tile_sequence(const Attention& p, int tile, int* row0, int* first, int* tokens) {
-    const int lane = (int)threadIdx.x & 63;
-    int b, left;                                            // tiles of b behind this one
-    if (p.s.B <= 64) {
-        int t0 = 0, n = 0, tiles = 0, before = 0;
-        int64_t length = 0;
-        if (lane < p.s.B) {
-            t0 = clamp_int(p.s.cu[lane], 0, p.s.T);
-            n = clamp_int(p.s.cu[lane + 1], t0, p.s.T) - t0;
-            tiles = (n * p.G + ROWS - 1) / ROWS;
-            length = (int64_t)p.s.starts[lane] + n;
-        }
-        const int size = (int)(length < 0 ? 0 : length < 0x7FFFFFFF ? length : 0x7FFFFFFF);
-        for (int j = 0; j < p.s.B; ++j) {
-            const int other = __builtin_amdgcn_readlane(size, j), more = __builtin_amdgcn_readlane(tiles, j);
-            if (other > size || (other == size && j < lane)) before += more;
-        }
-        const uint64_t which = __ballot(tile >= before && tile < before + tiles);
-        if (which == 0) return -1;
-        b = __builtin_ctzll(which);
-        *first = __builtin_amdgcn_readlane(t0, b);
-        *tokens = __builtin_amdgcn_readlane(n, b);
-        left = __builtin_amdgcn_readlane(before + tiles, b) - 1 - tile;
-    } else {
-        int r = 0;
-        b = tile_sequence<ROWS>(p, tile, &r, first, tokens);
-        if (b < 0) return -1;
-        left = (*tokens * p.G + ROWS - 1) / ROWS - 1 - r / ROWS;
+__device__ __forceinline__ TileOf long_tile_sequence(const Attention& p, int tile) {
+    if (p.s.B > 64) {
+        TileOf t = tile_sequence<ROWS>(p, tile);
+        t.row0 = (t.tokens * p.G + ROWS - 1) / ROWS * ROWS - ROWS - t.row0;
+        return t;
     }
-    *row0 = left * ROWS;
-    return b;
+    const int lane = (int)threadIdx.x & 63;
+    int t0 = 0, n = 0, tiles = 0, before = 0, start = 0;
+    if (lane < p.s.B) {
+        start = p.s.starts[lane];
+        t0 = clamp_int(p.s.cu[lane], 0, p.s.T);
+        n = clamp_int(p.s.cu[lane + 1], t0, p.s.T) - t0;
+        tiles = (n * p.G + ROWS - 1) / ROWS;
+    }
+    const int64_t length = (int64_t)start + n;
+    const int size = (int)(length < 0 ? 0 : length < 0x7FFFFFFF ? length : 0x7FFFFFFF);
+    for (int j = 0; j < p.s.B; ++j) {
+        const int other = __builtin_amdgcn_readlane(size, j), more = __builtin_amdgcn_readlane(tiles, j);
+        if (other > size || (other == size && j < lane)) before += more;
+    }
+    const uint64_t which = __ballot(tile >= before && tile < before + tiles);
+    TileOf t{-1, 0, 0, 0, 0};
+    if (which == 0) return t;
+    t.b = __builtin_ctzll(which);
+    t.first = __builtin_amdgcn_readlane(t0, t.b);
+    t.tokens = __builtin_amdgcn_readlane(n, t.b);
+    t.start = __builtin_amdgcn_readlane(start, t.b);
+    t.row0 = (__builtin_amdgcn_readlane(before + tiles, t.b) - 1 - tile) * ROWS;
+    return t;
 }
 
 // How far above the softmax's reference a score may be before the sums are put on a new one (in powers of two): the reference then hardly
@@ -266,14 +285,13 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
     const int lane = (int)threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = (int)(blockIdx.x % (unsigned)p.c.H), part = (int)(blockIdx.x / (unsigned)p.c.H / (unsigned)p.tiles);
-    int row0 = 0, t0 = 0, n = 0;
-    const int b = __builtin_amdgcn_readfirstlane(tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles), &row0, &t0, &n));
+    const TileOf tile = tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles));
+    const int b = __builtin_amdgcn_readfirstlane(tile.b);
     if (b < 0) return;
-    row0 = __builtin_amdgcn_readfirstlane(row0);
-    t0 = __builtin_amdgcn_readfirstlane(t0);
-    n = __builtin_amdgcn_readfirstlane(n);
+    const int row0 = __builtin_amdgcn_readfirstlane(tile.row0), t0 = __builtin_amdgcn_readfirstlane(tile.first);
+    const int n = __builtin_amdgcn_readfirstlane(tile.tokens);
     const int rows = n * p.G - row0 < ROWS ? n * p.G - row0 : ROWS;
-    const int64_t start = p.s.starts[b];
+    const int64_t start = __builtin_amdgcn_readfirstlane(tile.start);
 
     // this lane's query, and the positions that any of the tile sees and that all of it see
     const int row = row0 + (fr < rows ? fr : rows - 1), token = row / p.G, head = h * p.G + row % p.G;
@@ -603,14 +621,13 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
     const int tid = (int)threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = (int)(blockIdx.x % (unsigned)p.c.H), part = (int)(blockIdx.x / (unsigned)p.c.H / (unsigned)p.tiles);
-    int row0 = 0, t0 = 0, n = 0;
-    const int b = __builtin_amdgcn_readfirstlane(long_tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles), &row0, &t0, &n));
+    const TileOf tile = long_tile_sequence<ROWS>(p, (int)(blockIdx.x / (unsigned)p.c.H % (unsigned)p.tiles));
+    const int b = __builtin_amdgcn_readfirstlane(tile.b);
     if (b < 0) return;
-    row0 = __builtin_amdgcn_readfirstlane(row0);
-    t0 = __builtin_amdgcn_readfirstlane(t0);
-    n = __builtin_amdgcn_readfirstlane(n);
+    const int row0 = __builtin_amdgcn_readfirstlane(tile.row0), t0 = __builtin_amdgcn_readfirstlane(tile.first);
+    const int n = __builtin_amdgcn_readfirstlane(tile.tokens);
     const int rows = n * p.G - row0 < ROWS ? n * p.G - row0 : ROWS;
-    const int64_t start = p.s.starts[b];
+    const int64_t start = __builtin_amdgcn_readfirstlane(tile.start);
     const int first_token = row0 / p.G, last_token = (row0 + rows - 1) / p.G;
     const Seen first = positions_seen(p, start + first_token), last = positions_seen(p, start + last_token);
     const int64_t first_seen = start + first_token - p.window + 1, past = start + last_token + 1;
@@ -896,56 +913,56 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
     }
 }
 
-// The parts of a row put together, one workgroup per row: its parts' maxima and sums, one to a lane, then their columns, four to a lane, as
-// many parts at once as there are lanes for.
-template <Elem T>
+// Most parts: what a weight each fits in LDS for.
+constexpr int kMostParts = 2048;
+
+// The parts of a row put together, one workgroup per row: every wave finds the parts' common maximum, 64 parts to a look, and their weights
+// meet in LDS; then their columns, four to a lane, as many parts at once as there are lanes for, the first of them asked for ahead.
+template <Elem T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(Attention p) {
-    __shared__ float weight[256], red[2][4];
+    __shared__ float weight[kMostParts];
     __shared__ f32x4 partial[256];
+    constexpr int AHEAD = 4;
+    constexpr int lanes = D / 4, groups = 256 / lanes;
     const int64_t rows = (int64_t)p.s.T * p.Hq, row = blockIdx.x;
-    const int t = (int)(row / p.Hq), head = (int)(row % p.Hq), tid = (int)threadIdx.x, D = p.c.D;
-    int64_t position;
-    if (sequence_of(p.s, t, &position) < 0) return;
-    const int lanes = D / 4, groups = 256 / lanes, group = tid / lanes, d = tid % lanes * 4;
+    const int t = (int)(blockIdx.x / (unsigned)p.Hq), head = (int)(blockIdx.x % (unsigned)p.Hq), tid = (int)threadIdx.x, lane = tid & 63;
+    const int group = tid / lanes, d = tid % lanes * 4;
+    auto columns = [&](int k) { return *reinterpret_cast<const f32x4*>(p.sums + (k * rows + row) * D + d); };
+    const int past = p.s.cu[p.s.B];
+    f32x4 first[AHEAD];                                     // (of parts without a position: not written, and not used)
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (group < groups && group + i * groups < p.parts) first[i] = columns(group + i * groups);
+    float all = -__builtin_inff();
+    for (int i = lane; i < p.parts; i += 64) all = __builtin_fmaxf(all, p.stats[2 * (i * rows + row)]);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) all = __builtin_fmaxf(all, __shfl_xor(all, m));
+    const float base = all == -__builtin_inff() ? 0.0f : all;
+    float sum = 0.0f;
+    for (int i = lane; i < p.parts; i += 64) {
+        const float total = p.stats[2 * (i * rows + row) + 1], f = total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(p.stats[2 * (i * rows + row)] - base);
+        sum += total * f;
+        weight[i] = f;                                      // (by every wave, the same)
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+    __syncthreads();
+    if (t >= past) return;                                  // behind the last sequence
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    float all = -__builtin_inff(), sum = 0.0f;
-    for (int i0 = 0; i0 < p.parts; i0 += 256) {             // (256 parts hold any cache but the longest)
-        const int i = i0 + tid, n = p.parts - i0 < 256 ? p.parts - i0 : 256;
-        float top = -__builtin_inff(), total = 0.0f;
-        if (i < p.parts) {
-            top = p.stats[2 * (i * rows + row)];
-            total = p.stats[2 * (i * rows + row) + 1];
-        }
-        float most = top;
+    auto add = [&](const f32x4& x, float w) {
+        if (w != 0.0f)                                      // (NaN is not 0)
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, m));
-        if ((tid & 63) == 0) red[0][tid >> 6] = most;
-        __syncthreads();
-        most = __builtin_fmaxf(__builtin_fmaxf(red[0][0], red[0][1]), __builtin_fmaxf(red[0][2], red[0][3]));
-        const float next = __builtin_fmaxf(all, most), base = next == -__builtin_inff() ? 0.0f : next;
-        const float f = __builtin_amdgcn_exp2f(top - base), shrink = __builtin_amdgcn_exp2f(all - base);
-        all = next;
-        weight[tid] = total == 0.0f ? 0.0f : f;             // (a part without a position has written no columns)
-        float part = total * f;
+            for (int e = 0; e < 4; ++e) v[e] += x[e] * w;
+    };
+    if (group < groups) {
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) part += __shfl_xor(part, m);
-        if ((tid & 63) == 0) red[1][tid >> 6] = part;
-        __syncthreads();
-        sum = sum * shrink + ((red[1][0] + red[1][1]) + (red[1][2] + red[1][3]));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= shrink;
-        if (group < groups) {
+        for (int i = 0; i < AHEAD; ++i)
+            if (group + i * groups < p.parts) add(first[i], weight[group + i * groups]);
 #pragma unroll 4
-            for (int k = group; k < n; k += groups) {
-                const float w = weight[k];
-                if (w != 0.0f) {                            // (NaN is not 0)
-                    const f32x4 x = *reinterpret_cast<const f32x4*>(p.sums + ((i0 + k) * rows + row) * D + d);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] += x[e] * w;
-                }
-            }
+        for (int k = group + AHEAD * groups; k < p.parts; k += groups) {
+            const float w = weight[k];
+            if (w != 0.0f) add(columns(k), w);
         }
-        __syncthreads();
     }
     partial[tid] = v;
     __syncthreads();
@@ -979,6 +996,7 @@ static AttentionPlan plan_attention(int64_t T, int64_t B, int64_t H, int64_t Hq,
     const int64_t want = ceil_div(per_cu * cus, tiles * H), can = ceil_div(range, 32 * kAttendWaves * 2), fit = ((int64_t)48 << 20) / (T * Hq * (D + 2) * 4);
     int64_t parts = want < can ? want : can;
     parts = parts < fit ? parts : fit;
+    parts = parts < kMostParts ? parts : kMostParts;
     if (parts > 1) {
         a.chunk = round_up(ceil_div(range + 31, parts), 32 * kAttendWaves);
         parts = ceil_div(range + 31, a.chunk);
@@ -1008,7 +1026,7 @@ static hipError_t run_attention(const Attention& p, const AttentionPlan& a, hipS
         e = launch_kernel(kTimeGemm, attend_rows_kernel<T, F, D>, grid, dim3(kAttendWaves * 64), 0, stream, p);
     }
     if (e != hipSuccess || p.parts == 1) return e;
-    return launch_kernel(0, attend_join_kernel<T>, dim3((unsigned)((int64_t)p.s.T * p.Hq)), dim3(256), 0, stream, p);
+    return launch_kernel(0, attend_join_kernel<T, D>, dim3((unsigned)((int64_t)p.s.T * p.Hq)), dim3(256), 0, stream, p);
 }
 
 template <Elem T, CacheFormat F>
