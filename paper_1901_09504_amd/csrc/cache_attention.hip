@@ -341,35 +341,45 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
         for (int g = 0; g < 2; ++g) w.at[g] = page_of(p, table, j0 + 16 * g, end);
     };
     auto there = [&](const PageAt& at) { return at.page >= 0 && at.page < p.c.pages; };
-    auto load = [&](const Where& w, Block& x) {
+    auto first_row = [&](const PageAt& at) {                // of the group's first position
+        const bool ok = there(at);
+        return ((int64_t)(ok ? at.page : 0) * p.c.H + h) * p.c.P + (ok ? at.at : 0);
+    };
+    auto load_keys = [&](const Where& w, Block& x) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const bool ok = there(w.at[g]);
-            const int64_t r = ((int64_t)(ok ? w.at[g].page : 0) * p.c.H + h) * p.c.P + (ok ? w.at[g].at : 0);       // of the group's first position
-            const uint8_t* keys = static_cast<const uint8_t*>(p.c.keys) + r * ROWB;
-            const uint8_t* values = static_cast<const uint8_t*>(p.c.values) + r * ROWB;
-            load_key<MX, D, 0>(keys + fr * ROWB, fq, x.k[g]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) load_bytes<VB>(values + (4 * fq + i) * ROWB + fr * VB, x.v[4 * g + i]);
+            const int64_t r = first_row(w.at[g]);
+            load_key<MX, D, 0>(static_cast<const uint8_t*>(p.c.keys) + r * ROWB + fr * ROWB, fq, x.k[g]);
             if constexpr (MX) {
                 const uint8_t* ks = static_cast<const uint8_t*>(p.c.kscales) + r * (D / 32) + fr * (D / 32);
-                const uint8_t* vs = static_cast<const uint8_t*>(p.c.vscales) + r * (D / 32) + 4 * fq * (D / 32);
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
                     if (Columns::steps(s) != 4 || s % 4 == 0) x.kscale[g][s] = ks[Columns::column(s, fq) / 32];
+            } else {
+                const f32x4 ks = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.c.kscales) + r + 4 * fq);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x.kstep[g][i] = ks[i];
+            }
+        }
+    };
+    auto load_values = [&](const Where& w, Block& x) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int64_t r = first_row(w.at[g]);
+            const uint8_t* values = static_cast<const uint8_t*>(p.c.values) + r * ROWB;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_bytes<VB>(values + (4 * fq + i) * ROWB + fr * VB, x.v[4 * g + i]);
+            if constexpr (MX) {
+                const uint8_t* vs = static_cast<const uint8_t*>(p.c.vscales) + r * (D / 32) + 4 * fq * (D / 32);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     x.vscale[4 * g + i][0] = vs[i * (D / 32) + fr * DT / 32];
                     if constexpr (32 % DT != 0) x.vscale[4 * g + i][1] = vs[i * (D / 32) + (fr * DT + DT - 2) / 32];
                 }
             } else {
-                const f32x4 ks = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.c.kscales) + r + 4 * fq);
                 const f32x4 vs = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.c.vscales) + r + 4 * fq);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x.kstep[g][i] = ks[i];
-                    x.vstep[g][i] = vs[i];
-                }
+                for (int i = 0; i < 4; ++i) x.vstep[g][i] = vs[i];
             }
         }
     };
@@ -378,7 +388,8 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     float top = -__builtin_inff(), total = 0.0f;            // the softmax's reference; the sum over this lane's positions
-    auto use = [&](int j0, const Where& where, const Block& x) {
+    // Positions j0 on; the next ones' keys and values (more: there are some) take the place of these as soon as they have been multiplied.
+    auto use = [&](int j0, const Where& where, Block& x, bool more, const Where& next) {
         float s[8];
         // whether every row of the tile sees all 32
         const bool whole = j0 >= all_from && j0 + 32 <= all_end && j0 + 32 <= end && there(where.at[0]) && there(where.at[1]);
@@ -405,6 +416,7 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[4 * g + i] = MX ? a[i] * p.scale : a[i] * (x.kstep[g][i] * p.scale);
         }
+        if (more) load_keys(next, x);
         unsigned sees = 0xFFu;                              // a bit per position of this lane
         if (!whole) {
             sees = 0;
@@ -495,29 +507,26 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
 #pragma unroll
                 for (int m = N - 1; m >= 0; --m) acc[t + e] = multiply_bf16(v[e], pw[m], acc[t + e]);
         }
+        if (more) load_values(next, x);
     };
     {
-        // pages are looked up two blocks ahead, rows loaded one ahead; two blocks by turns, so that none is copied
+        // pages are looked up two blocks ahead, rows asked for most of a block ahead
         constexpr int STRIDE = 32 * NW;
         int j = begin + 32 * wave;
-        Block even, odd;
-        Where at_even{}, at_odd{};
+        Block x;
+        Where now{}, next{};
         if (j < end) {
-            look_up(j, at_even);
-            if (j + STRIDE < end) look_up(j + STRIDE, at_odd);
-            load(at_even, even);
+            look_up(j, now);
+            look_up(j + STRIDE, next);
+            load_keys(now, x);
+            load_values(now, x);
         }
-        auto turn = [&](Where& at, Block& x, const Where& next_at, Block& next) {
-            if (j + STRIDE < end) load(next_at, next);
-            const Where now = at;
-            if (j + 2 * STRIDE < end) look_up(j + 2 * STRIDE, at);
-            use(j, now, x);
-            j += STRIDE;
-        };
-        while (j < end) {
-            turn(at_even, even, at_odd, odd);
-            if (j >= end) break;
-            turn(at_odd, odd, at_even, even);
+        for (; j < end; j += STRIDE) {
+            Where further;
+            look_up(j + 2 * STRIDE, further);
+            use(j, now, x, j + STRIDE < end, next);
+            now = next;
+            next = further;
         }
     }
     total = over_quarters_sum(total);
