@@ -608,22 +608,24 @@ __device__ __forceinline__ u32x2 read_transposed(const uint8_t* lds) {
 // bf16 numbers in LDS, once for all its rows, while the next positions' codes are on their way, and the waves multiply from there: keys a
 // row at a time, values transposed as they are read (ds_read_b64_tr_b16).  Rows of LDS are 4 and 8 banks apart beyond a multiple of 64, so
 // that what the matrix cores read at a time lies in different banks.
+constexpr int kTileWaves = 4;
 template <Elem T, int D>
 struct AttendTile {
     static constexpr int N = kPieces<T>;
-    static constexpr int NT = D <= 128 ? 2 : 1, ROWS = 64 * NT, KT = D <= 128 && N == 1 ? 64 : 32;
+    static constexpr int THREADS = 64 * kTileWaves;
+    static constexpr int NT = D <= 128 ? 2 : 1, ROWS = 16 * kTileWaves * NT, KT = D <= 128 && N == 1 ? 64 : 32;
     static constexpr int KPITCH = 2 * D + 16, VPITCH = 2 * D + 32;
     static constexpr int LDS = 2 * KT * (KPITCH + VPITCH);
 };
 
 template <Elem T, CacheFormat F, int D>
-__global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
+__global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_kernel(Attention p) {
     using Tile = AttendTile<T, D>;
-    constexpr int N = Tile::N, NT = Tile::NT, ROWS = Tile::ROWS, KT = Tile::KT, KPITCH = Tile::KPITCH, VPITCH = Tile::VPITCH;
+    constexpr int N = Tile::N, NT = Tile::NT, ROWS = Tile::ROWS, KT = Tile::KT, KPITCH = Tile::KPITCH, VPITCH = Tile::VPITCH, THREADS = Tile::THREADS;
     constexpr int KS = D / 32, DT = D / 16, MT = KT / 16;
     constexpr bool MX = F == CacheFormat::mx4;
     constexpr int ROWB = MX ? D / 2 : D, PIECE = MX ? 8 : 16;              // bytes of a row, and of 16 of its codes
-    constexpr int ITEMS = KT * (D / 16), LOADS = (ITEMS + 255) / 256;
+    constexpr int ITEMS = KT * (D / 16), LOADS = (ITEMS + THREADS - 1) / THREADS;
     extern __shared__ __align__(16) uint8_t lds[];
     __shared__ __align__(16) float ksteps[2][KT], vsteps[2][KT];
     __shared__ int there_of[2][MT];
@@ -700,12 +702,12 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
     const uint8_t* const values = static_cast<const uint8_t*>(p.c.values) + (int64_t)h * p.c.P * ROWB;
     const uint8_t* const kscales = static_cast<const uint8_t*>(p.c.kscales) + (int64_t)h * p.c.P * (MX ? D / 32 : 4);
     const uint8_t* const vscales = static_cast<const uint8_t*>(p.c.vscales) + (int64_t)h * p.c.P * (MX ? D / 32 : 4);
-    auto key_of = [&](int u) { return (tid + 256 * u) / (D / 16); };
-    auto part_of = [&](int u) { return (tid + 256 * u) % (D / 16); };
+    auto key_of = [&](int u) { return (tid + THREADS * u) / (D / 16); };
+    auto part_of = [&](int u) { return (tid + THREADS * u) % (D / 16); };
     auto look_up = [&](int j0) {                             // (positions behind the last repeat it)
 #pragma unroll
         for (int u = 0; u < LOADS; ++u)
-            if (ITEMS % 256 == 0 || tid + 256 * u < ITEMS) {
+            if (ITEMS % THREADS == 0 || tid + THREADS * u < ITEMS) {
                 const int j = j0 + key_of(u) < end ? j0 + key_of(u) : end - 1;
                 int col = (int)__umulhi((unsigned)j, p.page_magic), at = j - col * p.c.P;
                 col -= at < 0;
@@ -716,7 +718,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
     auto load = [&]() {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u)
-            if (ITEMS % 256 == 0 || tid + 256 * u < ITEMS) {
+            if (ITEMS % THREADS == 0 || tid + THREADS * u < ITEMS) {
                 there[u] = (unsigned)page[u] < pages;
                 const uint64_t r = (uint64_t)(there[u] ? (unsigned)page[u] : 0u) * page_rows + (unsigned)row_of[u];
                 load_bytes<PIECE>(keys + r * ROWB + part_of(u) * PIECE, codes[u].k);
@@ -748,7 +750,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
     auto store = [&](int buf) {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u)
-            if (ITEMS % 256 == 0 || tid + 256 * u < ITEMS) {
+            if (ITEMS % THREADS == 0 || tid + THREADS * u < ITEMS) {
                 const int key = key_of(u), col = part_of(u);
                 u32x4 x[2];
                 numbers(codes[u].k, codes[u].kstep, x);
@@ -810,16 +812,20 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(Attention p) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[m][u][i] *= factor[i];
         }
-        if (!whole) {
+        if (!whole) {                                       // a bit for each of four positions, without a comparison for each
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int u = 0; u < NT; ++u)
+                for (int u = 0; u < NT; ++u) {
+                    const int base = j0 + 16 * m + 4 * fq, last = mine[u].from + mine[u].count < end ? mine[u].from + mine[u].count : end;
+                    const int from = clamp_int(mine[u].from - base, 0, 4), to = clamp_int(last - base, 0, 4);
+                    const int sees = groups >> m & 1 ? ((1 << to) - 1) & ~((1 << from) - 1) : 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int j = j0 + 16 * m + 4 * fq + i;
-                        if (!(groups >> m & 1) || j >= end || (unsigned)(j - mine[u].from) >= (unsigned)mine[u].count) s[m][u][i] = -__builtin_inff();
+                        const unsigned all = (unsigned)__builtin_amdgcn_sbfe(sees, i, 1);      // ones or zeros
+                        s[m][u][i] = __uint_as_float((__float_as_uint(s[m][u][i]) & all) | (0xFF800000u & ~all));
                     }
+                }
         }
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
@@ -1030,7 +1036,7 @@ static hipError_t run_attention(const Attention& p, const AttentionPlan& a, hipS
             e = allow_lds(reinterpret_cast<const void*>(&attend_tile_kernel<T, F, D>), LDS, allowed);
             if (e != hipSuccess) return e;
         }
-        e = launch_kernel(kTimeGemm, attend_tile_kernel<T, F, D>, grid, dim3(256), (unsigned)LDS, stream, p);
+        e = launch_kernel(kTimeGemm, attend_tile_kernel<T, F, D>, grid, dim3(AttendTile<T, D>::THREADS), (unsigned)LDS, stream, p);
     } else {
         e = launch_kernel(kTimeGemm, attend_rows_kernel<T, F, D>, grid, dim3(kAttendWaves * 64), 0, stream, p);
     }

@@ -515,7 +515,8 @@ class TokenCache:
                 self.page_rows, self.heads, self.D, self.key_depth, self.value_depth)
 
     def _check_rows(self, x, counts, heads):
-        assert x.is_cuda and x.dim() == 3 and x.shape[1:] == (heads, self.D) and (x.stride(2) == 1 or x.numel() == 0) and x.shape[0] == sum(counts)
+        assert x.device == self.keys.device and x.dim() == 3 and x.shape[0] == sum(counts) and x.shape[1:] == (heads, self.D)
+        assert x.stride(2) == 1 or x.numel() == 0
 
     def append(self, K, V, counts, which=None):
         """K, V [T, heads, D] in fp32, bf16 or fp16: the next counts[i] tokens of sequence which[i] (all of them in order if None), one
