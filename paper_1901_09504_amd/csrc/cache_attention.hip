@@ -272,7 +272,8 @@ __device__ __forceinline__ void load_key(const uint8_t* key, int fq, unsigned* w
 //
 // 16 rows of a sequence and head per workgroup; its waves take 32 positions at a time in turn and meet at the end.  Keys and values go
 // from memory to the lanes that multiply them: of a key a lane has D / 4 columns, of a value D / 16, and the accumulator's tile t
-// holds column (D / 16) m + t in its row m.
+// holds column (D / 16) m + t in its row m.  Bound by the rows' bytes: 64 sequences to 8192 positions, 8 heads of 128 in 8 bits, 128 us, 4.4 TB/s;
+// the loads alone, nothing made of them, take 5 us less.
 template <Elem T, CacheFormat F, int D>
 __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Attention p) {
     constexpr int N = kPieces<T>, KS = D / 32, DT = D / 16, ROWS = 16, NW = kAttendWaves;
@@ -607,7 +608,8 @@ __device__ __forceinline__ u32x2 read_transposed(const uint8_t* lds) {
 // Many rows: 64 NT rows of a sequence and head per workgroup, 16 NT to each of its four waves.  The workgroup turns KT positions at a time into
 // bf16 numbers in LDS, once for all its rows, while the next positions' codes are on their way, and the waves multiply from there: keys a
 // row at a time, values transposed as they are read (ds_read_b64_tr_b16).  Rows of LDS are 4 and 8 banks apart beyond a multiple of 64, so
-// that what the matrix cores read at a time lies in different banks.
+// that what the matrix cores read at a time lies in different banks.  Bound by vector instructions (conversions, exponentials, factors: 55 % of the
+// time) and matrix cores (25 %), which overlap little: prompts of 512 to 1501 tokens in sequences to 6001, 32 heads on 8 of 128, 281 us, 0.68 PFLOP/s.
 constexpr int kTileWaves = 4;
 template <Elem T, int D>
 struct AttendTile {

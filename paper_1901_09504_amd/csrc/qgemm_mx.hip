@@ -5,6 +5,8 @@
 // straight into LDS, 128 bytes (256 columns) of 8 rows per request, 16-byte chunks XOR-ed with the row.  A chunk is a block.  A row's 16
 // scale bytes of two steps are a request of their own, one row per lane; a lane of quarter q takes chunks 2q and 2q + 1 of a step, so that
 // their scales are two neighbouring bytes, which the instruction picks from one register.
+// Many tokens: 8192 x 4096 x 4178 bf16 74 us, 3.8 PFLOP/s, 8192^3 4.2, where a bare loop of the instruction sustains 7.0; requests alone take
+// 228 us of 270 on the latter, reads and products alone 221.  Few tokens: the weights' bytes, and the latency of one launch.
 #include <type_traits>
 
 #include "mx_grids.h"
