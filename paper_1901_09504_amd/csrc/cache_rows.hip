@@ -44,7 +44,7 @@ template <Elem T, CacheFormat F, int LANES, int TIMES, bool WRITE>
 __global__ __launch_bounds__(256) void cache_rows_kernel(CacheRows p, unsigned waves_per_token) {
     constexpr int ROWS = 64 / LANES;
     const int lane = (int)threadIdx.x & 63, c = lane % LANES * 8, H = p.c.H, D = p.c.D;
-    const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const unsigned wave = __builtin_amdgcn_readfirstlane(neighbours_on_an_xcd(blockIdx.x, gridDim.x) * 4 + (threadIdx.x >> 6));
     const unsigned nth = wave / waves_per_token, t = p.t0 + nth;
     if (t >= (unsigned)p.s.T) return;
     const int first = (int)(wave - nth * waves_per_token) * (ROWS * TIMES) + lane / LANES;

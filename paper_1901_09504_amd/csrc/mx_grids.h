@@ -20,6 +20,13 @@ struct MxRows {
     int64_t lds;
 };
 
+// Workgroup ids are dealt to the 8 XCDs in turn, each with an L2 of its own.  The id that gives an XCD a run of neighbours instead, which share
+// lines of memory.
+__device__ __forceinline__ unsigned neighbours_on_an_xcd(unsigned w, unsigned total) {
+    const unsigned each = total / 8, more = total % 8, xcd = w % 8;
+    return xcd * each + (xcd < more ? xcd : more) + w / 8;
+}
+
 // The scale byte of a block whose largest magnitude has these bits: 2^(floor(log2 max) - 2) puts it into [4, 8), the binade of the
 // largest code; the exponent field is that logarithm already.  Below 2^-125 the byte ends at 0.  NaN comes above infinity.
 __device__ __forceinline__ unsigned mx_scale_byte(unsigned magnitude) {

@@ -11,7 +11,7 @@ namespace ocs {
 // `blocks` blocks a row, the padding of codes and scales among them.
 template <Elem T, bool SCALED>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(MxRows p, unsigned blocks, unsigned magic) {
-    const unsigned at = (blockIdx.x * 256 + threadIdx.x) >> 2;      // (kMostLanes fits 32 bits)
+    const unsigned at = (neighbours_on_an_xcd(blockIdx.x, gridDim.x) * 256 + threadIdx.x) >> 2;      // (kMostLanes fits 32 bits)
     const int part = (int)(threadIdx.x & 3);
     unsigned r = __umulhi(at, magic);                               // at / blocks or one more: magic is 2^32 / blocks and one more, at below 2^30
     int block = (int)(at - r * blocks);
