@@ -547,3 +547,93 @@ def test_scores_behind_a_quantized_cache():
     rows = score.run_cache(sequences=2, length=40, vocab=500)
     assert [(b, r) for b, r, _, _ in rows] == [(32, 0.0), (8, 0.0), (8, 0.1), (4, 0.0), (4, 0.1)]
     assert all(math.isfinite(p) and p >= 1 and 0 <= same <= 1 for _, _, p, same in rows)
+
+
+# ---- what the calls above do not reach -------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("D,P", [(64, 16), (160, 1024), (224, 32)])
+def test_prompts_of_more_sequences_than_a_wave_has_lanes(fmt, D, P):
+    rng = np.random.default_rng(D)
+    new = [int(n) for n in rng.integers(0, 60, 70)]
+    held = [n + int(e) for n, e in zip(new, rng.integers(0, 90, 70))]
+    pool = Pool(fmt, held, 1, D, P, seed=2)
+    fill(pool, 2)
+    check_attention(pool, new, 2, BF16, window=50)
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("new,held,window", [([70], [2900], 0), ([70], [2900], 1500), ([130, 3], [2050, 700], 0)])
+def test_prompts_whose_positions_are_shared_by_workgroups(fmt, dtype, new, held, window):
+    pool = Pool(fmt, held, 1, 64, 32, seed=7, halved=True)
+    fill(pool, 7)
+    assert B.ocs_cache_attention_workspace_bytes(sum(new), len(new), 1, 2, 64, max(held), window) > 0
+    check_attention(pool, new, 2, dtype, window=window)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [90, 40]])
+def test_a_captured_attention_in_parts_and_the_same_bits_each_time(new):
+    """A graph of its own workspace on a side stream, eager calls of other lengths between the replays; no sum depends on an order that changes."""
+    held = [2500, 1900]
+    pool = Pool(INT8, held, 2, 128, 64, seed=1)
+    fill(pool, 1)
+    T, args = sum(new), pool.args()
+    cu, st, _ = tokens_of(new, [h - n for h, n in zip(held, new)])
+    q = torch.randn((T, 4, 128), device="cuda").to(BF16)
+    ys = [torch.empty_like(q) for _ in range(2)]
+    wss = [workspace(T, 2, 2, 4, 128, 2500) for _ in range(2)]
+    assert wss[0] is not None
+
+    def call(y, ws, stream=None):
+        B.ocs_cache_attention(q, 512, 128, 4, T, cu, st, 2, 2500, *args, 0.1, 0, y, 512, 128, None, ws, stream=stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(ys[1], wss[1], stream=side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(ys[0], wss[0])
+    for seed in range(4):
+        q.copy_(torch.randn((T, 4, 128), generator=torch.Generator().manual_seed(seed)))
+        ys[0].fill_(3.0)
+        graph.replay()
+        got = ys[0].clone()
+        torch.cuda.synchronize()
+        call(ys[1], wss[1])
+        assert torch.equal(got, ys[1])
+        check_attention(pool, [1, 1], 4, F32, seed=seed)
+
+
+def test_written_and_read_on_another_stream():
+    pool, other = (Pool(MX4, [50], 2, 64, 16, seed=5) for _ in range(2))
+    k, v = random_rows(50, 2, 64, F16, 1), random_rows(50, 2, 64, F16, 2)
+    write(pool, k, v, [50], [0])
+    cu, st, _ = tokens_of([50], [0])
+    out = [torch.empty_like(k) for _ in range(2)]
+    args = other.args()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    B.ocs_cache_write(k, 128, 64, v, 128, 64, 50, cu, st, 1, *args, stream=side)
+    B.ocs_cache_read(out[0], 128, 64, out[1], 128, 64, 50, cu, st, 1, *args, stream=side)
+    side.synchronize()
+    for a, b in zip(out, read(pool, F16, [50], [0])):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+def test_queries_that_are_no_numbers_stay_alone(fmt):
+    pool = Pool(fmt, [100, 100], 1, 64, 16, seed=3)
+    fill(pool, 3)
+    for new in ([1, 1], [80, 80]):
+        T = sum(new)
+        q = torch.randn((T, 2, 64), generator=torch.Generator().manual_seed(1)).cuda()
+        cu, st, _ = tokens_of(new, [100 - n for n in new])
+        y, z = torch.empty_like(q), torch.empty_like(q)
+        for to in (y, z):
+            B.ocs_cache_attention(q, 128, 64, 2, T, cu, st, 2, 100, *pool.args(), 0.1, 0, to, 128, 64, None, workspace(T, 2, 1, 2, 64, 100))
+            q[0, 1, 5] = torch.nan
+        assert bool(z[0, 1].isnan().all())
+        z[0, 1], y[0, 1] = 0, 0
+        assert torch.equal(y, z)
