@@ -3,7 +3,7 @@
 // For expanded column k of row m: x' = X[m, source(k)] * 2^-depth; over a block a = max|x'|, e = floor(log2 a) - 2 (at least -127),
 // code = nearest e2m1 number to x' * 2^-e.  Four lanes share a block, 8 columns each: the block's maximum is two exchanges between
 // neighbours, loads and stores are whole 16- and 4-byte pieces of consecutive lanes, and nothing waits for a row: bound by HBM for many
-// rows (4096 x 4096 bf16 with 82 splits 11.7 us, 3.7 TB/s; back to bf16 8.2, 5.3), by one launch for few (64 x 256 3.2).
+// rows (4096 x 4096 bf16 with 82 splits 10.3 us, 4.2 TB/s; back to bf16 8.2, 5.3), by one launch for few (64 x 256 3.2).
 #include "mx_grids.h"
 
 namespace ocs {
