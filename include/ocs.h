@@ -594,7 +594,7 @@ int ocs_forward_mx(const void *X, int type, int64_t M, int C, int g, int64_t ldx
  *        s_j = scale * q . k_j,   Y[t, i] = sum exp(s_j) v_j / sum exp(s_j),   lse[t, i] = log sum exp(s_j)   (dense fp32, may be NULL).
  *   A token that sees none: Y 0, lse -inf.  One that sees a row with NaN (a value with scales from 253 on): NaN.  What positions' rows hold
  *   that it does not see does not matter.  `most` is at least the longest sequence's
- *   positions, this call's among them.  Scores and sums in fp32; bf16 queries meet weights rounded to bf16, others finer ones.
+ *   positions, this call's among them, and at most 2^31 - 2^16.  Scores and sums in fp32; bf16 queries meet weights rounded to bf16, others finer ones.
  *   workspace: at least ocs_cache_attention_workspace_bytes() bytes, 256-byte aligned; it may be NULL where that is 0.  Needs no
  *   initialisation.
  * T = 0 or B = 0 is OCS_OK and launches nothing.

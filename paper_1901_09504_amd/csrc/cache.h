@@ -10,6 +10,7 @@ namespace ocs {
 
 enum class CacheFormat { int8 = 0, mx4 = 1 };   // OCS_CACHE_INT8, OCS_CACHE_MX4
 
+constexpr int kMostPositions = 0x7FFF0000;      // attention's: its next blocks of positions are numbers of 32 bits, too
 constexpr int kMostDepth = 126;                 // 2^126 and 2^-126 are normal numbers
 
 struct Cache {

@@ -174,7 +174,7 @@ __device__ __forceinline__ TileOf tile_sequence(const Attention& p, int tile) {
     return t;
 }
 
-// What a query sees: `count` positions from `from` on (the cache holds fewer than 2^31).
+// What a query sees: `count` positions from `from` on (no position beyond kMostPositions is looked at).
 struct Seen {
     int from, count;
 };

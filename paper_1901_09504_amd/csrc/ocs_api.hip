@@ -1186,7 +1186,7 @@ static bool attention_fits(int64_t T, int64_t B, int64_t heads, int64_t query_he
 
 size_t ocs_cache_attention_workspace_bytes(int64_t T, int64_t B, int heads, int query_heads, int D, int64_t most, int64_t window) {
     if (T <= 0 || B <= 0 || T > (int64_t)1 << 30 || B > (int64_t)1 << 30 || !attention_fits(T, B, heads, query_heads) || D <= 0 || most < 0 ||
-        most > 0x7FFFFFFF || window < 0)
+        most > kMostPositions || window < 0)
         return 0;
     return cache_attention_workspace_bytes(T, B, heads, query_heads, D, most, window);
 }
@@ -1201,7 +1201,7 @@ int ocs_cache_attention(const void* Q, int type, int64_t ldq, int64_t hdq, int q
                   const_cast<void*>(value_scales), pages, page_rows, heads, D, key_depth, value_depth};
     int rc = check_cache(T, cu, starts, B, format, c);
     if (rc) return rc;
-    if (!attention_fits(T, B, heads, query_heads) || most < 0 || most > 0x7FFFFFFF || window < 0 || window > (int64_t)1 << 40) return OCS_E_SHAPE;
+    if (!attention_fits(T, B, heads, query_heads) || most < 0 || most > kMostPositions || window < 0 || window > (int64_t)1 << 40) return OCS_E_SHAPE;
     if (B == 0) T = 0;
     rc = check_head_rows(Q, type, T, query_heads, D, ldq, hdq, false);
     if (rc) return rc;

@@ -115,6 +115,14 @@ def test_rows_refusals():
         assert _rows(B.lib().ocs_cache_read, over) == -2
 
 
+def test_positions_whose_numbers_would_pass_32_bits():
+    # blocks beyond the last one seen are counted in 32 bits
+    for most in (0x7FFF0001, 0x7FFFFFFF):
+        assert _attend(most=most, P=1 << 24, cols=128, ldt=128) == -2
+        assert B.ocs_cache_attention_workspace_bytes(3, 2, 2, 8, 64, most) == 0
+    assert B.ocs_cache_attention_workspace_bytes(3, 2, 2, 8, 64, 0x7FFF0000) > 0
+
+
 def test_attention_refusals():
     for over, code in ((dict(Q=None), -1), (dict(Y=None), -1), (dict(Hq=7), -2), (dict(Hq=1), -2), (dict(Hq=0), -2), (dict(most=-1), -2),
                        (dict(most=1 << 31), -2), (dict(window=-1), -2), (dict(ldy=63), -2), (dict(hdy=32), -2), (dict(Q=A + 2), -3),
