@@ -957,7 +957,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attention p) {
     const float base = all == -__builtin_inff() ? 0.0f : all;
     float sum = 0.0f;
     for (int i = lane; i < p.parts; i += 64) {
-        const float total = p.stats[2 * (i * rows + row) + 1], f = total == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(p.stats[2 * (i * rows + row)] - base);
+        const float total = p.stats[2 * (i * rows + row) + 1];
+        // at least 2^-126 where there are positions: nothing beside the part with the maximum, but a NaN stays one
+        const float f = total == 0.0f ? 0.0f : __builtin_fmaxf(__builtin_amdgcn_exp2f(p.stats[2 * (i * rows + row)] - base), 0x1p-126f);
         sum += total * f;
         weight[i] = f;                                      // (by every wave, the same)
     }

@@ -364,6 +364,34 @@ def test_rows_that_are_no_numbers_reach_only_those_who_see_them(fmt, dtype, many
     assert bool(y[sees].isnan().all()) and not bool(y[~sees].isnan().any())
 
 
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("new", [1, 60])
+def test_a_value_that_is_no_number_far_below_the_largest_score(fmt, dtype, new):
+    # its weight is 0 beside the largest, in a part of its own of the positions
+    L = 2048
+    pool = Pool(fmt, [L], 1, 64, 16, seed=12)
+    k, v = torch.zeros((L, 1, 64), device="cuda"), random_rows(L, 1, 64, F32, 13)
+    k[1500] = 8
+    v[10, 0, 5] = torch.nan
+    write(pool, k, v, [L], [0])
+    assert workspace(new, 1, 1, 2, 64, L) is not None
+    q = torch.full((new, 2, 64), 8.0, dtype=dtype, device="cuda")
+    q[:, 1] = 0
+    for window in (0, 1024):
+        y = torch.zeros_like(q)
+        cu, st, _ = tokens_of([new], [L - new])
+        B.ocs_cache_attention(q, 128, 64, 2, new, cu, st, 1, L, *pool.args(), 1.0, window, y, 128, 64, None,
+                              workspace(new, 1, 1, 2, 64, L, window))
+        assert bool(y.isnan().all()) if window == 0 else bool(y.isfinite().all())
+        if window:
+            # position 1500's value: its weight and the output rounded, half a step each, sums and the quotient in 32 bits; of the others less
+            # than 2048 times the largest value (2^9) times 2^-126
+            page, row = pool.row(0, 1500)
+            want = pool.numbers(1)[page, 0, row]
+            assert bool(((y[:, 0].double() - want).abs() <= want.abs() * (torch.finfo(dtype).eps + 2.0 ** -22) + 2.0 ** -106).all())
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("new", [[1, 1], [40, 3]])
 def test_layouts_of_queries_and_outputs(dtype, new):
