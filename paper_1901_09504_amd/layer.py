@@ -455,7 +455,7 @@ class TokenCache:
     positions each sequence has, is kept on the host, and every call sends what it needs of that to the device; a program that captures
     its steps into graphs keeps the table and the positions on the device itself and makes the calls of `binding`.
     key_depth, value_depth: int32 [heads, D], how often a channel is halved before its row's grid (outlier_depths gives them).
-    Calls run on the current stream; one on another stream than the last waits for that one's work.  Not to be captured: what a call sends
+    Calls run on the current stream, of the pool's device; one on another stream than the last waits for that one's work.  Not to be captured: what a call sends
     comes from the host."""
 
     def __init__(self, sequences, pages, heads, D, page_rows=64, bits=8, key_depth=None, value_depth=None, device="cuda"):
@@ -476,10 +476,12 @@ class TokenCache:
         self.tables = [[] for _ in range(self.sequences)]
         self.spare = list(range(self.pages - 1, -1, -1))
         self._stream = torch.cuda.current_stream()          # the last call's
+        assert self._stream.device == self.keys.device, "the pool's device is to be the current one"
 
     def _use_on_current_stream(self):
         stream = torch.cuda.current_stream()
         if stream != self._stream:
+            assert stream.device == self.keys.device, "the pool's device is to be the current one"
             stream.wait_stream(self._stream)
             for t in (self.keys, self.key_scales, self.values, self.value_scales, self.key_depth, self.value_depth):
                 if t is not None:

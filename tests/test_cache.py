@@ -2,6 +2,7 @@
 against 64 bits; lengths from none to long ones, pages that are missing or out of range, rubbish where nothing is seen, windows, strides,
 layouts, streams, graphs and pools beyond 4 GB."""
 import math
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -565,6 +566,10 @@ def test_a_cache_refuses_what_does_not_fit():
         cache.attend(k, [2, 1])                                              # more queries than positions
     with pytest.raises(AssertionError):
         TokenCache(2, 4, 2, 32, bits=5)
+    cache = TokenCache(2, 4, 2, 32)
+    with pytest.MonkeyPatch.context() as m, pytest.raises(AssertionError, match="device"):
+        m.setattr(torch.cuda, "current_stream", lambda: SimpleNamespace(device=torch.device("cuda", 1)))
+        cache.read()
     with pytest.raises(B.OcsError):
         TokenCache(2, 4, 2, 48).append(random_rows(2, 2, 48, F32, 1), random_rows(2, 2, 48, F32, 1), [1, 1])
 
