@@ -596,7 +596,7 @@ int ocs_forward_mx(const void *X, int type, int64_t M, int C, int g, int64_t ldx
  *   for a value NaN or the number.  What rows that it does not see hold does not matter.  `most` is at least the longest sequence's
  *   positions, this call's among them, and at most 2^31 - 2^16.
  *   Scores and sums in fp32, as are queries times 2^key_depth, with weights up to 2^8 (values whose sum times 2^8 passes fp32's range come
- *   out infinite or NaN); bf16 queries meet weights rounded to bf16, others finer ones.
+ *   out infinite or NaN), each off by 2^-16 of itself at most where it meets the values (fp32: 2^-24).
  *   workspace: at least ocs_cache_attention_workspace_bytes() bytes, 256-byte aligned; it may be NULL where that is 0.  Needs no
  *   initialisation.
  * T = 0 or B = 0 is OCS_OK and launches nothing.

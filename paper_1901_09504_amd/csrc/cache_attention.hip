@@ -5,8 +5,10 @@
 // sequence's tokens make the rows of a tile.  Both products run on the matrix cores (v_mfma_f32_16x16x32_bf16) with the cache's side
 // down the accumulator: S^T = K Q^T leaves a lane four scores of one query, which are, as they are, its part of P^T in O^T = V^T P^T.
 // Codes of 8 bits and of 4 are exact in bf16, and so are the steps: an 8-bit row's step multiplies scores (keys) or weights (values), a
-// block's power of two goes into the number itself.  Queries and weights are taken as sums of bf16 numbers, one for bf16 (8 bits), two
-// for fp16 (16 bits, where 11 count), three for fp32 (24): scores are as exact as 32-bit sums, and a weight is rounded like the output.
+// block's power of two goes into the number itself.  Queries are taken as sums of bf16 numbers, one for bf16 (8 bits), two for fp16 (16 bits,
+// where 11 count), three for fp32 (24): scores are as exact as 32-bit sums.  A weight is two of them, off by 2^-16 of itself at most, or three
+// for fp32, so that an output is off by its own rounding.  (One for bf16 would be a second rounding of that size: prompts off 64 bits by 0.0023
+// of their norm where two leave 0.0017, in 283 us where two take 333; single tokens, which wait for memory, take as long either way.)
 #include <type_traits>
 
 #include "cache.h"
@@ -36,6 +38,8 @@ struct Attention {
 
 template <Elem T>
 constexpr int kPieces = T == Elem::bf16 ? 1 : T == Elem::f16 ? 2 : 3;      // bf16 numbers that make one of T
+template <Elem T>
+constexpr int kWeightPieces = T == Elem::f32 ? 3 : 2;                      // and that make a weight of the values
 
 __device__ __forceinline__ unsigned bf16_pair(float lo, float hi) {         // of numbers that are bf16 already
     return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
@@ -276,7 +280,7 @@ __device__ __forceinline__ void load_key(const uint8_t* key, int fq, unsigned* w
 // the loads alone, nothing made of them, take 5 us less.
 template <Elem T, CacheFormat F, int D>
 __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Attention p) {
-    constexpr int N = kPieces<T>, KS = D / 32, DT = D / 16, ROWS = 16, NW = kAttendWaves;
+    constexpr int N = kPieces<T>, NV = kWeightPieces<T>, KS = D / 32, DT = D / 16, ROWS = 16, NW = kAttendWaves;
     constexpr bool MX = F == CacheFormat::mx4;
     constexpr int KB = MX ? D / 8 : D / 4, VB = MX ? D / 32 : D / 16;       // bytes of a lane's part of a key and of a value
     using Columns = KeyColumns<MX, D>;
@@ -473,8 +477,8 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = sees >> i & 1 ? w[i] * x.vstep[i / 4][i % 4] : 0.0f;
         }
-        u32x4 pw[N];
-        bf16_sums<N>(w, pw);
+        u32x4 pw[NV];
+        bf16_sums<NV>(w, pw);
 #pragma unroll
         for (int t = 0; t < DT; t += 2) {                   // two columns of 8 values at a time
             u32x4 v[2];
@@ -506,7 +510,7 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
-                for (int m = N - 1; m >= 0; --m) acc[t + e] = multiply_bf16(v[e], pw[m], acc[t + e]);
+                for (int m = NV - 1; m >= 0; --m) acc[t + e] = multiply_bf16(v[e], pw[m], acc[t + e]);
         }
         if (more) load_values(next, x);
     };
@@ -609,7 +613,7 @@ __device__ __forceinline__ u32x2 read_transposed(const uint8_t* lds) {
 // bf16 numbers in LDS, once for all its rows, while the next positions' codes are on their way, and the waves multiply from there: keys a
 // row at a time, values transposed as they are read (ds_read_b64_tr_b16).  Rows of LDS are 4 and 8 banks apart beyond a multiple of 64, so
 // that what the matrix cores read at a time lies in different banks.  Bound by vector instructions (conversions, exponentials, factors: 55 % of the
-// time) and matrix cores (25 %), which overlap little: prompts of 512 to 1501 tokens in sequences to 6001, 32 heads on 8 of 128, 281 us, 0.68 PFLOP/s.
+// time) and matrix cores (25 %), which overlap little: prompts of 512 to 1501 tokens in sequences to 6001, 32 heads on 8 of 128, 333 us, 0.57 PFLOP/s.
 constexpr int kTileWaves = 4;
 template <Elem T, int D>
 struct AttendTile {
@@ -624,7 +628,7 @@ template <Elem T, CacheFormat F, int D>
 __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_kernel(Attention p) {
     using Tile = AttendTile<T, D>;
     constexpr int N = Tile::N, NT = Tile::NT, ROWS = Tile::ROWS, KT = Tile::KT, KPITCH = Tile::KPITCH, VPITCH = Tile::VPITCH, THREADS = Tile::THREADS;
-    constexpr int KS = D / 32, DT = D / 16, MT = KT / 16;
+    constexpr int NV = kWeightPieces<T>, KS = D / 32, DT = D / 16, MT = KT / 16;
     constexpr bool MX = F == CacheFormat::mx4;
     constexpr int ROWB = MX ? D / 2 : D, PIECE = MX ? 8 : 16;              // bytes of a row, and of 16 of its codes
     constexpr int ITEMS = KT * (D / 16), LOADS = (ITEMS + THREADS - 1) / THREADS;
@@ -849,7 +853,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_k
         }
 #pragma unroll
         for (int kk = 0; kk < MT / 2; ++kk) {
-            u32x4 w[NT][N];
+            u32x4 w[NT][NV];
 #pragma unroll
             for (int u = 0; u < NT; ++u) {
                 const float base = top[u] == -__builtin_inff() ? 0.0f : top[u];
@@ -866,7 +870,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_k
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[i] *= f[i / 4][i % 4];
                 }
-                bf16_sums<N>(x, w[u]);
+                bf16_sums<NV>(x, w[u]);
             }
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
@@ -876,7 +880,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_k
 #pragma unroll
                 for (int u = 0; u < NT; ++u)
 #pragma unroll
-                    for (int e = N - 1; e >= 0; --e) acc[t][u] = multiply_bf16(vt, w[u][e], acc[t][u]);
+                    for (int e = NV - 1; e >= 0; --e) acc[t][u] = multiply_bf16(vt, w[u][e], acc[t][u]);
             }
         }
     };
