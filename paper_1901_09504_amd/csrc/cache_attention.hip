@@ -174,7 +174,7 @@ __device__ __forceinline__ TileOf tile_sequence(const Attention& p, int tile) {
         begin = t.first * p.G / ROWS + t.b;
     }
     t.row0 = (tile - begin) * ROWS;
-    if (t.row0 >= t.tokens * p.G) t.b = -1;
+    if (t.row0 < 0 || t.row0 >= t.tokens * p.G) t.b = -1;       // (below 0 where offsets do not ascend)
     return t;
 }
 

@@ -1,7 +1,9 @@
 """The quantized cache on the GPU, further: how fine the weights of the values are, and cases at the edges of what a call may be given."""
+import numpy as np
 import pytest
 import torch
 
+from paper_1901_09504_amd import binding as B
 from tests import gpu_util as G
 from tests import test_cache as C
 from tests.test_cache import BF16, F16, F32, INT8, MX4, Pool, check_attention, fill
@@ -24,3 +26,30 @@ def test_weights_of_the_values_have_16_bits_with_bf16_queries(monkeypatch, fmt, 
     pool = Pool(fmt, held, 2, D, 32, seed=D)
     fill(pool, 4)
     check_attention(pool, new, 4, BF16, window=window)
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("T,Hq", [(100, 6), (400, 6), (37, 2)])
+def test_offsets_that_do_not_ascend_stay_inside_the_tensors(fmt, T, Hq):
+    """They are against the interface, and what comes out is nobody's; but nothing is read or written beyond the tensors, by either kernel and
+    for sequences that a wave looks at together or searches."""
+    H, D = 2, 64
+    pool = Pool(fmt, [70], H, D, 16, seed=1)
+    fill(pool, 1)
+    rng = np.random.default_rng(T)
+    lists = [[0, T, 0, T], [T, T, 0, 0, T], [T, 0], [5, -3, 2 ** 31 - 1, -2 ** 31, 9], [0, 0, T, 0, T // 2, 3, T], [T] * 40 + [0] * 25,
+             rng.integers(-T, 2 * T, 30).tolist(), rng.integers(0, T + 1, 5).tolist(), rng.permutation(90).tolist(), [T] * 100 + [0] * 50,
+             rng.integers(0, T + 1, 200).tolist()]
+    for cu in lists:
+        n = len(cu) - 1
+        table = torch.full((n, 5), int(pool.table[0, 0]), dtype=torch.int32, device="cuda")
+        starts = torch.from_numpy(rng.integers(-5, 60, n).astype(np.int32)).cuda()
+        whole = torch.full((T + 64, Hq, D), 7.0, dtype=BF16, device="cuda")
+        lses = torch.full((T + 64, Hq), 7.0, device="cuda")
+        q, y, lse = torch.zeros((T + 64, Hq, D), dtype=BF16, device="cuda")[32:-32], whole[32:-32], lses[32:-32]
+        for most in (70, 4000):                                              # in parts too
+            ws = C.workspace(T, n, H, Hq, D, most)
+            B.ocs_cache_attention(q, Hq * D, D, Hq, T, G.dev(np.array(cu, dtype=np.int64).astype(np.int32)), starts, n, most, *pool.args(table), 0.1,
+                                  0, y, Hq * D, D, lse, ws)
+        for t in (whole, lses):
+            assert bool((t[:32] == 7).all()) and bool((t[-32:] == 7).all()), cu
