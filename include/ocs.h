@@ -592,7 +592,7 @@ int ocs_forward_mx(const void *X, int type, int64_t M, int C, int g, int64_t ldx
  *   head i / (query_heads / heads).  Over the positions j that a token at position p sees, j <= p, j > p - window (window 0: all),
  *   j < most, with a page that is there:
  *        s_j = scale * q . k_j,   Y[t, i] = sum exp(s_j) v_j / sum exp(s_j),   lse[t, i] = log sum exp(s_j)   (dense fp32, may be NULL).
- *   A token that sees none: Y 0, lse -inf.  One that sees a row with NaN (a value with scales from 253 on): Y NaN, and lse NaN for a key,
+ *   A token that sees none: Y 0, lse -inf.  One that sees a row with NaN (a value any of whose scales is 253 or more): Y NaN, and lse NaN for a key,
  *   for a value NaN or the number.  What rows that it does not see hold does not matter.  `most` is at least the longest sequence's
  *   positions, this call's among them, and at most 2^31 - 2^16.
  *   Scores and sums in fp32, as are queries times 2^key_depth, with weights up to 2^8 (values whose sum times 2^8 passes fp32's range come

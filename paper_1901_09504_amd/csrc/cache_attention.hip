@@ -112,6 +112,14 @@ __device__ __forceinline__ float over_quarters_sum(float v) {
     return a + b;
 }
 
+// Bits that any of each 16 neighbouring lanes has.
+__device__ __forceinline__ unsigned or_of_16(unsigned v) {
+    v |= (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xF, 0xF, true);     // lanes of a row turned by 1, 2, 4, 8
+    v |= (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xF, 0xF, true);
+    v |= (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xF, 0xF, true);
+    return v | (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true);
+}
+
 // `BYTES` bytes at an address that is a multiple of its largest power of two
 template <int BYTES>
 __device__ __forceinline__ void load_bytes(const uint8_t* p, unsigned (&w)[(BYTES + 3) / 4]) {
@@ -243,8 +251,14 @@ __device__ __forceinline__ TileOf long_tile_sequence(const Attention& p, int til
 constexpr float kSlack = 8.0f;
 
 // Scale bytes of values from here on are no numbers: 255 by definition, the two below it because 6 times their power of two is beyond
-// bf16 (no row that was written has them, but rubbish where nothing is seen may, and infinity times a weight of 0 is NaN).
+// bf16 (no row that was written has them, but rubbish where nothing is seen may, and infinity times a weight of 0 is NaN).  One such block makes
+// the row none, whichever it is.
 constexpr unsigned kNoNumber = 253;
+
+// whether any of four scale bytes is no number: their low seven bits carry into the eighth, which is set
+__device__ __forceinline__ bool any_no_number(unsigned bytes) {
+    return (((bytes & 0x7F7F7F7Fu) + (256 - kNoNumber) * 0x01010101u) & bytes & 0x80808080u) != 0u;
+}
 
 constexpr int kAttendWaves = 4;
 
@@ -463,12 +477,17 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend_rows_kernel(Atten
                     highest = vscale[i][e] > highest ? vscale[i][e] : highest;
                 }
             if (__any(highest >= kNoNumber)) {              // a NaN for those who see it, nothing for the others
+                unsigned bad = 0;                           // a bit per position; its blocks are those of the quarter's 16 lanes
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (vscale[i][0] < kNoNumber && (32 % DT == 0 || vscale[i][1] < kNoNumber)) continue;
-                    if (sees >> i & 1) w[i] = __uint_as_float(0x7FC00000u);
-                    vscale[i][0] = vscale[i][1] = 127u;
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (vscale[i][0] >= kNoNumber || (32 % DT != 0 && vscale[i][1] >= kNoNumber)) {
+                        bad |= 1u << i;
+                        vscale[i][0] = vscale[i][1] = 127u;
+                    }
+                bad = or_of_16(bad) & sees;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (bad >> i & 1) w[i] = __uint_as_float(0x7FC00000u);
             }
         } else if (whole) {
 #pragma unroll
@@ -697,7 +716,8 @@ __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_k
     // codes of KT positions on their way: 16 of a key and of a value to a lane
     struct Codes {
         unsigned k[PIECE / 4], v[PIECE / 4];
-        float kstep, vstep;                                 // 4 bits: the scale bytes' numbers
+        float kstep, vstep;                                 // 4 bits: of the key, the scale byte's number
+        unsigned vscale[(D / 32 + 3) / 4];                  // and the value's scale bytes, all of them
     };
     Codes codes[LOADS];
     int page[LOADS], row_of[LOADS];
@@ -731,7 +751,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_k
                 load_bytes<PIECE>(values + r * ROWB + part_of(u) * PIECE, codes[u].v);
                 if constexpr (MX) {
                     codes[u].kstep = mx_scale_value(kscales[r * (D / 32) + part_of(u) / 2]);
-                    codes[u].vstep = mx_scale_value(vscales[r * (D / 32) + part_of(u) / 2]);
+                    load_bytes<D / 32>(vscales + r * (D / 32), codes[u].vscale);
                 } else {
                     codes[u].kstep = *reinterpret_cast<const float*>(kscales + r * 4);
                     codes[u].vstep = *reinterpret_cast<const float*>(vscales + r * 4);
@@ -763,12 +783,16 @@ __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_k
                 uint8_t* k = lds + (buf * KT + key) * KPITCH + col * 32;
                 *reinterpret_cast<u32x4*>(k) = x[0];
                 *reinterpret_cast<u32x4*>(k + 16) = x[1];
-                const bool number = (__float_as_uint(codes[u].vstep) >> 23 & 0xFFu) < (MX ? kNoNumber : 0xFFu);
+                bool number = true;
                 if constexpr (MX) {
 #pragma unroll
+                    for (int e = 0; e < (D / 32 + 3) / 4; ++e) number = number && !any_no_number(codes[u].vscale[e]);
+                    const unsigned four = D > 128 && col >= 8 ? codes[u].vscale[(D / 32 - 1) / 4] : codes[u].vscale[0];
+#pragma unroll
                     for (int e = 0; e < PIECE / 4; ++e) codes[u].v[e] = number ? codes[u].v[e] : 0u;
-                    numbers(codes[u].v, number ? codes[u].vstep : 1.0f, x);
+                    numbers(codes[u].v, number ? mx_scale_value(four >> (col / 2 % 4 * 8) & 0xFFu) : 1.0f, x);
                 } else {
+                    number = (__float_as_uint(codes[u].vstep) >> 23 & 0xFFu) < 0xFFu;
                     numbers(codes[u].v, 1.0f, x);
                 }
                 uint8_t* v = lds + 2 * KT * KPITCH + (buf * KT + key) * VPITCH + col * 32;

@@ -53,3 +53,28 @@ def test_offsets_that_do_not_ascend_stay_inside_the_tensors(fmt, T, Hq):
                                   0, y, Hq * D, D, lse, ws)
         for t in (whole, lses):
             assert bool((t[:32] == 7).all()) and bool((t[-32:] == 7).all()), cu
+
+
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 224, 256])
+@pytest.mark.parametrize("G_,dtype", [(1, F32), (3, BF16), (2, F16)])
+@pytest.mark.parametrize("new", [3, 60])
+def test_a_value_with_one_block_that_is_no_number_is_none_for_those_who_see_it(D, G_, dtype, new):
+    """In the first, a middle or the last block: every output of the tokens that see it is NaN, the others' are what they are without it."""
+    held, at, blocks = 130, 128, D // 32
+    for block, byte in ((0, 255), (blocks // 2, 254), (blocks - 1, 253), (blocks - 1, 255)):
+        pool = Pool(MX4, [held], 2, D, 16, seed=8)
+        fill(pool, 8)
+        q = torch.randn((new, 2 * G_, D), generator=torch.Generator().manual_seed(0)).to(dtype).cuda()
+        cu, st, _ = C.tokens_of([new], [held - new])
+        ys = []
+        for bad in (False, True):
+            if bad:
+                page, row = pool.row(0, at)
+                pool.scales[1][page, 1, row, block] = byte
+            y = torch.full_like(q, 7.0)
+            B.ocs_cache_attention(q, 2 * G_ * D, D, 2 * G_, new, cu, st, 1, held, *pool.args(), 0.1, 0, y, 2 * G_ * D, D, None,
+                                  C.workspace(new, 1, 2, 2 * G_, D, held))
+            ys.append(y)
+        sees = torch.arange(held - new, held) >= at
+        assert bool(ys[1][sees, G_:].isnan().all()), (block, byte)
+        assert torch.equal(ys[1][~sees], ys[0][~sees]) and torch.equal(ys[1][:, :G_], ys[0][:, :G_]) and bool(ys[0].isfinite().all())
