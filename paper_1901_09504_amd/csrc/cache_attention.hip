@@ -986,9 +986,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attention p) {
     float sum = 0.0f;
     for (int i = lane; i < p.parts; i += 64) {
         const float total = p.stats[2 * (i * rows + row) + 1];
-        // at least 2^-126 where there are positions: nothing beside the part with the maximum, but a NaN stays one
-        const float f = total == 0.0f ? 0.0f : __builtin_fmaxf(__builtin_amdgcn_exp2f(p.stats[2 * (i * rows + row)] - base), 0x1p-126f);
-        sum += total * f;
+        // below 0: a part without positions, which is left out; any other counts, if only by 0, so that a NaN among its values stays one
+        const float f = total == 0.0f ? -1.0f : __builtin_amdgcn_exp2f(p.stats[2 * (i * rows + row)] - base);
+        if (total != 0.0f) sum += total * f;
         weight[i] = f;                                      // (by every wave, the same)
     }
 #pragma unroll
@@ -997,7 +997,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attention p) {
     if (t >= past) return;                                  // behind the last sequence
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     auto add = [&](const f32x4& x, float w) {
-        if (w != 0.0f)                                      // (NaN is not 0)
+        if (!(w < 0.0f))                                    // (NaN is not below 0)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += x[e] * w;
     };
@@ -1008,7 +1008,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attention p) {
 #pragma unroll 4
         for (int k = group + AHEAD * groups; k < p.parts; k += groups) {
             const float w = weight[k];
-            if (w != 0.0f) add(columns(k), w);
+            if (!(w < 0.0f)) add(columns(k), w);
         }
     }
     partial[tid] = v;

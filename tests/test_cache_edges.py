@@ -78,3 +78,27 @@ def test_a_value_with_one_block_that_is_no_number_is_none_for_those_who_see_it(D
         sees = torch.arange(held - new, held) >= at
         assert bool(ys[1][sees, G_:].isnan().all()), (block, byte)
         assert torch.equal(ys[1][~sees], ys[0][~sees]) and torch.equal(ys[1][:, :G_], ys[0][:, :G_]) and bool(ys[0].isfinite().all())
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("new", [1, 60])
+def test_large_values_whose_weight_is_nothing_add_nothing(fmt, dtype, new):
+    """Position 1500's score is 4096 above the others', which lie in parts of their own and hold values 2^140 times as large: their weights
+    are 0, and the output is position 1500's value, its weight's and its own rounding off."""
+    L = 2048
+    pool = Pool(fmt, [L], 1, 64, 16, seed=12)
+    k, v = torch.zeros((L, 1, 64), device="cuda"), torch.full((L, 1, 64), 2.0 ** 100, device="cuda")
+    k[1500], v[1500] = 8, C.random_rows(1, 1, 64, F32, 13)[0] * 2.0 ** -40
+    C.write(pool, k, v, [L], [0])
+    q = torch.full((new, 1, 64), 8.0, dtype=dtype, device="cuda")
+    y, lse = torch.zeros_like(q), torch.zeros((new, 1), device="cuda")
+    cu, st, _ = C.tokens_of([new], [L - new])
+    ws = C.workspace(new, 1, 1, 1, 64, L)
+    assert ws is not None
+    B.ocs_cache_attention(q, 64, 64, 1, new, cu, st, 1, L, *pool.args(), 1.0, 0, y, 64, 64, lse, ws)
+    page, row = pool.row(0, 1500)
+    want = pool.numbers(1)[page, 0, row]
+    assert bool(((y[:, 0].double() - want).abs() <= want.abs() * (C.HALF_STEP[dtype] + 2.0 ** -15)).all())
+    k1500 = pool.numbers(0)[page, 0, row]
+    assert bool(((lse.double() - 8 * k1500.sum()).abs() <= 4096 * 2.0 ** -21).all())
