@@ -708,9 +708,9 @@ __global__ __launch_bounds__(kTileWaves * 64, 8 / kTileWaves) void attend_tile_k
     }
     if (wave_row < rows) {
         const int last_row = wave_row + 16 * NT < rows ? wave_row + 16 * NT - 1 : rows - 1;
-        const Seen a = positions_seen(p, start + (row0 + wave_row) / p.G), z = positions_seen(p, start + (row0 + last_row) / p.G);
-        wave_from = a.count > 0 ? a.from : z.from;
-        wave_end = z.count > 0 ? z.from + z.count : a.from + a.count;
+        const int64_t from = start + (row0 + wave_row) / p.G - p.window + 1, to = start + (row0 + last_row) / p.G + 1;
+        wave_from = p.window > 0 && from > 0 ? (int)(from < p.held ? from : p.held) : 0;
+        wave_end = to < 0 ? 0 : to < p.held ? (int)to : p.held;
     }
 
     // codes of KT positions on their way: 16 of a key and of a value to a lane

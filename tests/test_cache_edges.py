@@ -102,3 +102,18 @@ def test_large_values_whose_weight_is_nothing_add_nothing(fmt, dtype, new):
     assert bool(((y[:, 0].double() - want).abs() <= want.abs() * (C.HALF_STEP[dtype] + 2.0 ** -15)).all())
     k1500 = pool.numbers(0)[page, 0, row]
     assert bool(((lse.double() - 8 * k1500.sum()).abs() <= 4096 * 2.0 ** -21).all())
+
+
+@pytest.mark.parametrize("fmt,D", [(INT8, 64), (MX4, 128), (INT8, 160)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [3, 5, 40, 0])
+@pytest.mark.parametrize("columns", [2, 5, 6, 7])
+def test_windows_over_the_end_of_the_table(fmt, D, dtype, window, columns):
+    """Tokens on both sides of the table's last position: the later ones of a wave's see none of it, those before them do."""
+    new, held = [70, 75], [126, 131]                                         # 32 tokens to a wave, from position 56 on
+    pool = Pool(fmt, held, 1, D, 16, seed=3)
+    pool.table = np.ascontiguousarray(pool.table[:, :columns])
+    pool.held = [min(n, 16 * columns) for n in held]
+    fill(pool, 3)
+    pool.held = held
+    check_attention(pool, new, 1, dtype, window=window)
