@@ -522,7 +522,7 @@ class TokenCache:
 
     def append(self, K, V, counts, which=None):
         """K, V [T, heads, D] in fp32, bf16 or fp16: the next counts[i] tokens of sequence which[i] (all of them in order if None), one
-        sequence after the other.  MemoryError where the pool has too few pages left; nothing is changed then."""
+        sequence after the other.  MemoryError where the pool has too few pages left; after that or any other error nothing is changed."""
         which = self._sequences(which, counts)
         assert len(which) == len(set(which)) and all(n >= 0 for n in counts) and V.dtype == K.dtype
         self._check_rows(K, counts, self.heads)
@@ -530,10 +530,19 @@ class TokenCache:
         need = [-(-(self.lengths[b] + n) // self.page_rows) - len(self.tables[b]) for b, n in zip(which, counts)]
         if sum(need) > len(self.spare):
             raise MemoryError(f"{sum(need)} pages wanted, {len(self.spare)} left")
+        taken = [self.spare.pop() for _ in range(sum(need))]
+        at = 0
         for b, n in zip(which, need):
-            self.tables[b] += [self.spare.pop() for _ in range(n)]
-        cu, starts, table = self._on_device(which, counts, [self.lengths[b] for b in which])
-        B.ocs_cache_write(K, K.stride(0), K.stride(1), V, V.stride(0), V.stride(1), K.shape[0], cu, starts, len(which), *self._pool(table))
+            self.tables[b] += taken[at:at + n]
+            at += n
+        try:
+            cu, starts, table = self._on_device(which, counts, [self.lengths[b] for b in which])
+            B.ocs_cache_write(K, K.stride(0), K.stride(1), V, V.stride(0), V.stride(1), K.shape[0], cu, starts, len(which), *self._pool(table))
+        except BaseException:                               # a type that no call takes, a copy that failed: the pages are spare again
+            for b, n in zip(which, need):
+                del self.tables[b][len(self.tables[b]) - n:]
+            self.spare += reversed(taken)
+            raise
         for b, n in zip(which, counts):
             self.lengths[b] += n
 

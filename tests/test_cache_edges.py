@@ -117,3 +117,33 @@ def test_windows_over_the_end_of_the_table(fmt, D, dtype, window, columns):
     fill(pool, 3)
     pool.held = held
     check_attention(pool, new, 1, dtype, window=window)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_an_append_that_fails_leaves_the_cache_as_it_was(monkeypatch, bits):
+    from paper_1901_09504_amd.layer import TokenCache
+
+    def state(cache):
+        return [list(t) for t in cache.tables], list(cache.lengths), list(cache.spare)
+
+    def fails(*_):
+        raise RuntimeError("no copy")
+
+    cache = TokenCache(2, 4, 2, 64, page_rows=16, bits=bits)
+    rows = C.random_rows(40, 2, 64, F32, 1)
+    for begun in (0, 5):
+        if begun:
+            cache.append(rows[:begun], rows[:begun], [begun], [1])
+        before = state(cache)
+        with pytest.raises(B.OcsError):                                      # an element type that no call takes
+            cache.append(rows.double(), rows.double(), [40], [0])
+        assert state(cache) == before
+        with monkeypatch.context() as m, pytest.raises(RuntimeError, match="no copy"):
+            m.setattr(TokenCache, "_on_device", fails)
+            cache.append(rows[:38], rows[:38], [20, 18])
+        assert state(cache) == before
+    cache.append(rows[:31], rows[:31], [1, 30])
+    assert cache.lengths == [1, 35] and [len(t) for t in cache.tables] == [1, 3] and not cache.spare
+    want = TokenCache(2, 4, 2, 64, page_rows=16, bits=bits)
+    want.append(torch.cat([rows[:1], rows[:5], rows[1:31]]), torch.cat([rows[:1], rows[:5], rows[1:31]]), [1, 35])
+    assert all(torch.equal(a, b) for a, b in zip(cache.read(), want.read()))
