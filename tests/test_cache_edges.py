@@ -147,3 +147,72 @@ def test_an_append_that_fails_leaves_the_cache_as_it_was(monkeypatch, bits):
     want = TokenCache(2, 4, 2, 64, page_rows=16, bits=bits)
     want.append(torch.cat([rows[:1], rows[:5], rows[1:31]]), torch.cat([rows[:1], rows[:5], rows[1:31]]), [1, 35])
     assert all(torch.equal(a, b) for a, b in zip(cache.read(), want.read()))
+
+
+def eight_bits(x):
+    """fp32 rows [.., D] that are finite and not all zeros -> codes and steps of Eq. 1, each quotient and product rounded to 32 bits once."""
+    T = np.abs(x).max(-1).astype(np.float64)
+    factor, step = (127 / T).astype(np.float32), (T / 127).astype(np.float32)
+    scaled = (x.astype(np.float64) * factor[..., None].astype(np.float64)).astype(np.float32)
+    return np.rint(scaled).clip(-127, 127).astype(np.int8), step
+
+
+def check_rows(fmt, dtype, H, D, P, new, held, starts, extra, seed):
+    """Writes the tokens into a pool, compares every row of it with the definition (the others as they were), and what is read back."""
+    pool = Pool(fmt, held, H, D, P, seed=seed, halved=seed % 2 == 1)
+    before = [t.clone() for t in pool.codes + pool.scales]
+    T = sum(new)
+    rows = [C.random_rows(T + extra, H, D, dtype, seed + i) for i in (1, 2)]
+    C.write(pool, *rows, new, starts)
+    position = np.concatenate([np.arange(s, s + n) for s, n in zip(starts, new)]).astype(np.int64)
+    page = pool.table[np.repeat(np.arange(len(new)), new), position // P].astype(np.int64)
+    at = torch.from_numpy(page * P + position % P).cuda()                    # [T], of [pages, P]
+    assert len(at.unique()) == T
+    for i in range(2):
+        x = G.host(rows[i][:T].float())
+        if pool.depth[i] is not None:
+            x = (x * np.ldexp(np.float32(1), -G.host(pool.depth[i]).astype(np.int64)).astype(np.float32)).astype(np.float32)
+        if fmt == INT8:
+            codes, scales = eight_bits(x)
+            few = [C.ref.quantize(np.ascontiguousarray(r[None]), 8, ldq=D) for r in x[:3, 0]]
+            assert all(np.array_equal(q[0], c) and s[1] == t for (q, s), c, t in zip(few, codes[:3, 0], scales[:3, 0]))
+        else:
+            codes, scales = C.on_grids(x.reshape(-1, D))
+            codes, scales = C.packed(codes, D // 2).reshape(T, H, -1), scales.reshape(T, H, -1)
+        for now, was, new_rows in ((pool.codes[i], before[i], codes), (pool.scales[i], before[2 + i], scales)):
+            if now.dim() == 3:
+                now, was, new_rows = now[..., None], was[..., None], new_rows[..., None]
+            want = was.transpose(1, 2).flatten(0, 1).contiguous()            # [pages * P, H, ..]
+            want[at] = torch.from_numpy(np.ascontiguousarray(new_rows)).cuda()
+            assert torch.equal(now.transpose(1, 2).flatten(0, 1).contiguous().view(torch.uint8), want.view(torch.uint8))
+    back = C.read(pool, F32, new, starts, extra=extra)
+    for i in range(2):
+        want = pool.numbers(i).transpose(1, 2).flatten(0, 1)[at]
+        assert bool(((back[i][:T].double() - want).abs() <= 2.0 ** -23 * 1.01 * want.abs()).all()) and bool((back[i][T:] == 7).all())
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("B_", [64, 65, 100, 300])
+@pytest.mark.parametrize("kind", ["a token each", "an empty one in front", "empty ones among them", "tokens behind the last"])
+def test_rows_of_many_sequences(fmt, B_, kind):
+    rng = np.random.default_rng(B_)
+    new, extra = [1] * B_, 0
+    if kind == "an empty one in front":
+        new[0] = 0
+    elif kind == "empty ones among them":
+        new = [int(n) for n in rng.choice([0, 0, 1, 2, 37], B_)]
+    elif kind == "tokens behind the last":
+        new, extra = [int(n) for n in rng.integers(0, 4, B_)], 9
+    starts = [int(s) for s in rng.integers(0, 50, B_)]
+    check_rows(fmt, BF16, 3, 64, 16, new, [s + n for s, n in zip(starts, new)], starts, extra, B_)
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("dtype,H,D,P,new", [(F32, 3, 256, 32, [2001, 0, 1500, 77]), (BF16, 5, 96, 16, [4099, 1]), (F16, 7, 32, 64, [9001]),
+                                             (BF16, 1, 160, 48, [5000]), (F32, 8, 128, 64, [1, 2500]), (F16, 33, 64, 16, [1111, 0, 222])])
+def test_rows_of_long_prompts(fmt, dtype, H, D, P, new):
+    """Enough rows that a wave takes four times as many as it holds at once; heads that leave its last times part empty."""
+    lanes = 4 if D <= 32 else 8 if D <= 64 else 16 if D <= 128 else 32
+    assert -(-2 * H // (64 // lanes)) * sum(new) >= 16 * 256
+    starts = [5 * i for i in range(len(new))]
+    check_rows(fmt, dtype, H, D, P, new, [s + n for s, n in zip(starts, new)], starts, 2, H)
