@@ -597,6 +597,9 @@ int ocs_forward_mx(const void *X, int type, int64_t M, int C, int g, int64_t ldx
  *   positions, this call's among them, and at most 2^31 - 2^16.
  *   Scores and sums in fp32, as are queries times 2^key_depth, with weights up to 2^8 (values whose sum times 2^8 passes fp32's range come
  *   out infinite or NaN), each off by 2^-16 of itself at most where it meets the values (fp32: 2^-24).
+ *   What is fast: the kernel goes by the call's mean of tokens times queries a head to a sequence, so prompts and single tokens are calls of their
+ *   own (63 tokens to 8192 and a prompt of 4096, 8 bits: 537 us, apart 131 and 265), and parts of positions follow `most`, so it is as tight as
+ *   the program knows it (one token at 4096: 11 us, with most = 131072 29).
  *   workspace: at least ocs_cache_attention_workspace_bytes() bytes, 256-byte aligned; it may be NULL where that is 0.  Needs no
  *   initialisation.
  * T = 0 or B = 0 is OCS_OK and launches nothing.

@@ -1035,10 +1035,22 @@ struct AttentionPlan {
 };
 
 // Which kernel, and parts of the positions where the tiles alone leave compute units idle.
+//
+// Tiles of many rows from five eighths of one to a sequence on, by the call's mean (us, 16 rows a workgroup / tiles; 8 bits, bf16, sequences of an
+// eighth of the longest on).  A call that mixes prompts with single tokens goes one way altogether.
+//   rows:                            48             64             80             96            128
+//   64 to 8192, 4 heads of 128   195 / 186      196 / 196      254 / 216      265 / 202      324 / 258
+//   64, in 4 bits                143 / 179      151 / 189      198 / 214      205 / 196      239 / 248
+//   64 to 1024                  52.7 / 61.2    57.6 / 66.7    74.3 / 73.6    79.5 / 79.2    60.9 / 81.2
+//   16 to 2048, heads of 256    55.5 / 37.5    54.0 / 43.2    67.0 / 63.2    62.8 / 57.9    76.1 / 57.7
+// Workgroups a compute unit: 2 of up to three sequences, whose parts the join has to read, 8 of more, whose lengths differ (us, 2 / 4 / 8; 8 bits, 8
+// heads of 128, 4 queries each): one of 100003 41.7 / 47.8 / 51.8, two of 100000 82.7 / 91.1 / 90.8, three to 60000 51.0 / 50.3 / 53.6, 8 to 30000
+// 77.1 / 63.1 / 64.1, 64 to 8192 149 / 142 / 136.
 static AttentionPlan plan_attention(int64_t T, int64_t B, int64_t H, int64_t Hq, int64_t D, int64_t most, int64_t window) {
     const int64_t G = Hq / H, cus = compute_units(), range = window > 0 && window + T < most ? window + T : most;
-    const bool many = T * G >= 48 * B;
-    const int64_t rows = !many ? 16 : D <= 128 ? 128 : 64, tiles = T * G / rows + B, per_cu = B < 4 ? 2 * B : 8;
+    const int64_t tile_rows = D <= 128 ? 128 : 64;
+    const bool many = 8 * T * G >= 5 * tile_rows * B;
+    const int64_t rows = many ? tile_rows : 16, tiles = T * G / rows + B, per_cu = B < 4 ? 2 : 8;
     AttentionPlan a{many, tiles, 1, 0};
     const int64_t want = ceil_div(per_cu * cus, tiles * H), can = ceil_div(range, 32 * kAttendWaves * 2), fit = ((int64_t)48 << 20) / (T * Hq * (D + 2) * 4);
     int64_t parts = want < can ? want : can;

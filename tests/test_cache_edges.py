@@ -57,7 +57,7 @@ def test_offsets_that_do_not_ascend_stay_inside_the_tensors(fmt, T, Hq):
 
 @pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 224, 256])
 @pytest.mark.parametrize("G_,dtype", [(1, F32), (3, BF16), (2, F16)])
-@pytest.mark.parametrize("new", [3, 60])
+@pytest.mark.parametrize("new", [3, 60, 100])
 def test_a_value_with_one_block_that_is_no_number_is_none_for_those_who_see_it(D, G_, dtype, new):
     """In the first, a middle or the last block: every output of the tokens that see it is NaN, the others' are what they are without it."""
     held, at, blocks = 130, 128, D // 32
@@ -82,7 +82,7 @@ def test_a_value_with_one_block_that_is_no_number_is_none_for_those_who_see_it(D
 
 @pytest.mark.parametrize("fmt", [INT8, MX4])
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("new", [1, 60])
+@pytest.mark.parametrize("new", [1, 60, 100])
 def test_large_values_whose_weight_is_nothing_add_nothing(fmt, dtype, new):
     """Position 1500's score is 4096 above the others', which lie in parts of their own and hold values 2^140 times as large: their weights
     are 0, and the output is position 1500's value, its weight's and its own rounding off."""
@@ -110,7 +110,7 @@ def test_large_values_whose_weight_is_nothing_add_nothing(fmt, dtype, new):
 @pytest.mark.parametrize("columns", [2, 5, 6, 7])
 def test_windows_over_the_end_of_the_table(fmt, D, dtype, window, columns):
     """Tokens on both sides of the table's last position: the later ones of a wave's see none of it, those before them do."""
-    new, held = [70, 75], [126, 131]                                         # 32 tokens to a wave, from position 56 on
+    new, held = [90, 95], [146, 151]                                         # 32 tokens to a wave, from position 56 on
     pool = Pool(fmt, held, 1, D, 16, seed=3)
     pool.table = np.ascontiguousarray(pool.table[:, :columns])
     pool.held = [min(n, 16 * columns) for n in held]
@@ -216,3 +216,29 @@ def test_rows_of_long_prompts(fmt, dtype, H, D, P, new):
     assert -(-2 * H // (64 // lanes)) * sum(new) >= 16 * 256
     starts = [5 * i for i in range(len(new))]
     check_rows(fmt, dtype, H, D, P, new, [s + n for s, n in zip(starts, new)], starts, 2, H)
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("G_,window", [(1, 0), (4, 37), (7, 1)])
+def test_tiles_of_many_rows(fmt, dtype, D, G_, window):
+    """Prompts among sequences without tokens and with one: from five eighths of a tile's rows to a sequence on they go by tiles."""
+    new, held = ([170, 0, 129, 1, 64], [200, 3, 129, 90, 99]) if G_ == 1 else ([33, 0, 70, 1, 25], [133, 3, 70, 90, 26])
+    if D > 128:
+        new, held = [n // 2 for n in new], [h - n + n // 2 for h, n in zip(held, new)]
+    assert 8 * sum(new) * G_ >= 5 * (128 if D <= 128 else 64) * len(new) or G_ == 1
+    pool = Pool(fmt, held, 2, D, 16, seed=D + G_, halved=G_ == 4)
+    fill(pool, G_)
+    check_attention(pool, new, 2 * G_, dtype, window=window, seed=D, extra=2)
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+def test_tiles_of_more_sequences_than_a_wave_has_lanes(fmt):
+    rng = np.random.default_rng(5)
+    new = [int(n) for n in rng.integers(0, 50, 70)]
+    held = [n + int(e) for n, e in zip(new, rng.integers(0, 90, 70))]
+    pool = Pool(fmt, held, 1, 64, 16, seed=2)
+    fill(pool, 2)
+    assert 8 * sum(new) * 4 >= 5 * 128 * 70
+    check_attention(pool, new, 4, BF16, window=30)
