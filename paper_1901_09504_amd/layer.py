@@ -455,8 +455,8 @@ class TokenCache:
     positions each sequence has, is kept on the host, and every call sends what it needs of that to the device; a program that captures
     its steps into graphs keeps the table and the positions on the device itself and makes the calls of `binding`.
     key_depth, value_depth: int32 [heads, D], how often a channel is halved before its row's grid (outlier_depths gives them).
-    Calls run on the current stream, of the pool's device; one on another stream than the last waits for that one's work.  Not to be captured: what a call sends
-    comes from the host."""
+    Calls run on the current stream, of the pool's device; one on another stream than the last waits for that one's work.  Refused while the stream is captured:
+    what a call sends comes from the host."""
 
     def __init__(self, sequences, pages, heads, D, page_rows=64, bits=8, key_depth=None, value_depth=None, device="cuda"):
         assert bits in (8, 4)
@@ -479,6 +479,7 @@ class TokenCache:
         assert self._stream.device == self.keys.device, "the pool's device is to be the current one"
 
     def _use_on_current_stream(self):
+        assert not torch.cuda.is_current_stream_capturing(), "a TokenCache's calls are not to be captured"
         stream = torch.cuda.current_stream()
         if stream != self._stream:
             assert stream.device == self.keys.device, "the pool's device is to be the current one"

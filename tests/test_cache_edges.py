@@ -242,3 +242,18 @@ def test_tiles_of_more_sequences_than_a_wave_has_lanes(fmt):
     fill(pool, 2)
     assert 8 * sum(new) * 4 >= 5 * 128 * 70
     check_attention(pool, new, 4, BF16, window=30)
+
+
+def test_a_cache_that_is_captured_refuses_and_stays_as_it_was():
+    from paper_1901_09504_amd.layer import TokenCache
+
+    cache = TokenCache(1, 4, 2, 64, page_rows=16)
+    rows = C.random_rows(20, 2, 64, BF16, 1)
+    cache.append(rows, rows, [20])
+    want, stream = cache.attend(rows, [20]), cache._stream
+    for call in (lambda: cache.append(rows, rows, [20]), lambda: cache.attend(rows, [20]), lambda: cache.read()):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph), pytest.raises(AssertionError, match="captured"):
+            call()
+        assert cache.lengths == [20] and len(cache.tables[0]) == 2 and cache._stream == stream
+    assert torch.equal(cache.attend(rows, [20]), want)
