@@ -496,6 +496,7 @@ class TokenCache:
 
     def free(self, sequence):
         """Gives the sequence's pages back: it has no positions."""
+        self._sequences([sequence], None)
         self.spare += reversed(self.tables[sequence])
         self.tables[sequence], self.lengths[sequence] = [], 0
 

@@ -257,3 +257,18 @@ def test_a_cache_that_is_captured_refuses_and_stays_as_it_was():
             call()
         assert cache.lengths == [20] and len(cache.tables[0]) == 2 and cache._stream == stream
     assert torch.equal(cache.attend(rows, [20]), want)
+
+
+def test_only_sequences_are_freed():
+    from paper_1901_09504_amd.layer import TokenCache
+
+    cache = TokenCache(2, 4, 2, 64, page_rows=16)
+    rows = C.random_rows(20, 2, 64, BF16, 1)
+    cache.append(rows, rows, [3, 17])
+    for none in (-1, 2):
+        with pytest.raises(AssertionError):
+            cache.free(none)
+    assert cache.lengths == [3, 17] and [len(t) for t in cache.tables] == [1, 2]
+    cache.free(0)
+    cache.free(0)                                                            # nothing left of it: nothing happens
+    assert cache.lengths == [0, 17] and sorted(cache.spare + cache.tables[1]) == [0, 1, 2, 3]
