@@ -92,13 +92,13 @@ def run_cache(sequences=4, length=200, heads=4, query_heads=8, D=64, vocab=10000
     noise = torch.rand(logits.shape, device=Q.device, generator=gen).clamp_min_(1e-20).log_().neg_().log_()
     ids = (logits - noise).argmax(1).to(torch.int32)
     exact, best = perplexity(logits, ids)
-    rows = [(32, 0.0, exact, 1.0)]
+    rows, prompt = [(32, 0.0, exact, 1.0)], max(length - 8, 0)
     of = [x.view(sequences, length, -1, D) for x in (Q, K, V)]
     for bits in (8, 4):
         for r in ratios:
             cache = TokenCache(sequences, sequences * -(-length // 32), heads, D, page_rows=32, bits=bits, key_depth=outlier_depths(K, r))
             y = torch.empty_like(of[0])
-            for begin, end in [(0, length - 8)] + [(i, i + 1) for i in range(length - 8, length)]:
+            for begin, end in ([(0, prompt)] if prompt else []) + [(i, i + 1) for i in range(prompt, length)]:
                 q, k, v = (x[:, begin:end].flatten(0, 1) for x in of)
                 counts = [end - begin] * sequences
                 cache.append(k, v, counts)

@@ -272,3 +272,12 @@ def test_only_sequences_are_freed():
     cache.free(0)
     cache.free(0)                                                            # nothing left of it: nothing happens
     assert cache.lengths == [0, 17] and sorted(cache.spare + cache.tables[1]) == [0, 1, 2, 3]
+
+
+@pytest.mark.parametrize("length", [1, 5, 8, 9])
+def test_scores_behind_a_cache_of_short_sequences(length):
+    """8 tokens one by one behind the prompt, or as many as there are."""
+    from paper_1901_09504_amd import score
+
+    rows = score.run_cache(sequences=2, length=length, vocab=100)
+    assert len(rows) == 5 and all(p >= 1 and 0 <= same <= 1 for _, _, p, same in rows)
