@@ -8,7 +8,7 @@
 // block's power of two goes into the number itself.  Queries are taken as sums of bf16 numbers, one for bf16 (8 bits), two for fp16 (16 bits,
 // where 11 count), three for fp32 (24): scores are as exact as 32-bit sums.  A weight is two of them, off by 2^-16 of itself at most, or three
 // for fp32, so that an output is off by its own rounding.  (One for bf16 would be a second rounding of that size: prompts off 64 bits by 0.0023
-// of their norm where two leave 0.0017, in 283 us where two take 333; single tokens, which wait for memory, take as long either way.)
+// of their norm where two leave 0.0017, in 283 us where two take 330; single tokens, which wait for memory, take as long either way.)
 #include <type_traits>
 
 #include "cache.h"
@@ -631,8 +631,9 @@ __device__ __forceinline__ u32x2 read_transposed(const uint8_t* lds) {
 // Many rows: 64 NT rows of a sequence and head per workgroup, 16 NT to each of its four waves.  The workgroup turns KT positions at a time into
 // bf16 numbers in LDS, once for all its rows, while the next positions' codes are on their way, and the waves multiply from there: keys a
 // row at a time, values transposed as they are read (ds_read_b64_tr_b16).  Rows of LDS are 4 and 8 banks apart beyond a multiple of 64, so
-// that what the matrix cores read at a time lies in different banks.  Bound by vector instructions (conversions, exponentials, factors: 55 % of the
-// time) and matrix cores (25 %), which overlap little: prompts of 512 to 1501 tokens in sequences to 6001, 32 heads on 8 of 128, 333 us, 0.57 PFLOP/s.
+// that what the matrix cores read at a time lies in different banks.  Bound by vector instructions (conversions, exponentials, factors, the weights' second halves: 51 % of
+// the time) and matrix cores (35 %), which overlap little: prompts of 512 to 1501 tokens in sequences to 6001, 32 heads on 8 of 128, 330 us, 0.57 PFLOP/s
+// (4 bits 313; fp16 queries 366, fp32 472).
 constexpr int kTileWaves = 4;
 template <Elem T, int D>
 struct AttendTile {

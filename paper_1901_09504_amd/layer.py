@@ -452,8 +452,9 @@ class TokenCache:
     """Keys and values of sequences of tokens, quantized as they come into pages of a pool, and attention over them.
 
     A sequence is a number 0 .. sequences - 1; it takes pages as it grows and gives them back when it is freed.  Which pages, and how many
-    positions each sequence has, is kept on the host, and every call sends what it needs of that to the device; a program that captures
-    its steps into graphs keeps the table and the positions on the device itself and makes the calls of `binding`.
+    positions each sequence has, is kept on the host, and every call sends what it needs of that to the device and waits for the copy (350 us
+    of the host for 64 sequences to 8192 positions, 55 for four of 500); a program for which that counts, or that captures its steps into graphs,
+    keeps the table and the positions on the device itself and makes the calls of `binding`.
     key_depth, value_depth: int32 [heads, D], how often a channel is halved before its row's grid (outlier_depths gives them).
     Calls run on the current stream, of the pool's device; one on another stream than the last waits for that one's work.  Refused while the stream is captured:
     what a call sends comes from the host."""
