@@ -281,3 +281,53 @@ def test_scores_behind_a_cache_of_short_sequences(length):
 
     rows = score.run_cache(sequences=2, length=length, vocab=100)
     assert len(rows) == 5 and all(p >= 1 and 0 <= same <= 1 for _, _, p, same in rows)
+
+
+@pytest.mark.parametrize("fmt", [INT8, MX4])
+def test_a_long_run_of_generation_in_one_graph(fmt):
+    """A step captured once for lengths that it does not know: positions advance on the device across pages and across the parts that the bound
+    `most` gives, a sequence without tokens of its own comes and goes; every replay against the same calls made eagerly, and the last
+    against 64 bits."""
+    H, Hq, D, P, steps = 2, 8, 128, 64, 12
+    n0 = [250, 1, 1532, 60]
+    held = [n + 10 * steps for n in n0]
+    pool, eager = (Pool(fmt, held, H, D, P, seed=3) for _ in range(2))
+    for p in (pool, eager):
+        fill(p, 3)
+    most, T = 4096, 4
+    cu = torch.arange(5, dtype=torch.int32, device="cuda")
+    starts = torch.tensor(n0, dtype=torch.int32, device="cuda")
+    kt, vt = (torch.empty((T, H, D), dtype=BF16, device="cuda") for _ in range(2))
+    qt, y = (torch.empty((T, Hq, D), dtype=BF16, device="cuda") for _ in range(2))
+    ws, other = C.workspace(T, 4, H, Hq, D, most), C.workspace(T, 4, H, Hq, D, most)
+    assert ws is not None
+    args = pool.args()
+
+    def step(st, offsets, out, args, ws):
+        B.ocs_cache_write(kt, H * D, D, vt, H * D, D, T, offsets, st, 4, *args)
+        B.ocs_cache_attention(qt, Hq * D, D, Hq, T, offsets, st, 4, most, *args, 0.1, 0, out, Hq * D, D, None, ws)
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step(starts, cu, y, args, ws)
+        starts.add_(cu.diff() * 10)                                          # (the positions between hold what fill() left there)
+    eager_args, at = eager.args(), list(n0)
+    for i in range(steps):
+        new = [1, 0, 1, 1] if i % 3 == 2 else [1, 1, 1, 1]
+        cu.copy_(torch.tensor([0] + list(np.cumsum(new))))
+        kt.copy_(C.random_rows(T, H, D, BF16, 10 + i))
+        vt.copy_(C.random_rows(T, H, D, BF16, 20 + i))
+        qt.copy_(C.random_rows(T, Hq, D, BF16, 30 + i))
+        graph.replay()
+        got = y[:sum(new)].clone()
+        torch.cuda.synchronize()
+        want = torch.empty_like(y)
+        step(torch.tensor(at, dtype=torch.int32, device="cuda"), cu.clone(), want, eager_args, other)
+        assert torch.equal(got, want[:sum(new)]), i
+        at = [a + 10 * n for a, n in zip(at, new)]
+    assert starts.tolist() == at
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(pool.codes + pool.scales, eager.codes + eager.scales))
+    pool.held = at
+    check_attention(pool, [1] * 4, Hq, BF16, most=most, seed=1)
